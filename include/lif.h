@@ -48,7 +48,7 @@ enum lif_status {
     LIF_HIP_ERROR = 4      /* a HIP runtime call failed; see lif_last_error_string (lif_state.error: a lost launch) */
 };
 
-enum lif_dtype { LIF_F32 = 0, LIF_F16 = 1 };
+enum lif_dtype { LIF_F32 = 0, LIF_F16 = 1, LIF_BF16 = 2 /* bfloat16: key-value caches only */ };
 
 /* How lif_sparse_ffn reads the cache (Section 3.3, inference over the cached rows). */
 enum lif_ffn_mode {
@@ -360,6 +360,193 @@ int lif_profile_read(const void* src_dev, size_t bytes, void* sink_dev, void* st
  */
 int lif_profile_handoff(void* scratch_dev, int32_t mode, uint32_t stamp, void* stream);
 size_t lif_profile_handoff_bytes(void);
+
+/*
+ * ---- Attention beside the FFN: a paged key-value cache -----------------------------------------------------------------
+ *
+ * The attention weights stay resident (Section 3, selective persistence); what a decode step needs beside them is the
+ * cache of keys and values.  One handle (lif_kv) = the cache of a stack of attention layers.  Per decode step the caller
+ * issues, on one HIP stream and without any host synchronisation,
+ *
+ *     lif_kv_reserve  ->  for every layer:  lif_kv_append -> lif_kv_attend
+ *
+ * and lif_kv_truncate, lif_kv_fork, lif_kv_compact between steps.  Lengths, tables and counts stay on the device, every
+ * launch has a geometry that does not depend on them, so a step can be captured into a HIP graph.
+ *
+ *   - A sequence is a slot 0..max_seqs-1.  Its tokens 0..lengths[slot]-1 lie in the pages table[slot][0..]; a page holds
+ *     page_tokens tokens of all layers.  refs[page] counts the table entries that name a page; a page with none is free.
+ *   - E is fp32, fp16 or bfloat16, n = 16 / sizeof(E) elements make 16 bytes.
+ *       keys    [layers][pages][kv_heads][page_tokens][head_dim]          E
+ *       values  [layers][pages][kv_heads][page_tokens / n][head_dim][n]   E   (n consecutive tokens of one dimension together)
+ *   - The tokens of a step are the last fresh[slot] tokens of their sequence.  A call takes `batch` rows of up to n_tokens
+ *     tokens; row i belongs to slot slots[i] (slots == NULL: slot i), its token t < fresh is at position length - fresh + t,
+ *     its tokens t >= fresh are padding: their outputs are zeros.  A slot number outside 0..max_seqs-1 makes a row of padding.
+ *     A slot must not appear in two rows of a lif_kv_append.
+ *   - Shape limits: head_dim a multiple of 8, 8..256; heads a multiple of kv_heads; page_tokens 16, 32, 64, 128 or 256;
+ *     pages at most 2^24; max_seqs at most 1024; max_pages at most 2^20; max_tokens at most 256.
+ *   - A device-detected error (lif_kv_state.error) is sticky: until lif_kv_truncate (LIF_CAPACITY, LIF_INVALID_ARG) or
+ *     lif_kv_reset (any) the other calls do nothing on the device, so a step that did not get its pages writes none.
+ *   - The library allocates no device memory.  Calls on one handle must not overlap (one stream at a time).
+ */
+typedef struct lif_kv lif_kv;
+
+enum lif_norm { LIF_NORM_NONE = 0, LIF_NORM_RMS = 1, LIF_NORM_LAYER = 2 };
+enum lif_rotary { LIF_ROTARY_HALF = 0, LIF_ROTARY_INTERLEAVED = 1 };
+/* Frequencies of the rotated pairs for contexts longer than the trained one (lif_rope_frequencies). */
+enum lif_rope_scaling {
+    LIF_ROPE_PLAIN = 0,    /* f_i = base^(-2i / rotary_dim)                                                          */
+    LIF_ROPE_LINEAR = 1,   /* positions divided by `factor`: f_i / factor                                            */
+    LIF_ROPE_BASE = 2,     /* the base raised so that the slowest pair turns `factor` times slower, the fastest as    */
+                           /* before: base * factor^(rotary_dim / (rotary_dim - 2))                                  */
+    LIF_ROPE_RAMP = 3      /* by the turns w_i = trained * f_i / 2 pi a pair makes over the trained length: pairs of at */
+                           /* least `fast` turns keep f_i, of at most `slow` turns get f_i / factor, linear between   */
+};
+
+typedef struct lif_kv_config {
+    int32_t layers;         /* attention layers that share the tables                            */
+    int32_t heads;          /* query heads                                                       */
+    int32_t kv_heads;       /* heads of keys and values; query head h reads head h / (heads / kv_heads) */
+    int32_t head_dim;
+    int32_t page_tokens;
+    int32_t pages;
+    int32_t max_seqs;
+    int32_t max_pages;      /* pages of a sequence at most: the width of the table               */
+    int32_t max_tokens;     /* new tokens per sequence and call at most                          */
+    int32_t dtype;          /* enum lif_dtype: queries, keys, values, outputs                    */
+    int32_t norm;           /* enum lif_norm: of every query and key head                        */
+    int32_t rotary;         /* enum lif_rotary: pairs (i, i + rotary_dim / 2) or (2i, 2i + 1)    */
+    int32_t rotary_dim;     /* the first rotary_dim dimensions turn: 0 (none) .. head_dim; a multiple of 16 (half), of 2 (interleaved) */
+    float norm_eps;
+    float rotary_scale;     /* factor on the rotated dimensions (1: a plain rotation)            */
+    float scale;            /* of the scores; 1 / sqrt(head_dim) as a rule                       */
+} lif_kv_config;
+
+typedef struct lif_kv_buffers {
+    void* k;                /* device, the layouts above, 16-byte aligned                        */
+    void* v;
+    int32_t* table;         /* device [max_seqs x max_pages]; -1 where no page is                */
+    int32_t* lengths;       /* device [max_seqs]                                                 */
+    int32_t* fresh;         /* device [max_seqs]                                                 */
+    int32_t* refs;          /* device [pages]                                                    */
+    const double* frequencies; /* device [rotary_dim / 2]: angle per position of a pair; NULL if rotary_dim is 0 */
+    void* workspace;        /* device, lif_kv_workspace_bytes(cfg) bytes, 256-byte aligned       */
+    size_t workspace_bytes;
+} lif_kv_buffers;
+
+typedef struct lif_kv_state {
+    int32_t used_pages;
+    int32_t error;          /* LIF_OK; LIF_CAPACITY: pages or table columns did not suffice (the call changed nothing); */
+                            /* LIF_INVALID_ARG: a lif_kv_fork on slots that it cannot take (it changed nothing);        */
+                            /* LIF_BAD_STATE: lif_kv_adopt found tables that do not fit the cache (reset it)            */
+    int32_t moved_pages;    /* pages copied by the last lif_kv_fork, lif_kv_compact or lif_kv_reserve               */
+} lif_kv_state;
+
+/* Rows of a lif_kv_append: row r = i * n_tokens + t is token t of batch row i, its heads one after the other at r * stride. */
+typedef struct lif_kv_rows {
+    const void* q;          /* [heads x head_dim] E per row                                      */
+    const void* k;          /* [kv_heads x head_dim] E per row                                   */
+    const void* v;
+    void* q_out;            /* [heads x head_dim] E per row, written                             */
+    int64_t q_stride, k_stride, v_stride, q_out_stride;  /* elements between rows, multiples of 16 bytes */
+    const float* q_weight;  /* [head_dim] fp32, device; NULL: ones.  Unused without a norm       */
+    const float* q_bias;    /* [head_dim] fp32; NULL: zeros.  LIF_NORM_LAYER only                */
+    const float* k_weight;
+    const float* k_bias;
+    const int32_t* positions; /* device [batch x n_tokens], angles of rotation; NULL: the position in the sequence */
+    const int32_t* slots;   /* device [batch] or NULL                                            */
+    int32_t batch;
+    int32_t n_tokens;
+} lif_kv_rows;
+
+/* Rows of a lif_kv_attend, laid out the same. */
+typedef struct lif_kv_query {
+    const void* q;          /* [heads x head_dim] E per row                                      */
+    void* out;              /* [heads x head_dim] E per row, written                             */
+    float* lse;             /* [batch x n_tokens x heads] fp32, written: log of the sum of e^score (-inf: nothing visible); or NULL */
+    int64_t q_stride, out_stride;
+    const int32_t* slots;   /* device [batch] or NULL                                            */
+    const int32_t* starts;  /* device [batch]: first visible position; NULL: 0                   */
+    const uint64_t* tree;   /* device [batch x n_tokens], n_tokens <= 64: bit u of word t: new token t sees new token u;
+                             * NULL: it sees those with u <= t                                   */
+    int32_t batch;
+    int32_t n_tokens;
+    int32_t window;         /* positions more than window - 1 before a token's own are not visible to it; 0: all are */
+} lif_kv_query;
+
+/* Bytes of scratch lif_kv_create needs for this configuration (0 if cfg is invalid). */
+size_t lif_kv_workspace_bytes(const lif_kv_config* cfg);
+
+/* As lif_create: validates, enqueues nothing; call lif_kv_reset (or write the tables and call lif_kv_adopt) first. */
+int lif_kv_create(const lif_kv_config* cfg, const lif_kv_buffers* buf, lif_kv** out);
+int lif_kv_destroy(lif_kv* kv);
+
+/* No sequences, all pages free, no error.  The pages' contents are not touched. */
+int lif_kv_reset(lif_kv* kv, void* stream);
+
+/*
+ * Takes over table, lengths and fresh as the caller has written them (a cache that was filled elsewhere): counts refs, finds
+ * the free pages, writes -1 behind the pages in use.  Lengths, fresh counts (0..length) or pages out of range: LIF_BAD_STATE.
+ */
+int lif_kv_adopt(lif_kv* kv, void* stream);
+
+/*
+ * Pages for counts[slot] more tokens of every slot (device [max_seqs]; negative counts as 0): lengths grow, fresh[slot] =
+ * counts[slot].  The lowest free pages are taken, by slot and then by position.  Where tokens are added to a partly filled
+ * page that other sequences hold too (possible after a truncation into forked pages), the slot gets a copy of it first, in the
+ * same order; a page that everyone has left that way is free after the call.
+ * Too few pages, or more than max_pages for a sequence: LIF_CAPACITY, nothing changes.
+ */
+int lif_kv_reserve(lif_kv* kv, const int32_t* counts_dev, void* stream);
+
+/*
+ * Shortens every slot to lengths[slot] tokens (device [max_seqs]; negative or beyond its length: unchanged; 0 ends the sequence).
+ * Pages no longer named by any table entry are free again; fresh = 0 for all slots.  Clears LIF_CAPACITY and LIF_INVALID_ARG.
+ */
+int lif_kv_truncate(lif_kv* kv, const int32_t* lengths_dev, void* stream);
+
+/*
+ * Slot dst[i] becomes a copy of slot src[i], i < n <= max_seqs (device arrays): it shares the full pages (refs + 1) and gets a
+ * copy of the partly filled last one, in the lowest free pages, by i.  fresh[dst] = 0.  A destination must be empty and named once;
+ * sources are read as they were before the call.  Otherwise, or for numbers out of range: LIF_INVALID_ARG, nothing changes; too
+ * few pages: LIF_CAPACITY, nothing changes.
+ */
+int lif_kv_fork(lif_kv* kv, const int32_t* src_dev, const int32_t* dst_dev, int32_t n, void* stream);
+
+/*
+ * Makes the pool dense: with U pages in use, the j-th lowest free page below U receives the j-th highest used page at or
+ * above U (contents of all layers, refs, table entries).  Afterwards pages 0..U-1 are in use.
+ */
+int lif_kv_compact(lif_kv* kv, void* stream);
+
+/*
+ * Queries and keys: norm per head, then rotation (both in fp32, angle = position * frequency in fp64, rounded once to E); keys and values
+ * go to their pages of `layer`, queries to q_out.
+ *   RMS    x / sqrt(mean x^2 + eps) * weight            LAYER  (x - mean) / sqrt(var + eps) * weight + bias
+ *   rotation by a of a pair (x, y): (x cos a - y sin a, x sin a + y cos a) * rotary_scale
+ * q_out may be q itself with the same stride.
+ */
+int lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* rows, void* stream);
+
+/*
+ * Attention of the new tokens over their sequences' cached tokens (their own included):
+ *   out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m),   s_j = scale * q . k_j,  over the visible positions j
+ * position j of a sequence of n tokens, f of them new, is visible to new token t iff  starts <= j,  j > n - f + t - window (if a
+ * window is given), and j < n - f or new token j - (n - f) is visible to t (tree, or causal).  Nothing visible: zeros.
+ * Keys and values at positions that a token does not see never reach its output, whatever they hold.
+ * Scores, sums and outputs are accumulated in fp32 and rounded once to E; the weights e^(s_j - m) are rounded to E for the product with the
+ * values.  Every sum has a fixed order for given lengths: results are reproducible bit for bit.
+ */
+int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* stream);
+
+/* Synchronises `stream`, then copies the device-side state to the host. */
+int lif_kv_get_state(lif_kv* kv, lif_kv_state* out, void* stream);
+
+/*
+ * Frequencies of the rotated pairs, host only: out[0 .. rotary_dim / 2).  rotary_dim a positive even number, base > 0; factor > 0 for the
+ * scaled kinds (LIF_ROPE_BASE: rotary_dim > 2); LIF_ROPE_RAMP: trained > 0, fast > slow.
+ */
+int lif_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double trained, double slow, double fast,
+                         double* out);
 
 /* Message of the last LIF_HIP_ERROR / LIF_INVALID_ARG on the calling thread. */
 const char* lif_last_error_string(void);

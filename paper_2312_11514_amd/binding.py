@@ -12,9 +12,12 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "liblif.so")
 
 LIF_OK, LIF_INVALID_ARG, LIF_BAD_STATE, LIF_CAPACITY, LIF_HIP_ERROR = 0, 1, 2, 3, 4
-LIF_F32, LIF_F16 = 0, 1
+LIF_F32, LIF_F16, LIF_BF16 = 0, 1, 2
 FFN_SKIP_DEAD, FFN_FULL_BUNDLE = 0, 1
 PRED_LOWRANK, PRED_GATE = 0, 1
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP = 0, 1, 2, 3
 KERNEL_NAMES = ("predict_xa", "predict_mask", "window", "load", "ffn_up", "ffn_down")
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "BAD_STATE", 3: "CAPACITY", 4: "HIP_ERROR"}
 
@@ -41,6 +44,33 @@ class LifState(C.Structure):
 class LifCounters(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in ("steps", "added", "removed", "rows_moved", "h2d_bytes",
                                           "ffn_calls", "ffn_rows", "ffn_active")]
+
+
+class LifKvConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layers", "heads", "kv_heads", "head_dim", "page_tokens", "pages", "max_seqs", "max_pages",
+                                         "max_tokens", "dtype", "norm", "rotary", "rotary_dim")] + \
+        [(n, C.c_float) for n in ("norm_eps", "rotary_scale", "scale")]
+
+
+class LifKvBuffers(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "table", "lengths", "fresh", "refs", "frequencies", "workspace")] + \
+        [("workspace_bytes", C.c_size_t)]
+
+
+class LifKvState(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("used_pages", "error", "moved_pages")]
+
+
+class LifKvRows(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "q_out")] + \
+        [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")] + \
+        [(n, C.c_void_p) for n in ("q_weight", "q_bias", "k_weight", "k_bias", "positions", "slots")] + \
+        [("batch", C.c_int32), ("n_tokens", C.c_int32)]
+
+
+class LifKvQuery(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "lse")] + [("q_stride", C.c_int64), ("out_stride", C.c_int64)] + \
+        [(n, C.c_void_p) for n in ("slots", "starts", "tree")] + [(n, C.c_int32) for n in ("batch", "n_tokens", "window")]
 
 
 EXPORTS = {
@@ -70,6 +100,19 @@ EXPORTS = {
     "lif_profile_handoff_bytes": (C.c_size_t, []),
     "lif_profile_begin": (C.c_int, [C.c_void_p, C.c_int32]),
     "lif_profile_collect": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.c_void_p]),
+    "lif_kv_workspace_bytes": (C.c_size_t, [C.POINTER(LifKvConfig)]),
+    "lif_kv_create": (C.c_int, [C.POINTER(LifKvConfig), C.POINTER(LifKvBuffers), C.POINTER(C.c_void_p)]),
+    "lif_kv_destroy": (C.c_int, [C.c_void_p]),
+    "lif_kv_reset": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "lif_kv_adopt": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "lif_kv_reserve": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "lif_kv_truncate": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
+    "lif_kv_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
+    "lif_kv_compact": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "lif_kv_append": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(LifKvRows), C.c_void_p]),
+    "lif_kv_attend": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(LifKvQuery), C.c_void_p]),
+    "lif_kv_get_state": (C.c_int, [C.c_void_p, C.POINTER(LifKvState), C.c_void_p]),
+    "lif_rope_frequencies": (C.c_int, [C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4 + [C.POINTER(C.c_double)]),
 }
 
 _lib = None

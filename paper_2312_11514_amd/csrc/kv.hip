@@ -1,0 +1,298 @@
+// C ABI of the paged key-value cache and its attention (see include/lif.h for the contract of every call).
+// Host side only: argument checks, workspace layout, launch geometry.
+#include "../../include/lif.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "lif_host.h"
+#include "lif_kv.h"
+#include "lif_kv_pages.h"
+#include "lif_kv_append.h"
+#include "lif_kv_attend.h"
+
+using namespace lif;
+
+struct lif_kv {
+    lif_kv_config cfg;
+    KvView view;
+    const double* frequencies;
+    float* parts;
+    float2* stats;
+};
+
+namespace {
+
+constexpr long long kMaxPositions = 1 << 24;     // of a sequence: the steps of 1024 of them are counted in 32 bits
+constexpr int kMoveBlocks = 2048;                // 8 workgroups of copies per compute unit
+constexpr int kCopyBlocks = 256;                 // ... behind lif_kv_reserve, which has a page to copy once in a while
+
+size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+int elem_bytes(int dtype) { return dtype == LIF_F32 ? 4 : 2; }
+int log_of(int v) { return __builtin_ctz((unsigned)v); }
+
+bool config_ok(const lif_kv_config* c, const char** why) {
+    *why = "";
+    if (!c) return (*why = "null config", false);
+    if (c->dtype != LIF_F32 && c->dtype != LIF_F16 && c->dtype != LIF_BF16) return (*why = "dtype", false);
+    if (c->layers < 1 || c->layers > 65536) return (*why = "layers", false);
+    if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8) return (*why = "head_dim must be a multiple of 8 in 8..256", false);
+    if (c->kv_heads < 1 || c->heads < c->kv_heads || c->heads % c->kv_heads || c->heads > 65536)
+        return (*why = "heads must be a multiple of kv_heads", false);
+    if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1)))
+        return (*why = "page_tokens must be 16, 32, 64, 128 or 256", false);
+    if (c->pages < 1 || c->pages > 1 << 24) return (*why = "pages must be in 1..2^24", false);
+    if (c->max_seqs < 1 || c->max_seqs > kKvMaxSeqs) return (*why = "max_seqs must be in 1..1024", false);
+    if (c->max_pages < 1 || c->max_pages > 1 << 20 || (long long)c->max_pages * c->page_tokens > kMaxPositions)
+        return (*why = "max_pages must be in 1..2^20, and a sequence of at most 2^24 tokens", false);
+    if (c->max_tokens < 1 || c->max_tokens > 256) return (*why = "max_tokens must be in 1..256", false);
+    if (c->norm != LIF_NORM_NONE && c->norm != LIF_NORM_RMS && c->norm != LIF_NORM_LAYER) return (*why = "norm", false);
+    if (c->rotary != LIF_ROTARY_HALF && c->rotary != LIF_ROTARY_INTERLEAVED) return (*why = "rotary", false);
+    if (c->rotary_dim < 0 || c->rotary_dim > c->head_dim || c->rotary_dim % (c->rotary == LIF_ROTARY_HALF ? 16 : 2))
+        return (*why = "rotary_dim must be 0..head_dim, a multiple of 16 (half layout) or 2 (interleaved)", false);
+    if (!std::isfinite(c->scale) || !std::isfinite(c->rotary_scale) || !(c->norm_eps >= 0.f) || !std::isfinite(c->norm_eps))
+        return (*why = "scale, rotary_scale and norm_eps must be finite, norm_eps not negative", false);
+    return true;
+}
+
+struct KvLayout {
+    size_t state, free_bits, moves, remap, stats, parts, total;
+};
+
+int rows_of_block(const lif_kv_config& c, int n_tokens) {
+    return 16 * attend_tiles(n_tokens * (c.heads / c.kv_heads), attend_dim_pad(c.head_dim));
+}
+
+KvLayout make_layout(const lif_kv_config& c) {
+    KvLayout L;
+    size_t off = 0;
+    L.state = off;
+    off = align_up(off + sizeof(KvState), 256);
+    L.free_bits = off;
+    off = align_up(off + sizeof(unsigned long long) * ((size_t)(c.pages + 63) / 64), 256);
+    L.moves = off;
+    off = align_up(off + sizeof(int2) * c.pages, 256);
+    L.remap = off;
+    off = align_up(off + sizeof(int32_t) * std::max(c.pages, c.max_seqs), 256);
+    const size_t rows = (size_t)2 * kAttendGroups * rows_of_block(c, c.max_tokens);
+    L.stats = off;
+    off = align_up(off + sizeof(float2) * rows, 256);
+    L.parts = off;
+    off = align_up(off + sizeof(float) * rows * attend_dim_pad(c.head_dim), 256);
+    L.total = off;
+    return L;
+}
+
+int launched() {
+    hipError_t e = hipGetLastError();
+    return e == hipSuccess ? LIF_OK : fail(LIF_HIP_ERROR, "launch: %s", hipGetErrorString(e));
+}
+
+int batch_ok(const lif_kv* kv, int32_t layer, int32_t batch, int32_t n_tokens) {
+    if (layer < 0 || layer >= kv->cfg.layers) return fail(LIF_INVALID_ARG, "layer out of range");
+    if (batch < 1 || batch > kKvMaxSeqs) return fail(LIF_INVALID_ARG, "batch must be in 1..1024");
+    if (n_tokens < 1 || n_tokens > kv->cfg.max_tokens) return fail(LIF_INVALID_ARG, "n_tokens must be in 1..max_tokens");
+    return LIF_OK;
+}
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// a stride of at least one row, in whole 16 bytes
+int stride_ok(const lif_kv* kv, int64_t stride, int heads) {
+    const int per = 16 / elem_bytes(kv->cfg.dtype);
+    if (stride < (int64_t)heads * kv->cfg.head_dim || stride % per || stride > (int64_t)1 << 40)
+        return fail(LIF_INVALID_ARG, "a row stride must hold the heads and be a multiple of 16 bytes");
+    return LIF_OK;
+}
+
+}  // namespace
+
+#define LIF_TRY(call)              \
+    do {                           \
+        int rc_ = (call);          \
+        if (rc_ != LIF_OK) return rc_; \
+    } while (0)
+
+extern "C" {
+
+size_t lif_kv_workspace_bytes(const lif_kv_config* cfg) {
+    const char* why;
+    return config_ok(cfg, &why) ? make_layout(*cfg).total : 0;
+}
+
+int lif_kv_create(const lif_kv_config* cfg, const lif_kv_buffers* buf, lif_kv** out) {
+    const char* why;
+    if (!cfg || !buf || !out) return fail(LIF_INVALID_ARG, "null pointer");
+    if (!config_ok(cfg, &why)) return fail(LIF_INVALID_ARG, "configuration: %s", why);
+    if (!buf->k || !buf->v || !buf->table || !buf->lengths || !buf->fresh || !buf->refs || !buf->workspace)
+        return fail(LIF_INVALID_ARG, "null buffer");
+    if (cfg->rotary_dim > 0 && !buf->frequencies) return fail(LIF_INVALID_ARG, "rotary_dim without frequencies");
+    if (!aligned16(buf->k) || !aligned16(buf->v)) return fail(LIF_INVALID_ARG, "keys and values must be 16-byte aligned");
+    const KvLayout L = make_layout(*cfg);
+    if (buf->workspace_bytes < L.total || reinterpret_cast<uintptr_t>(buf->workspace) % 256)
+        return fail(LIF_INVALID_ARG, "workspace too small or not 256-byte aligned");
+    lif_kv* kv = new (std::nothrow) lif_kv;
+    if (!kv) return fail(LIF_INVALID_ARG, "out of host memory");
+    char* w = static_cast<char*>(buf->workspace);
+    kv->cfg = *cfg;
+    KvView& v = kv->view;
+    v.k = static_cast<char*>(buf->k);
+    v.v = static_cast<char*>(buf->v);
+    v.table = buf->table;
+    v.lengths = buf->lengths;
+    v.fresh = buf->fresh;
+    v.refs = buf->refs;
+    v.st = reinterpret_cast<KvState*>(w + L.state);
+    v.free_bits = reinterpret_cast<unsigned long long*>(w + L.free_bits);
+    v.moves = reinterpret_cast<int2*>(w + L.moves);
+    v.remap = reinterpret_cast<int32_t*>(w + L.remap);
+    v.pages = cfg->pages;
+    v.max_seqs = cfg->max_seqs;
+    v.max_pages = cfg->max_pages;
+    v.log_page = log_of(cfg->page_tokens);
+    v.layers = cfg->layers;
+    v.page_bytes = (unsigned long long)cfg->kv_heads * cfg->page_tokens * cfg->head_dim * elem_bytes(cfg->dtype);
+    kv->frequencies = buf->frequencies;
+    kv->parts = reinterpret_cast<float*>(w + L.parts);
+    kv->stats = reinterpret_cast<float2*>(w + L.stats);
+    *out = kv;
+    return LIF_OK;
+}
+
+int lif_kv_destroy(lif_kv* kv) {
+    delete kv;
+    return LIF_OK;
+}
+
+int lif_kv_reset(lif_kv* kv, void* stream) {
+    if (!kv) return fail(LIF_INVALID_ARG, "null handle");
+    const long long most = std::max<long long>(kv->cfg.pages, (long long)kv->cfg.max_seqs * kv->cfg.max_pages);
+    hipLaunchKernelGGL((k_kv_clear<true>), dim3((unsigned)std::min<long long>((most + 255) / 256, 1024)), dim3(256), 0, (hipStream_t)stream, kv->view);
+    return launched();
+}
+
+int lif_kv_adopt(lif_kv* kv, void* stream) {
+    if (!kv) return fail(LIF_INVALID_ARG, "null handle");
+    hipLaunchKernelGGL((k_kv_clear<false>), dim3(std::min((kv->cfg.pages + 255) / 256, 1024)), dim3(256), 0, (hipStream_t)stream, kv->view);
+    hipLaunchKernelGGL(k_kv_adopt, dim3(kv->cfg.max_seqs), dim3(256), 0, (hipStream_t)stream, kv->view);
+    return launched();
+}
+
+int lif_kv_reserve(lif_kv* kv, const int32_t* counts_dev, void* stream) {
+    if (!kv || !counts_dev) return fail(LIF_INVALID_ARG, "null pointer");
+    hipLaunchKernelGGL(k_kv_reserve, dim3(1), dim3(kKvPlanThreads), 0, (hipStream_t)stream, kv->view, counts_dev);
+    hipLaunchKernelGGL((k_kv_move<KV_COPY>), dim3(kCopyBlocks), dim3(256), 0, (hipStream_t)stream, kv->view, nullptr, nullptr, 0);
+    return launched();
+}
+
+int lif_kv_truncate(lif_kv* kv, const int32_t* lengths_dev, void* stream) {
+    if (!kv || !lengths_dev) return fail(LIF_INVALID_ARG, "null pointer");
+    hipLaunchKernelGGL(k_kv_truncate, dim3(kv->cfg.max_seqs), dim3(256), 0, (hipStream_t)stream, kv->view, lengths_dev);
+    return launched();
+}
+
+int lif_kv_fork(lif_kv* kv, const int32_t* src_dev, const int32_t* dst_dev, int32_t n, void* stream) {
+    if (!kv || !src_dev || !dst_dev) return fail(LIF_INVALID_ARG, "null pointer");
+    if (n < 1 || n > kv->cfg.max_seqs) return fail(LIF_INVALID_ARG, "n must be in 1..max_seqs");
+    hipLaunchKernelGGL(k_kv_fork, dim3(1), dim3(kKvPlanThreads), 0, (hipStream_t)stream, kv->view, src_dev, dst_dev, n);
+    hipLaunchKernelGGL((k_kv_move<KV_FORK>), dim3(n + kMoveBlocks), dim3(256), 0, (hipStream_t)stream, kv->view, src_dev, dst_dev, n);
+    return launched();
+}
+
+int lif_kv_compact(lif_kv* kv, void* stream) {
+    if (!kv) return fail(LIF_INVALID_ARG, "null handle");
+    hipLaunchKernelGGL(k_kv_compact, dim3(1), dim3(kKvPlanThreads), 0, (hipStream_t)stream, kv->view);
+    hipLaunchKernelGGL((k_kv_move<KV_COMPACT>), dim3(kv->cfg.max_seqs + kMoveBlocks), dim3(256), 0, (hipStream_t)stream, kv->view, nullptr, nullptr,
+                       kv->cfg.max_seqs);
+    return launched();
+}
+
+int lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* rows, void* stream) {
+    if (!kv || !rows) return fail(LIF_INVALID_ARG, "null pointer");
+    const lif_kv_config& c = kv->cfg;
+    LIF_TRY(batch_ok(kv, layer, rows->batch, rows->n_tokens));
+    if (!rows->q || !rows->k || !rows->v || !rows->q_out) return fail(LIF_INVALID_ARG, "null rows");
+    if (!aligned16(rows->q) || !aligned16(rows->k) || !aligned16(rows->v) || !aligned16(rows->q_out))
+        return fail(LIF_INVALID_ARG, "rows must be 16-byte aligned");
+    LIF_TRY(stride_ok(kv, rows->q_stride, c.heads));
+    LIF_TRY(stride_ok(kv, rows->q_out_stride, c.heads));
+    LIF_TRY(stride_ok(kv, rows->k_stride, c.kv_heads));
+    LIF_TRY(stride_ok(kv, rows->v_stride, c.kv_heads));
+    AppendArgs a{static_cast<const char*>(rows->q), static_cast<const char*>(rows->k), static_cast<const char*>(rows->v),
+                 static_cast<char*>(rows->q_out), rows->q_stride, rows->k_stride, rows->v_stride, rows->q_out_stride,
+                 rows->q_weight, rows->q_bias, rows->k_weight, rows->k_bias, kv->frequencies, rows->positions, rows->slots,
+                 rows->n_tokens, c.heads, c.kv_heads, c.head_dim, layer, c.rotary_dim, c.norm, 0, c.norm_eps, c.rotary_scale};
+    const int count = rows->batch * rows->n_tokens, all = c.heads + 2 * c.kv_heads;
+    const int at_once = 256 / lanes_of_head(c.head_dim, 16 / elem_bytes(c.dtype));
+    // few rows: a workgroup per heads_at_once heads, to have the whole chip at it; many: all heads of a row by one, angles computed once
+    const int wanted = std::max(1, 2048 / count), blocks = std::min((all + at_once - 1) / at_once, wanted);
+    a.heads_per_block = ((all + blocks - 1) / blocks + at_once - 1) / at_once * at_once;
+    const int grid = (all + a.heads_per_block - 1) / a.heads_per_block;
+    const bool interleaved = c.rotary == LIF_ROTARY_INTERLEAVED;
+    hipStream_t s = (hipStream_t)stream;
+    if (c.dtype == LIF_F32) launch_append_f32(kv->view, a, interleaved, count, grid, s);
+    else if (c.dtype == LIF_F16) launch_append_f16(kv->view, a, interleaved, count, grid, s);
+    else launch_append_bf16(kv->view, a, interleaved, count, grid, s);
+    return launched();
+}
+
+int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* stream) {
+    if (!kv || !query) return fail(LIF_INVALID_ARG, "null pointer");
+    const lif_kv_config& c = kv->cfg;
+    LIF_TRY(batch_ok(kv, layer, query->batch, query->n_tokens));
+    if (!query->q || !query->out) return fail(LIF_INVALID_ARG, "null rows");
+    if (!aligned16(query->q) || !aligned16(query->out)) return fail(LIF_INVALID_ARG, "rows must be 16-byte aligned");
+    LIF_TRY(stride_ok(kv, query->q_stride, c.heads));
+    LIF_TRY(stride_ok(kv, query->out_stride, c.heads));
+    if (query->window < 0) return fail(LIF_INVALID_ARG, "window must not be negative");
+    if (query->tree && query->n_tokens > 64) return fail(LIF_INVALID_ARG, "a tree has at most 64 tokens");
+    const int share = c.heads / c.kv_heads, rows = query->n_tokens * share, pad = attend_dim_pad(c.head_dim), tiles = attend_tiles(rows, pad);
+    const int blocks = (rows + 16 * tiles - 1) / (16 * tiles);
+    AttendArgs a{static_cast<const char*>(query->q), static_cast<char*>(query->out), query->lse, query->q_stride, query->out_stride,
+                 query->slots, query->starts, reinterpret_cast<const unsigned long long*>(query->tree), kv->parts, kv->stats, query->batch,
+                 query->n_tokens, c.heads, c.kv_heads, share, c.head_dim, layer, query->window, blocks, c.scale * kLog2e};
+    const int step = 4 * 16 / elem_bytes(c.dtype) * kAttendWaves;
+    const long long most = (long long)query->batch * c.kv_heads * blocks * (((long long)c.max_pages * c.page_tokens + step - 1) / step + 1);
+    const int groups = (int)std::min<long long>(kAttendGroups, most);
+    hipStream_t s = (hipStream_t)stream;
+    if (c.dtype == LIF_F32) launch_attend_f32(kv->view, a, pad, tiles, groups, s);
+    else if (c.dtype == LIF_F16) launch_attend_f16(kv->view, a, pad, tiles, groups, s);
+    else launch_attend_bf16(kv->view, a, pad, tiles, groups, s);
+    return launched();
+}
+
+int lif_kv_get_state(lif_kv* kv, lif_kv_state* out, void* stream) {
+    if (!kv || !out) return fail(LIF_INVALID_ARG, "null pointer");
+    KvState st;
+    LIF_HIP(hipMemcpyAsync(&st, kv->view.st, sizeof(st), hipMemcpyDeviceToHost, (hipStream_t)stream));
+    LIF_HIP(hipStreamSynchronize((hipStream_t)stream));
+    *out = lif_kv_state{st.used, st.error, st.n_moves};
+    return LIF_OK;
+}
+
+int lif_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double trained, double slow, double fast, double* out) {
+    if (!out) return fail(LIF_INVALID_ARG, "null pointer");
+    if (rotary_dim < 2 || rotary_dim % 2 || rotary_dim > 65536) return fail(LIF_INVALID_ARG, "rotary_dim must be a positive even number");
+    if (!(base > 0) || !std::isfinite(base)) return fail(LIF_INVALID_ARG, "base must be positive");
+    if (scaling < LIF_ROPE_PLAIN || scaling > LIF_ROPE_RAMP) return fail(LIF_INVALID_ARG, "scaling");
+    if (scaling != LIF_ROPE_PLAIN && (!(factor > 0) || !std::isfinite(factor))) return fail(LIF_INVALID_ARG, "factor must be positive");
+    if (scaling == LIF_ROPE_BASE && rotary_dim == 2) return fail(LIF_INVALID_ARG, "a single pair has no base to raise");
+    if (scaling == LIF_ROPE_RAMP && (!(trained > 0) || !std::isfinite(trained) || !(fast > slow) || !std::isfinite(fast - slow)))
+        return fail(LIF_INVALID_ARG, "the ramp needs a trained length and fast > slow");
+    if (scaling == LIF_ROPE_BASE) base *= std::pow(factor, rotary_dim / (rotary_dim - 2.0));
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rotary_dim);
+        if (scaling == LIF_ROPE_LINEAR) f /= factor;
+        if (scaling == LIF_ROPE_RAMP) {
+            const double turns = trained * f / 6.283185307179586476925, keep = std::min(1.0, std::max(0.0, (turns - slow) / (fast - slow)));
+            f = keep * f + (1.0 - keep) * f / factor;
+        }
+        out[i] = f;
+    }
+    return LIF_OK;
+}
+
+}  // extern "C"

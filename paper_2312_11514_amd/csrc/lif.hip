@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "lif_common.h"
+#include "lif_host.h"
 #include "lif_ffn.h"
 #include "lif_ffn_down1.h"
 #include "lif_ffn_one.h"
@@ -27,20 +28,14 @@ using namespace lif;
 constexpr size_t kStaticScratchBytes = 5u << 20;
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
-
-int fail(int code, const char* fmt, const char* detail = "") {
+int lif::fail(int code, const char* fmt, const char* detail) {
     snprintf(g_err, sizeof(g_err), fmt, detail);
     return code;
 }
 
-#define LIF_HIP(call)                                                             \
-    do {                                                                          \
-        hipError_t e_ = (call);                                                   \
-        if (e_ != hipSuccess) return fail(LIF_HIP_ERROR, #call ": %s", hipGetErrorString(e_)); \
-    } while (0)
+namespace {
 
 // Bytes of host reads that lif_step keeps outstanding: pairs of loader workgroups (one bundle in flight per pair) =
 // kStepInflightBytes / bundle bytes, within 5..kStepPairs.  The link needs about 128 KiB (56 GB/s at 1.5 to 2.4 us); the rest
@@ -684,7 +679,7 @@ int check_launch() {
 
 extern "C" {
 
-int lif_version(void) { return 2; }
+int lif_version(void) { return 3; }
 
 const char* lif_last_error_string(void) { return g_err; }
 

@@ -1,0 +1,172 @@
+"""Paged key-value cache and its attention: ctypes binding of the lif_kv calls of include/lif.h, argument marshalling only.
+
+    kv = KVCache(layers=32, heads=32, kv_heads=8, head_dim=128, page_tokens=16, pages=4096, max_seqs=64, max_pages=512)
+    kv.reserve(counts)                            # pages for this step's tokens, once for all layers
+    for l in range(32):
+        kv.append(l, q, k, v, q_out)              # norms, rotation, keys and values into their pages
+        kv.attend(l, q_out, out)
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+from . import binding as _b
+from .binding import LIF_INVALID_ARG, LifError
+
+_DTYPES = {"f32": _b.LIF_F32, "f16": _b.LIF_F16, "bf16": _b.LIF_BF16}
+
+
+def rope_frequencies(rotary_dim, base=10000.0, scaling=_b.ROPE_PLAIN, factor=1.0, trained=0.0, slow=1.0, fast=32.0):
+    """lif_rope_frequencies: angle per position of every rotated pair, a float64 tensor on the CPU."""
+    import torch
+    out = torch.zeros(max(1, int(rotary_dim) // 2), dtype=torch.float64)
+    _b._check(_b.load_library().lif_rope_frequencies(int(rotary_dim), float(base), int(scaling), float(factor), float(trained), float(slow),
+                                                     float(fast), C.cast(out.data_ptr(), C.POINTER(C.c_double))))
+    return out
+
+
+def _refuse(message):
+    raise LifError(LIF_INVALID_ARG, message)
+
+
+class KVCache:
+    """The cache of a stack of attention layers behind the C ABI.  Owns (through torch) every array the library uses; `table`, `lengths`,
+    `fresh` and `refs` may be read at any time, and written before adopt().  All calls but state() enqueue on torch's current stream and
+    return immediately.
+
+    frequencies: float64 tensor [rotary_dim / 2] (rope_frequencies), needed if rotary_dim > 0.  scale: of the scores, 1 / sqrt(head_dim) if None.
+    """
+
+    def __init__(self, *, layers, heads, kv_heads, head_dim, page_tokens, pages, max_seqs, max_pages, max_tokens=1, dtype="f16",
+                 norm=_b.NORM_NONE, norm_eps=1e-5, rotary=_b.ROTARY_HALF, rotary_dim=0, rotary_scale=1.0, frequencies=None, scale=None,
+                 device="cuda"):
+        import torch
+        self.lib = _b.load_library()
+        self.torch = torch
+        if dtype not in _DTYPES:
+            _refuse("dtype must be f32, f16 or bf16")
+        self.cfg = _b.LifKvConfig(layers, heads, kv_heads, head_dim, page_tokens, pages, max_seqs, max_pages, max_tokens, _DTYPES[dtype],
+                                  norm, rotary, rotary_dim, norm_eps, rotary_scale, head_dim ** -0.5 if scale is None else scale)
+        ws_bytes = self.lib.lif_kv_workspace_bytes(C.byref(self.cfg))
+        if ws_bytes == 0:
+            _refuse("configuration rejected by lif_kv_workspace_bytes")
+        self.tdtype = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+        if rotary_dim and (frequencies is None or frequencies.dtype != torch.float64 or frequencies.numel() != rotary_dim // 2):
+            _refuse("frequencies must be a float64 tensor of rotary_dim / 2 elements")
+        n = 4 if dtype == "f32" else 8
+        new = lambda shape, dt: torch.empty(shape, dtype=dt, device=device)
+        self.k = new((layers, pages, kv_heads, page_tokens, head_dim), self.tdtype)
+        self.v = new((layers, pages, kv_heads, page_tokens // n, head_dim, n), self.tdtype)
+        self.table = new((max_seqs, max_pages), torch.int32)
+        self.lengths, self.fresh = new((max_seqs,), torch.int32), new((max_seqs,), torch.int32)
+        self.refs = new((pages,), torch.int32)
+        self.frequencies = frequencies.to(device).contiguous() if rotary_dim else None
+        self.workspace = new((ws_bytes,), torch.uint8)
+        self.buf = _b.LifKvBuffers(*[_b._ptr(t) for t in (self.k, self.v, self.table, self.lengths, self.fresh, self.refs, self.frequencies,
+                                                          self.workspace)], ws_bytes)
+        h = C.c_void_p()
+        _b._check(self.lib.lif_kv_create(C.byref(self.cfg), C.byref(self.buf), C.byref(h)))
+        self.handle = h
+        self.reset()
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self.lib.lif_kv_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # ---- argument checks -------------------------------------------------------------------------------------------------
+    def _ints(self, t, count, what):
+        if t.dtype != self.torch.int32 or t.numel() != count or not t.is_contiguous() or t.device != self.table.device:
+            _refuse(f"{what} must be a contiguous int32 tensor of {count} elements beside the cache")
+        return t.data_ptr()
+
+    def _rows(self, t, heads, what, like=None):
+        """[batch, tokens, heads, head_dim] with contiguous heads; any stride between tokens.  Returns the stride."""
+        b, n, h, d = t.shape if t.dim() == 4 else (0, 0, 0, 0)
+        sb, sn, sh, sd = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
+        if b == 1:
+            sb = n * sn
+        if n == 1:
+            sn = sb
+        if b == 1 and n == 1:
+            sn = sb = h * d
+        if h == 1:
+            sh = d
+        if (h != heads or d != self.cfg.head_dim or t.dtype != self.tdtype or sd != 1 or sh != d or sb != n * sn or
+                t.device != self.table.device or (like is not None and (b, n) != like)):
+            _refuse(f"{what} must be [batch, tokens, {heads}, {self.cfg.head_dim}] of the cache's type, heads contiguous, tokens at one stride")
+        return sn
+
+    def _norm(self, t, what):
+        if t is None:
+            return None
+        if t.dtype != self.torch.float32 or t.numel() != self.cfg.head_dim or not t.is_contiguous() or t.device != self.table.device:
+            _refuse(f"{what} must be a contiguous float32 tensor of head_dim elements beside the cache")
+        return t.data_ptr()
+
+    # ---- the C-ABI calls, same names -------------------------------------------------------------------------------------
+    def reset(self):
+        _b._check(self.lib.lif_kv_reset(self.handle, _b._stream()))
+
+    def adopt(self):
+        _b._check(self.lib.lif_kv_adopt(self.handle, _b._stream()))
+
+    def reserve(self, counts):
+        _b._check(self.lib.lif_kv_reserve(self.handle, self._ints(counts, self.cfg.max_seqs, "counts"), _b._stream()))
+
+    def truncate(self, lengths):
+        _b._check(self.lib.lif_kv_truncate(self.handle, self._ints(lengths, self.cfg.max_seqs, "lengths"), _b._stream()))
+
+    def fork(self, src, dst):
+        n = src.numel()
+        _b._check(self.lib.lif_kv_fork(self.handle, self._ints(src, n, "src"), self._ints(dst, n, "dst"), n, _b._stream()))
+
+    def compact(self):
+        _b._check(self.lib.lif_kv_compact(self.handle, _b._stream()))
+
+    def append(self, layer, q, k, v, q_out, norm=None, positions=None, slots=None):
+        """q, q_out [batch, tokens, heads, head_dim], k, v [batch, tokens, kv_heads, head_dim].  norm: (q weight, q bias, k weight, k bias),
+        each float32 [head_dim] or None."""
+        shape = tuple(q.shape[:2])
+        qw, qb, kw, kb = norm if norm is not None else (None, None, None, None)
+        rows = _b.LifKvRows(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), self._rows(q, self.cfg.heads, "q"),
+            self._rows(k, self.cfg.kv_heads, "k", shape), self._rows(v, self.cfg.kv_heads, "v", shape),
+            self._rows(q_out, self.cfg.heads, "q_out", shape), self._norm(qw, "q weight"), self._norm(qb, "q bias"), self._norm(kw, "k weight"),
+            self._norm(kb, "k bias"), self._ints(positions, shape[0] * shape[1], "positions") if positions is not None else None,
+            self._slots(slots, shape[0]), shape[0], shape[1])
+        _b._check(self.lib.lif_kv_append(self.handle, layer, C.byref(rows), _b._stream()))
+
+    def attend(self, layer, q, out, lse=None, window=0, starts=None, tree=None, slots=None):
+        """q, out [batch, tokens, heads, head_dim]; lse float32 [batch, tokens, heads]; starts int32 [batch]; tree int64 [batch, tokens], a
+        bit per new token that is seen; slots int32 [batch]."""
+        shape, torch = tuple(q.shape[:2]), self.torch
+        q_stride, out_stride = self._rows(q, self.cfg.heads, "q"), self._rows(out, self.cfg.heads, "out", shape)
+        if lse is not None and (lse.dtype != torch.float32 or lse.numel() != shape[0] * shape[1] * self.cfg.heads or not lse.is_contiguous() or
+                                lse.device != self.table.device):
+            _refuse("lse must be a contiguous float32 tensor [batch, tokens, heads]")
+        if tree is not None and (tree.dtype != torch.int64 or tree.numel() != shape[0] * shape[1] or not tree.is_contiguous() or
+                                 tree.device != self.table.device):
+            _refuse("tree must be a contiguous int64 tensor [batch, tokens]")
+        query = _b.LifKvQuery(q.data_ptr(), out.data_ptr(), _b._ptr(lse), q_stride, out_stride, self._slots(slots, shape[0]),
+                              self._ints(starts, shape[0], "starts") if starts is not None else None, _b._ptr(tree), shape[0], shape[1], window)
+        _b._check(self.lib.lif_kv_attend(self.handle, layer, C.byref(query), _b._stream()))
+
+    def _slots(self, slots, batch):
+        if slots is not None:
+            return self._ints(slots, batch, "slots")
+        if batch > self.cfg.max_seqs:
+            _refuse("more rows than slots")
+        return None
+
+    # ---- introspection ---------------------------------------------------------------------------------------------------
+    def state(self) -> dict:
+        s = _b.LifKvState()
+        _b._check(self.lib.lif_kv_get_state(self.handle, C.byref(s), _b._stream()))
+        return {n: getattr(s, n) for n, _ in _b.LifKvState._fields_}
