@@ -418,7 +418,7 @@ typedef struct lif_kv_config {
     int32_t rotary_dim;     /* the first rotary_dim dimensions turn: 0 (none) .. head_dim; a multiple of 16 (half), of 2 (interleaved) */
     float norm_eps;
     float rotary_scale;     /* factor on the rotated dimensions (1: a plain rotation)            */
-    float scale;            /* of the scores; 1 / sqrt(head_dim) as a rule                       */
+    float scale;            /* of the scores, positive; 1 / sqrt(head_dim) as a rule             */
 } lif_kv_config;
 
 typedef struct lif_kv_buffers {
@@ -534,9 +534,16 @@ int lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* rows, void* stre
  * window is given), and j < n - f or new token j - (n - f) is visible to t (tree, or causal).  Nothing visible: zeros.
  * Keys and values at positions that a token does not see never reach its output, whatever they hold.
  * Scores, sums and outputs are accumulated in fp32 and rounded once to E; the weights e^(s_j - m) are rounded to E for the product with the
- * values.  Every sum has a fixed order for given lengths: results are reproducible bit for bit.
+ * values.  Every sum has a fixed order for given lengths (and hint): results are reproducible bit for bit.
  */
 int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* stream);
+
+/*
+ * Performance hint for lif_kv_attend: cached tokens of a sequence as a rule; 0 (the default): as many as a table row holds.  Decides in
+ * which blocks the rows of a call are taken where there are more than 16 of a key head, and with that the order of their sums: results
+ * may differ in the last bits.
+ */
+int lif_kv_set_expected_tokens(lif_kv* kv, int32_t tokens);
 
 /* Synchronises `stream`, then copies the device-side state to the host. */
 int lif_kv_get_state(lif_kv* kv, lif_kv_state* out, void* stream);

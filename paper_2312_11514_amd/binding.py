@@ -111,6 +111,7 @@ EXPORTS = {
     "lif_kv_compact": (C.c_int, [C.c_void_p, C.c_void_p]),
     "lif_kv_append": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(LifKvRows), C.c_void_p]),
     "lif_kv_attend": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(LifKvQuery), C.c_void_p]),
+    "lif_kv_set_expected_tokens": (C.c_int, [C.c_void_p, C.c_int32]),
     "lif_kv_get_state": (C.c_int, [C.c_void_p, C.POINTER(LifKvState), C.c_void_p]),
     "lif_rope_frequencies": (C.c_int, [C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4 + [C.POINTER(C.c_double)]),
 }

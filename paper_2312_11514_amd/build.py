@@ -17,6 +17,13 @@ HIPCC_FLAGS = [
 ]
 
 
+def flags_of(source):
+    """The flags of a source.  Attention: sums of the matrix instructions stay in vector registers also where a wave has more than 256 of
+    them; as accumulation registers they are moved back and forth around every rescaling."""
+    name = os.path.basename(source)
+    return HIPCC_FLAGS + (["-mllvm", "-amdgpu-mfma-vgpr-form"] if name.startswith("kv_attend") else [])
+
+
 def _run(cmd, verbose):
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
@@ -32,7 +39,7 @@ def build_library(verbose: bool = False) -> str:
         objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SOURCES]
         jobs = min(len(SOURCES), os.cpu_count() or 1, 8)
         with ThreadPoolExecutor(jobs) as pool:
-            list(pool.map(lambda so: _run([hipcc, *HIPCC_FLAGS, "-c", "-o", so[1], so[0]], verbose), zip(SOURCES, objects)))
+            list(pool.map(lambda so: _run([hipcc, *flags_of(so[0]), "-c", "-o", so[1], so[0]], verbose), zip(SOURCES, objects)))
         linked = os.path.join(tmp, "liblif.so")
         _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", linked, *objects], verbose)
         with open(linked, "rb") as f, open(LIB_PATH + ".new", "wb") as g:

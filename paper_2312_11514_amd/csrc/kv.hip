@@ -21,12 +21,15 @@ struct lif_kv {
     KvView view;
     const double* frequencies;
     float* parts;
-    float2* stats;
+    unsigned* arrived;
+    size_t part_bytes;
+    int expected;            // cached tokens of a sequence as a rule (0: as many as the table holds)
 };
 
 namespace {
 
 constexpr long long kMaxPositions = 1 << 24;     // of a sequence: the steps of 1024 of them are counted in 32 bits
+constexpr int kAttendFew = 1024;                 // steps that run at once, or nearly
 constexpr int kMoveBlocks = 2048;                // 8 workgroups of copies per compute unit
 constexpr int kCopyBlocks = 256;                 // ... behind lif_kv_reserve, which has a page to copy once in a while
 
@@ -48,22 +51,43 @@ bool config_ok(const lif_kv_config* c, const char** why) {
     if (c->max_seqs < 1 || c->max_seqs > kKvMaxSeqs) return (*why = "max_seqs must be in 1..1024", false);
     if (c->max_pages < 1 || c->max_pages > 1 << 20 || (long long)c->max_pages * c->page_tokens > kMaxPositions)
         return (*why = "max_pages must be in 1..2^20, and a sequence of at most 2^24 tokens", false);
+    if ((long long)c->kv_heads * c->page_tokens * c->head_dim * elem_bytes(c->dtype) >= 1ll << 31)
+        return (*why = "a page of the keys of one layer must stay below 2 GiB", false);
     if (c->max_tokens < 1 || c->max_tokens > 256) return (*why = "max_tokens must be in 1..256", false);
     if (c->norm != LIF_NORM_NONE && c->norm != LIF_NORM_RMS && c->norm != LIF_NORM_LAYER) return (*why = "norm", false);
     if (c->rotary != LIF_ROTARY_HALF && c->rotary != LIF_ROTARY_INTERLEAVED) return (*why = "rotary", false);
     if (c->rotary_dim < 0 || c->rotary_dim > c->head_dim || c->rotary_dim % (c->rotary == LIF_ROTARY_HALF ? 16 : 2))
         return (*why = "rotary_dim must be 0..head_dim, a multiple of 16 (half layout) or 2 (interleaved)", false);
-    if (!std::isfinite(c->scale) || !std::isfinite(c->rotary_scale) || !(c->norm_eps >= 0.f) || !std::isfinite(c->norm_eps))
-        return (*why = "scale, rotary_scale and norm_eps must be finite, norm_eps not negative", false);
+    if (!std::isfinite(c->scale) || !(c->scale > 0.f) || !std::isfinite(c->rotary_scale) || !(c->norm_eps >= 0.f) || !std::isfinite(c->norm_eps))
+        return (*why = "scale, rotary_scale and norm_eps must be finite, scale positive, norm_eps not negative", false);
     return true;
 }
 
 struct KvLayout {
-    size_t state, free_bits, moves, remap, stats, parts, total;
+    size_t state, arrived, free_bits, moves, remap, parts, total;
 };
 
-int rows_of_block(const lif_kv_config& c, int n_tokens) {
-    return 16 * attend_tiles(n_tokens * (c.heads / c.kv_heads), attend_dim_pad(c.head_dim));
+// How the rows of an item, tokens x query heads of a key head, are dealt: blocks of 16 * tiles rows, `positions` to go through at most.
+// A workgroup reads the keys once for its block, so blocks are as large as registers allow; where there are so few that all their steps
+// run at once, the time is that of one workgroup, and smaller ones are faster.
+struct Tiling {
+    int tiles, blocks, block_rows;
+    long long steps;                     // of all items, at most
+};
+Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) {
+    const int step = 4 * 16 / elem_bytes(c.dtype) * kAttendWaves, need = (rows + 15) / 16;
+    const long long per_item = (positions + step - 1) / step + 1;
+    Tiling g;
+    g.tiles = std::min(attend_most_tiles(c.head_dim), need <= 1 ? 1 : need <= 2 ? 2 : 4);
+    while (g.tiles > 1 && (long long)batch * c.kv_heads * ((need + g.tiles / 2 - 1) / (g.tiles / 2)) * per_item <= kAttendFew) g.tiles /= 2;
+    g.blocks = (need + g.tiles - 1) / g.tiles;
+    g.block_rows = std::min(rows, 16 * g.tiles);
+    g.steps = (long long)batch * c.kv_heads * g.blocks * per_item;
+    return g;
+}
+// rows of the largest block of any call
+int most_block_rows(const lif_kv_config& c) {
+    return std::min(c.max_tokens * (c.heads / c.kv_heads), 16 * attend_most_tiles(c.head_dim));
 }
 
 KvLayout make_layout(const lif_kv_config& c) {
@@ -71,17 +95,17 @@ KvLayout make_layout(const lif_kv_config& c) {
     size_t off = 0;
     L.state = off;
     off = align_up(off + sizeof(KvState), 256);
+    L.arrived = off;                   // directly behind the state: a reset clears both
+    off = align_up(off + sizeof(unsigned) * 4 * kAttendGroups, 256);
     L.free_bits = off;
     off = align_up(off + sizeof(unsigned long long) * ((size_t)(c.pages + 63) / 64), 256);
     L.moves = off;
     off = align_up(off + sizeof(int2) * c.pages, 256);
     L.remap = off;
     off = align_up(off + sizeof(int32_t) * std::max(c.pages, c.max_seqs), 256);
-    const size_t rows = (size_t)2 * kAttendGroups * rows_of_block(c, c.max_tokens);
-    L.stats = off;
-    off = align_up(off + sizeof(float2) * rows, 256);
+    const size_t rows = (size_t)4 * kAttendGroups * most_block_rows(c);
     L.parts = off;
-    off = align_up(off + sizeof(float) * rows * attend_dim_pad(c.head_dim), 256);
+    off = align_up(off + sizeof(float) * rows * (attend_dim_pad(c.head_dim) + 4), 256);
     L.total = off;
     return L;
 }
@@ -146,6 +170,8 @@ int lif_kv_create(const lif_kv_config* cfg, const lif_kv_buffers* buf, lif_kv** 
     v.fresh = buf->fresh;
     v.refs = buf->refs;
     v.st = reinterpret_cast<KvState*>(w + L.state);
+    v.arrived = reinterpret_cast<unsigned*>(w + L.arrived);
+    v.n_arrived = 4 * kAttendGroups;
     v.free_bits = reinterpret_cast<unsigned long long*>(w + L.free_bits);
     v.moves = reinterpret_cast<int2*>(w + L.moves);
     v.remap = reinterpret_cast<int32_t*>(w + L.remap);
@@ -157,7 +183,9 @@ int lif_kv_create(const lif_kv_config* cfg, const lif_kv_buffers* buf, lif_kv** 
     v.page_bytes = (unsigned long long)cfg->kv_heads * cfg->page_tokens * cfg->head_dim * elem_bytes(cfg->dtype);
     kv->frequencies = buf->frequencies;
     kv->parts = reinterpret_cast<float*>(w + L.parts);
-    kv->stats = reinterpret_cast<float2*>(w + L.stats);
+    kv->arrived = reinterpret_cast<unsigned*>(w + L.arrived);
+    kv->part_bytes = L.total - L.parts;
+    kv->expected = 0;
     *out = kv;
     return LIF_OK;
 }
@@ -249,19 +277,33 @@ int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* st
     LIF_TRY(stride_ok(kv, query->out_stride, c.heads));
     if (query->window < 0) return fail(LIF_INVALID_ARG, "window must not be negative");
     if (query->tree && query->n_tokens > 64) return fail(LIF_INVALID_ARG, "a tree has at most 64 tokens");
-    const int share = c.heads / c.kv_heads, rows = query->n_tokens * share, pad = attend_dim_pad(c.head_dim), tiles = attend_tiles(rows, pad);
-    const int blocks = (rows + 16 * tiles - 1) / (16 * tiles);
+    const int share = c.heads / c.kv_heads, rows = query->n_tokens * share;
+    const long long width = (long long)c.max_pages * c.page_tokens;
+    const Tiling g = tiling(c, query->batch, rows, kv->expected ? std::min<long long>(kv->expected, width) : width);
+    const long long most = tiling(c, query->batch, rows, width).steps * 4;      // (in blocks of any size)
+    if (most >= (1ll << 31) - kAttendGroups) return fail(LIF_INVALID_ARG, "batch, heads and the width of the table are too large together");
+    const KvView& v = kv->view;
+    const size_t layer_at = (size_t)layer * c.pages * v.page_bytes;
     AttendArgs a{static_cast<const char*>(query->q), static_cast<char*>(query->out), query->lse, query->q_stride, query->out_stride,
-                 query->slots, query->starts, reinterpret_cast<const unsigned long long*>(query->tree), kv->parts, kv->stats, query->batch,
-                 query->n_tokens, c.heads, c.kv_heads, share, c.head_dim, layer, query->window, blocks, c.scale * kLog2e};
-    const int step = 4 * 16 / elem_bytes(c.dtype) * kAttendWaves;
-    const long long most = (long long)query->batch * c.kv_heads * blocks * (((long long)c.max_pages * c.page_tokens + step - 1) / step + 1);
-    const int groups = (int)std::min<long long>(kAttendGroups, most);
+                 query->slots, query->starts, reinterpret_cast<const unsigned long long*>(query->tree), v.k + layer_at, v.v + layer_at, v.table,
+                 v.lengths, v.fresh, &v.st->error, kv->parts, kv->arrived, (unsigned)kv->part_bytes, (unsigned)v.page_bytes,
+                 (unsigned)(v.page_bytes / c.kv_heads), c.pages, c.max_seqs, c.max_pages, v.log_page, query->batch, query->n_tokens, c.heads,
+                 c.kv_heads, share, c.head_dim, query->window, g.blocks, g.block_rows, c.scale * kLog2e};
+    const int groups = (int)std::min<long long>(kAttendUnits * attend_resident(attend_dim_pad(c.head_dim), g.tiles), most);      // (at most a step for each)
     hipStream_t s = (hipStream_t)stream;
-    if (c.dtype == LIF_F32) launch_attend_f32(kv->view, a, pad, tiles, groups, s);
-    else if (c.dtype == LIF_F16) launch_attend_f16(kv->view, a, pad, tiles, groups, s);
-    else launch_attend_bf16(kv->view, a, pad, tiles, groups, s);
+    using Launch = void (*)(const AttendArgs&, int, hipStream_t);
+    static constexpr Launch kLaunch[3][3] = {{launch_attend_f32_1, launch_attend_f32_2, launch_attend_f32_4},
+                                             {launch_attend_f16_1, launch_attend_f16_2, launch_attend_f16_4},
+                                             {launch_attend_bf16_1, launch_attend_bf16_2, launch_attend_bf16_4}};
+    kLaunch[c.dtype][g.tiles >> 1](a, groups, s);
     return launched();
+}
+
+int lif_kv_set_expected_tokens(lif_kv* kv, int32_t tokens) {
+    if (!kv) return fail(LIF_INVALID_ARG, "null handle");
+    if (tokens < 0) return fail(LIF_INVALID_ARG, "tokens must not be negative");
+    kv->expected = tokens;
+    return LIF_OK;
 }
 
 int lif_kv_get_state(lif_kv* kv, lif_kv_state* out, void* stream) {

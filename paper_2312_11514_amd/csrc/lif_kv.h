@@ -23,10 +23,11 @@ struct KvView {
     int32_t* fresh;
     int32_t* refs;
     KvState* st;
+    unsigned* arrived;               // counts of lif_kv_attend, zero between calls
     unsigned long long* free_bits;   // [ceil(pages / 64)]
     int2* moves;                     // [pages] from, to
     int32_t* remap;                  // [pages or max_seqs] where a moved page went; which copy a pair of a fork gets
-    int32_t pages, max_seqs, max_pages, log_page, layers;
+    int32_t pages, max_seqs, max_pages, log_page, layers, n_arrived;
     unsigned long long page_bytes;   // of the keys of one page of one layer (and of the values)
 };
 

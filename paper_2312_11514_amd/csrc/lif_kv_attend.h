@@ -14,9 +14,10 @@
 // together for that), and no LDS is used before the end.  With one row in use of 16 the products cost a fifteenth of the
 // time that the bytes take, so one token of an unshared head takes the same path.
 //
-// What bounds it: reading keys and values once.  Sequences differ in length, and the host does not know them: the steps of all items, one
-// after the other, are dealt to a fixed number of workgroups in equal contiguous runs, each of which works out its own from the
-// lengths.  A run that is a whole item writes its output, a part leaves m, the sum and the unscaled output behind, and k_kv_join adds them.
+// What bounds it: reading keys and values once, and for short sequences the chain slot -> length -> table entry -> keys -> sums.  Sequences
+// differ in length, and the host does not know them: the steps of all items, one after the other, are dealt to a fixed number of
+// workgroups in equal contiguous runs, each of which works out its own from the lengths.  A run that is a whole item writes its
+// output; of an item's parts every workgroup leaves the maximum, the sum and the unscaled output behind, and the last one to do so adds them.
 #pragma once
 
 #include "lif_kv.h"
@@ -24,8 +25,11 @@
 
 namespace lif {
 
+constexpr int kAttendUnits = 256;        // compute units
 constexpr int kAttendGroups = 512;       // workgroups at most: two per compute unit
 constexpr int kAttendWaves = 4;
+constexpr int kAttendFan = 16;           // parts that one workgroup adds at most; of more, such sums are added again
+constexpr int kAttendAsk = 8;            // ... and asks for at once
 constexpr float kLog2e = 1.44269504088896340736f;
 // added to the exponent of every weight, and taken out of the sums: fp16 has no exponents below 2^-24, and of a long sequence many small
 // weights count; none can pass 2^15
@@ -39,39 +43,69 @@ struct AttendArgs {
     const int32_t* slots;
     const int32_t* starts;
     const unsigned long long* tree;
-    float* parts;                          // [2 * groups][rows of a block][dim_pad] sums, unscaled
-    float2* stats;                         // [2 * groups][rows of a block] maximum (log2), sum
-    int32_t batch, n_tokens, heads, kv_heads, share, dim, layer, window, row_blocks;
+    const char* k;                         // of the layer
+    const char* v;
+    const int32_t* table;
+    const int32_t* lengths;
+    const int32_t* fresh;
+    const int32_t* error;
+    float* parts;                          // [2][2 * kAttendGroups][rows of a block][dim_pad + 4] sums, unscaled; maximum (log2) and sum behind
+                                           // them; of the parts, and of their runs
+    unsigned* arrived;                     // [2][2 * kAttendGroups] parts written; zero between calls
+    unsigned part_bytes;                   // of `parts`
+    unsigned page_bytes, head_bytes;       // of the keys of a page, and of one head of them
+    int32_t pages, max_seqs, max_pages, log_page;
+    int32_t batch, n_tokens, heads, kv_heads, share, dim, window;
+    int32_t row_blocks, block_rows;        // blocks of 16 * tiles rows of an item; rows of a block that are there at most
     float scale_log2;                      // scale * log2 e
 };
 
-void launch_attend_f16(const KvView& kv, const AttendArgs& a, int dim_pad, int tiles, int groups, hipStream_t s);
-void launch_attend_bf16(const KvView& kv, const AttendArgs& a, int dim_pad, int tiles, int groups, hipStream_t s);
-void launch_attend_f32(const KvView& kv, const AttendArgs& a, int dim_pad, int tiles, int groups, hipStream_t s);
+// per element type and tiles of 16 rows that a wave takes over the same keys
+void launch_attend_f16_1(const AttendArgs& a, int groups, hipStream_t s);
+void launch_attend_f16_2(const AttendArgs& a, int groups, hipStream_t s);
+void launch_attend_f16_4(const AttendArgs& a, int groups, hipStream_t s);
+void launch_attend_bf16_1(const AttendArgs& a, int groups, hipStream_t s);
+void launch_attend_bf16_2(const AttendArgs& a, int groups, hipStream_t s);
+void launch_attend_bf16_4(const AttendArgs& a, int groups, hipStream_t s);
+void launch_attend_f32_1(const AttendArgs& a, int groups, hipStream_t s);
+void launch_attend_f32_2(const AttendArgs& a, int groups, hipStream_t s);
+void launch_attend_f32_4(const AttendArgs& a, int groups, hipStream_t s);
 
 // head_dim rounded up to what the kernels are compiled for
-__host__ __device__ __forceinline__ int attend_dim_pad(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : 256; }
-// tiles of 16 rows that a workgroup takes over the same keys: as many as there are, up to what the registers hold
-__host__ __device__ __forceinline__ int attend_tiles(int rows, int dim_pad) {
-    const int most = dim_pad > 128 ? 2 : 4;
-    const int tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    return tiles < most ? tiles : most;
+__host__ __device__ __forceinline__ int attend_dim_pad(int dim) {
+    return dim <= 32 ? 32 : dim <= 64 ? 64 : dim == 80 ? 80 : dim <= 96 ? 96 : dim <= 128 ? 128 : 256;
 }
+// most tiles of 16 rows that a wave has registers for: dimensions that are not the compiled ones take some for their bounds
+__host__ __device__ __forceinline__ int attend_most_tiles(int dim) { return dim > 128 ? 1 : dim == attend_dim_pad(dim) ? 4 : 2; }
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// c + a b by one instruction of kParts
 template <typename T> struct Mat;
 template <> struct Mat<_Float16> {
-    static __device__ __forceinline__ f32x4 mul(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static constexpr int kParts = 1;
+    static __device__ __forceinline__ f32x4 mul(f16x8 a, f16x8 b, f32x4 c, int) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mat<__bf16> {
-    static __device__ __forceinline__ f32x4 mul(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static constexpr int kParts = 1;
+    static __device__ __forceinline__ f32x4 mul(bf16x8 a, bf16x8 b, f32x4 c, int) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mat<float> {
-    static __device__ __forceinline__ f32x4 mul(f32x4 a, f32x4 b, f32x4 c) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-        return c;
-    }
+    static constexpr int kParts = 4;
+    static __device__ __forceinline__ f32x4 mul(f32x4 a, f32x4 b, f32x4 c, int e) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0); }
 };
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// load_through of eight bytes
+__device__ __forceinline__ f32x2 load_through2(const float* base, unsigned off, unsigned bytes) {
+    constexpr int kFlags = 0x00027000, kPast = 1 << 4;           // a raw buffer of dwords; the cache policy bit sc1
+    return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(
+                                         __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, (int)bytes, kFlags), (int)off, 0, kPast));
+}
+
+// workgroups of four waves that fit a compute unit
+__host__ __device__ constexpr int attend_resident(int dim_pad, int tiles) { return dim_pad * tiles <= 128 ? 2 : 1; }
 
 // max and sum over the four lanes of a row (16 and 32 apart); every one of them gets the result
 __device__ __forceinline__ float row_max(float v) {
@@ -82,314 +116,498 @@ __device__ __forceinline__ float row_max(float v) {
     const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
     return fmaxf(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
 }
-__device__ __forceinline__ float row_sum(float v) { return swap_add<32>(swap_add<16>(v, v), swap_add<16>(v, v)); }
+__device__ __forceinline__ float row_sum(float v) {
+    const float w = swap_add<16>(v, v);
+    return swap_add<32>(w, w);
+}
 
 // factor on sums over the maximum m for the larger maximum `most`: with nothing visible (m = -inf) the sums are zeros, or NaN, which stays
-__device__ __forceinline__ float rescale(float m, float most) { return m == most ? 1.f : exp2f(m - most); }
+__device__ __forceinline__ float rescale(float m, float most) { return m == most ? 1.f : __builtin_amdgcn_exp2f(m - most); }
 
 // ---- how the steps are dealt -------------------------------------------------------------------------------------------------
-// A batch row of length n, f of its tokens new, has the positions [low, n) to go through, in steps of STEP positions from low rounded down
-// to a stage on; a row with nothing to do has one step (it writes zeros).  Its items, key heads x blocks of rows, have the same.
+// A batch row of length n, f of its tokens new, has the positions [low, n) to go through, in steps from low rounded down to a stage on; a
+// row with nothing to do has one step (it writes zeros).  Its items, key heads x blocks of rows, have the same.  The steps of all items, by
+// batch row, key head, block and position, are dealt in runs of equal length.  Every wave works this out by itself, 64 batch rows at a
+// time, one to a lane: for up to 64 that is no LDS and no barrier.
 struct RowRange {
-    int n, fresh, low;                     // length, new tokens, first position any of them may see
+    int n, fresh, start, slot;             // length, new tokens, first visible position, slot
 };
-__device__ __forceinline__ RowRange row_range(const KvView& kv, const AttendArgs& a, int i) {
-    RowRange r{0, 0, 0};
+__device__ __forceinline__ int low_of(const RowRange& r, int token, int window) {
+    return window ? max(r.start, r.n - r.fresh + token + 1 - window) : r.start;
+}
+__device__ __forceinline__ RowRange row_range(const AttendArgs& a, int i) {
+    RowRange r{0, 0, 0, 0};
     const int slot = a.slots ? a.slots[i] : i;
-    const int start = a.starts ? max(a.starts[i], 0) : 0;
-    if ((unsigned)slot < (unsigned)kv.max_seqs) {
-        r.n = length_of(kv, slot);
-        r.fresh = min(min(max(kv.fresh[slot], 0), r.n), a.n_tokens);
-        // (more new tokens than the call has room for: the call's are the first of them)
-        const int all = min(max(kv.fresh[slot], 0), r.n);
-        r.n -= all - r.fresh;
+    if (a.starts) r.start = max(a.starts[i], 0);
+    if ((unsigned)slot < (unsigned)a.max_seqs) {
+        r.slot = slot;
+        const int length = a.lengths[slot], fresh = a.fresh[slot];
+        r.n = min(max(length, 0), a.max_pages << a.log_page);
+        const int all = min(max(fresh, 0), r.n);
+        r.fresh = min(all, a.n_tokens);
+        r.n -= all - r.fresh;              // (more new tokens than the call has rows for: the call's are the first of them)
     }
-    r.low = a.window ? max(start, r.n - r.fresh + 1 - a.window) : start;
-    if (r.fresh == 0 || r.low >= r.n) r.low = r.n = 0;
+    if (r.fresh == 0 || low_of(r, 0, a.window) >= r.n) r.n = r.start = 0;
     return r;
 }
-template <int STAGE, int STEP>
-__device__ __forceinline__ int row_steps(const RowRange& r) { return max(1, (r.n - r.low / STAGE * STAGE + STEP - 1) / STEP); }
 
-// first[i] = steps of the batch rows before i, first[batch] = all; per key head and block.  By a workgroup of 256.
-template <int STAGE, int STEP>
-__device__ __forceinline__ void plan_steps(const KvView& kv, const AttendArgs& a, int* first, int* wave_tot) {
-    const int per = (a.batch + 255) / 256, i0 = threadIdx.x * per;
-    int sum = 0;
-    for (int e = 0; e < per; ++e)
-        if (i0 + e < a.batch) sum += row_steps<STAGE, STEP>(row_range(kv, a, i0 + e));
-    int total;
-    int at = block_exclusive_scan<4>(sum, wave_tot, &total);
-    for (int e = 0; e < per; ++e)
-        if (i0 + e < a.batch) {
-            first[i0 + e] = at;
-            at += row_steps<STAGE, STEP>(row_range(kv, a, i0 + e));
-        }
-    if (threadIdx.x == 0) first[a.batch] = total;
-    __syncthreads();
+// values that are the same in all lanes, as ones of the wave: what follows from them then runs on the scalar unit
+__device__ __forceinline__ int whole_wave(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ RowRange of_lane(const RowRange& r, int lane) {
+    return RowRange{__builtin_amdgcn_readlane(r.n, lane), __builtin_amdgcn_readlane(r.fresh, lane), __builtin_amdgcn_readlane(r.start, lane),
+                    __builtin_amdgcn_readlane(r.slot, lane)};
+}
+
+// a / b, the same in all lanes
+__device__ __forceinline__ int quotient(int a, int b) { return whole_wave((int)((unsigned)a / (unsigned)b)); }
+
+// 64 batch rows from `first` on, one to a lane
+struct RowChunk {
+    RowRange range;
+    int first, steps, before;              // first batch row; steps per item of the lane's row, and of the rows before it (all of them)
+    int after;                             // steps per item up to the chunk's end
+};
+__device__ __forceinline__ RowChunk row_chunk(const AttendArgs& a, int stage, int step, int first, int before) {
+    RowChunk c;
+    c.first = first;
+    c.range = RowRange{0, 0, 0, 0};
+    c.steps = 0;
+    const int lane = threadIdx.x & 63;
+    if (first + lane < a.batch) {
+        c.range = row_range(a, first + lane);
+        const int low = c.range.n ? low_of(c.range, 0, a.window) : 0;
+        c.steps = max(1, (c.range.n - (low & -stage) + step - 1) / step);        // (stage and step are powers of two)
+    }
+    const int up_to = wave_inclusive_scan(c.steps, lane);
+    c.before = before + up_to - c.steps;
+    c.after = before + __builtin_amdgcn_readlane(up_to, 63);
+    return c;
 }
 
 // ---- the pass over keys and values -------------------------------------------------------------------------------------------
-// grid = groups, block = 256.  HDP: head_dim rounded up (FULL: head_dim itself); QT: tiles of 16 rows.
-template <typename T, int HDP, int QT, bool FULL>
-__global__ __launch_bounds__(256, QT * HDP <= 128 ? 2 : 1) void k_kv_attend(const KvView kv, const AttendArgs a) {
+// grid = groups, block = 256.  HDP: head_dim rounded up (FULL: head_dim itself).  QT: tiles of 16 rows of a wave.
+template <typename T, int HDP, bool FULL, int QT>
+__global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(const AttendArgs a) {
     using V = typename Vec<T>::type;
+    using M = Mat<T>;
     constexpr int N = Vec<T>::N;               // elements of 16 bytes; positions of a lane in the second products
     constexpr int TILES = N / 4;               // K tiles of a stage
-    constexpr int STAGE = 4 * N, STEP = STAGE * kAttendWaves;
-    constexpr int CH = HDP / (4 * N);          // pieces of a key that a lane holds
+    constexpr int STAGE = 4 * N;
+    constexpr int CH = (HDP + 4 * N - 1) / (4 * N);          // pieces of a key that a lane holds
     constexpr int DT = HDP / 16;               // tiles of dimensions
     constexpr int HALF = HDP > 128 ? 2 : 1;    // the waves' sums meet in LDS, up to 128 dimensions at a time
-    constexpr int PITCH = HDP / HALF + 4;
-    __shared__ int first[kKvMaxSeqs + 1];
-    __shared__ int wave_tot[4];
+    constexpr int COLS = HDP / HALF, PITCH = COLS + 4;
+    constexpr int ROW = HDP + 4;               // floats of a row of a part
+    __shared__ int last;
     __shared__ float wave_max[kAttendWaves][16 * QT], wave_sum_[kAttendWaves][16 * QT];
+    __shared__ int2 out_at[16 * QT];          // of a row of the block: row of `out` (negative: padding), head
     __shared__ float sums[kAttendWaves][16][PITCH];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = lane & 15, g = lane >> 4, dim = FULL ? HDP : a.dim;
-    if (kv.st->error) return;
-    plan_steps<STAGE, STEP>(kv, a, first, wave_tot);
-    const int per_row = a.kv_heads * a.row_blocks;
-    const long long all = (long long)first[a.batch] * per_row;
-    const long long groups = min((long long)gridDim.x, all);      // (every one of them gets a step)
-    if (blockIdx.x >= groups) return;
-    long long at = all * blockIdx.x / groups;
-    const long long end = all * (blockIdx.x + 1) / groups;
-    int i = last_not_above(first, a.batch, (int)(at / per_row));
+    const int tid = threadIdx.x, lane = tid & 63, wv = whole_wave(tid >> 6), n = lane & 15, g = lane >> 4, dim = FULL ? HDP : a.dim;
+    constexpr int STEP = STAGE * kAttendWaves;
+    const int error = *a.error;
+    RowChunk rc = row_chunk(a, STAGE, STEP, 0, 0);
+    if (whole_wave(error)) return;
+    int total = rc.after;
+    for (int c0 = 64; c0 < a.batch; c0 += 64) total = row_chunk(a, STAGE, STEP, c0, total).after;
+    const int per_row = a.kv_heads * a.row_blocks, rows = a.n_tokens * a.share;
+    const int all = total * per_row;           // (below 2^31: lif_kv_attend has seen to it)
+    const int run_steps = quotient(all + (int)gridDim.x - 1, (int)gridDim.x);
+    const int end = (int)min((unsigned)run_steps * (blockIdx.x + 1), (unsigned)all);
+    int at = (int)min((unsigned)run_steps * blockIdx.x, (unsigned)all);
     bool first_segment = true;
 
     while (at < end) {
-        while (i + 1 < a.batch && (long long)first[i + 1] * per_row <= at) ++i;
-        const int steps = first[i + 1] - first[i];
-        const long long in_row = at - (long long)first[i] * per_row;
-        const int item = (int)(in_row / steps), s0 = (int)(in_row % steps);
-        const int s1 = (int)min((long long)steps, s0 + (end - at));
-        const int kvh = item / a.row_blocks, rb = item % a.row_blocks;
-        const RowRange r = row_range(kv, a, i);
-        const int slot = a.slots ? a.slots[i] : i;
-        const int start = a.starts ? max(a.starts[i], 0) : 0;
-        const int rows = a.n_tokens * a.share, row0 = rb * 16 * QT, base = r.n - r.fresh;
+        while (rc.after * per_row <= at) rc = row_chunk(a, STAGE, STEP, rc.first + 64, rc.after);
+        // the last row that begins at or before the step (rows behind the batch have no steps, and begin behind it)
+        const int il = __popcll(__ballot(rc.before * per_row <= at && rc.steps > 0)) - 1, i = rc.first + il;
+        const int before = __builtin_amdgcn_readlane(rc.before, il), steps = __builtin_amdgcn_readlane(rc.steps, il);
+        const RowRange r = of_lane(rc.range, il);
+        const int in_row = at - before * per_row, item = quotient(in_row, steps), s0 = in_row - item * steps, s1 = min(steps, s0 + end - at);
+        const int kvh = a.row_blocks == 1 ? item : quotient(item, a.row_blocks), row0 = (item - kvh * a.row_blocks) * QT * 16;
+        const int base = r.n - r.fresh, low_all = low_of(r, 0, a.window);
 
-        // the lane's rows: token, what it sees, query
-        int token[QT], low[QT];
+        // the lane's rows: first position it sees, last new token and which of those it sees, query
+        int low[QT], newest[QT];
+        int2 my_out[QT];
         unsigned long long seen[QT];
         V q[QT][CH];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const int row = row0 + 16 * t + n;
-            token[t] = row / a.share;
-            const bool ok = row < rows && token[t] < r.fresh;
-            if (!ok) token[t] = -1;
-            low[t] = a.window ? max(start, base + token[t] + 1 - a.window) : start;
-            seen[t] = 0;
-            if (ok && a.tree) seen[t] = a.tree[(size_t)i * a.n_tokens + token[t]];
-            const T* from = (const T*)a.q + ((size_t)i * a.n_tokens + (ok ? token[t] : 0)) * a.q_stride +
-                            (unsigned)((kvh * a.share + (ok ? row % a.share : 0)) * dim);
+            const int tok = (int)((unsigned)row / (unsigned)a.share), head = kvh * a.share + row - tok * a.share;
+            const bool ok = row < rows && tok < r.fresh;
+            my_out[t] = make_int2((i * a.n_tokens + tok) | (ok ? 0 : 1 << 31), head);
+            low[t] = ok ? low_of(r, tok, a.window) : 0x7fffffff;
+            newest[t] = a.tree ? 63 : tok;
+            seen[t] = ~0ull;
+            if (ok && a.tree) seen[t] = a.tree[(size_t)i * a.n_tokens + tok];
+            const T* from = (const T*)a.q + ((size_t)i * a.n_tokens + (ok ? tok : 0)) * a.q_stride + (unsigned)((ok ? head : 0) * dim);
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
+            for (int c = 0; c < CH; ++c) {             // (a row that is not there computes with one that is, and is not looked at)
+                const bool sure_in = FULL && (4 * c + 4) * N <= HDP;
                 const int d = (4 * c + g) * N;
-                q[t][c] = ok && (FULL || d < dim) ? *reinterpret_cast<const V*>(from + d) : V{};
+                q[t][c] = *reinterpret_cast<const V*>(from + (sure_in || d < dim ? d : 0));
+                if (!sure_in && d >= dim) q[t][c] = V{};
             }
         }
+        const float scale_log2 = a.scale_log2;
         f32x4 o[QT][DT];
-        float top[QT], off[QT], sum[QT];       // running maximum (log2), what is taken from the exponents, sum of the lane's weights
+        float top[QT], off[QT], sum[QT];       // running maximum, what is taken from the exponents, sum of the lane's weights
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             top[t] = -INFINITY;
-            off[t] = 0.f;
-            sum[t] = 0.f;
+            off[t] = sum[t] = 0.f;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
-        const int origin = r.low / STAGE * STAGE;
-        const int p_end = min(r.n, origin + s1 * STEP);
+        const int origin = low_all / STAGE * STAGE;
+        const int p_end = min(r.n, origin + s1 * STEP), p_last = r.n - 1;
         int p = origin + s0 * STEP + wv * STAGE;
-        const int32_t* row_table = kv.table + (size_t)((unsigned)slot < (unsigned)kv.max_seqs ? slot : 0) * kv.max_pages;
-        // positions in [sure, sure_end) are visible to all rows of the block
-        const int sure = a.window ? max(start, r.n - a.window) : start, sure_end = a.tree ? base : base + 1;
-        const size_t head_bytes = (size_t)kv.page_bytes / a.kv_heads;
-        const size_t layer0 = (size_t)a.layer * kv.pages;
-        const int page_mask = (1 << kv.log_page) - 1;
-
+        const int32_t* row_table = a.table + (size_t)r.slot * a.max_pages;
+        // positions in [sure, sure_end) are visible to all rows of the item
+        const int sure = a.window ? max(r.start, r.n - a.window) : r.start, sure_end = a.tree ? base : base + 1;
+        const char* k_pool = a.k + kvh * (size_t)a.head_bytes;
+        const char* v_pool = a.v + kvh * (size_t)a.head_bytes;
+        const int page_mask = (1 << a.log_page) - 1;
         // whether the lane's row of tile t sees a position
-        auto sees = [&](int t, int pos) {
+        auto sees = [&](int t, int pos) -> bool {
             const int own = pos - base;
-            const bool new_ok = a.tree ? own < 64 && (seen[t] >> (own & 63) & 1ull) : own <= token[t];
-            return token[t] >= 0 && pos >= low[t] && pos < r.n && (own < 0 || new_ok);
+            return (int)(pos >= low[t]) & (int)(pos < r.n) & ((int)(own < 0) | ((int)(own <= newest[t]) & (int)(seen[t] >> (own & 63) & 1ull)));
         };
-
-        while (p < p_end) {
-            // keys: row n of tile e is position p + N (n div 4) + 4 e + n mod 4; values: positions p + N g ..
-            const int kp = p + N * (n >> 2), vp = p + N * g;
-            int k_page = row_table[min(kp, r.n - 1) >> kv.log_page], v_page = row_table[min(vp, r.n - 1) >> kv.log_page];
-            if (!page_ok(kv, k_page)) k_page = 0;
-            if (!page_ok(kv, v_page)) v_page = 0;
-            const char* k_at = kv.k + (layer0 + k_page) * kv.page_bytes + kvh * head_bytes;
-            const char* v_at = kv.v + (layer0 + v_page) * kv.page_bytes + kvh * head_bytes;
-            V k[TILES][CH], v[DT];
+        auto page_at = [&](int pos) { return row_table[min(pos, p_last) >> a.log_page]; };
+        auto in_pool = [&](int page) { return (size_t)((unsigned)page < (unsigned)a.pages ? page : 0) * a.page_bytes; };
+        // keys of a stage: row n of tile e is position p + N (n div 4) + 4 e + n mod 4; values: positions p + N g ..
+        auto load_k = [&](V (&k)[TILES][CH], int p, int page) {
+            const T* from = (const T*)(k_pool + in_pool(page)) + (unsigned)((((p + N * (n >> 2)) & page_mask) + (n & 3)) * dim);
 #pragma unroll
             for (int e = 0; e < TILES; ++e)
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
+                    const bool sure_in = FULL && (4 * c + 4) * N <= HDP;
                     const int d = (4 * c + g) * N;
-                    const T* from = (const T*)k_at + (unsigned)(((kp & page_mask) + 4 * e + (n & 3)) * dim);
-                    k[e][c] = *reinterpret_cast<const V*>(from + (FULL || d < dim ? d : 0));
-                    if (!FULL && d >= dim) k[e][c] = V{};
+                    k[e][c] = *reinterpret_cast<const V*>(from + 4 * e * dim + (sure_in || d < dim ? d : 0));
+                    if (!sure_in && d >= dim) k[e][c] = V{};
                 }
+        };
+        auto v_from = [&](int p, int page) { return (const T*)(v_pool + in_pool(page)) + (unsigned)(((p + N * g) & page_mask) * dim); };
+        auto load_v = [&](V (&v)[DT], const T* from) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                const T* from = (const T*)v_at + (unsigned)((vp & page_mask) * dim);
                 v[d] = *reinterpret_cast<const V*>(from + (FULL || 16 * d + n < dim ? 16 * d + n : 0) * N);
                 if (!FULL && 16 * d + n >= dim) v[d] = V{};
             }
-            const bool edge = p < sure || p + STAGE > sure_end;
-            if (edge) {                        // what no row may see is not there, whatever it holds
+        };
+
+        // Keys of the next stage are asked for as soon as this stage's are used up, values likewise, table entries a stage ahead of both: a
+        // wave always has something on its way.  Loads come back in the order they were asked for in, so that order is keys, table entries,
+        // values, everywhere: a wait for one of them is then no wait for the next (the barriers keep the compiler to it).
+        if (p < p_end) {
+            V k[TILES][CH], v[DT];
+            const int k0 = page_at(p + N * (n >> 2)), v0 = page_at(p + N * g);
+            load_k(k, p, k0);
+            __builtin_amdgcn_sched_barrier(0);
+            int k_page = page_at(p + STEP + N * (n >> 2)), v_page = page_at(p + STEP + N * g);
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(v, v_from(p, v0));
+            __builtin_amdgcn_sched_barrier(0);
+            bool more;
+            do {
+                more = p + STEP < p_end;
+                float x[QT][N];
+                {
+                    // (two sums where one chain of products would be long)
+                    constexpr int CHAINS = QT == 1 && M::kParts > 1 ? 2 : 1;
+                    f32x4 s[QT][TILES][CHAINS];
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const bool in = vp + e >= r.low && vp + e < r.n;
+                    for (int t = 0; t < QT; ++t)
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) v[d][e] = in ? v[d][e] : (T)0.f;
+                        for (int e = 0; e < TILES; ++e)
+#pragma unroll
+                            for (int h = 0; h < CHAINS; ++h) s[t][e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < CH; ++c)
+#pragma unroll
+                        for (int u = 0; u < M::kParts; ++u)
+#pragma unroll
+                            for (int e = 0; e < TILES; ++e)
+#pragma unroll
+                                for (int t = 0; t < QT; ++t) s[t][e][u % CHAINS] = M::mul(k[e][c], q[t][c], s[t][e][u % CHAINS], u);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t)
+#pragma unroll
+                        for (int e = 0; e < TILES; ++e)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) x[t][4 * e + j] = CHAINS == 2 ? s[t][e][0][j] + s[t][e][CHAINS - 1][j] : s[t][e][0][j];
                 }
-            }
-            V w[QT];
-#pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                float x[N];
-#pragma unroll
-                for (int e = 0; e < TILES; ++e) {
-                    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int c = 0; c < CH; ++c) s = Mat<T>::mul(k[e][c], q[t][c], s);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[4 * e + j] = s[j] * a.scale_log2;
-                }
+                if (more) load_k(k, p + STEP, k_page);
+                const T* v_next = v_from(p + STEP, v_page);
+                __builtin_amdgcn_sched_barrier(0);
+                k_page = page_at(p + 2 * STEP + N * (n >> 2));
+                v_page = page_at(p + 2 * STEP + N * g);
+                __builtin_amdgcn_sched_barrier(0);
+                const int vp = p + N * g;
+                const bool edge = p < sure || p + STAGE > sure_end;
                 if (edge) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        x[e] = sees(t, vp + e) ? x[e] : -INFINITY;
+                    for (int t = 0; t < QT; ++t)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) x[t][e] = sees(t, vp + e) ? x[t][e] : -INFINITY;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {          // what no row may see is not there, whatever it holds
+                        auto in = [&](int e) { return vp + e >= low_all && vp + e < r.n; };
+                        const unsigned mask = N == 4 ? (in(u) ? ~0u : 0u) : (in(2 * u) ? 0xffffu : 0u) | (in(2 * u + 1) ? 0xffff0000u : 0u);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            u32x4 bits = __builtin_bit_cast(u32x4, v[d]);
+                            bits[u] &= mask;
+                            v[d] = __builtin_bit_cast(V, bits);
+                        }
                     }
                 }
-                float most = x[0];
+                V w[QT];
 #pragma unroll
-                for (int e = 1; e < N; ++e) most = fmaxf(most, x[e]);
-                if (__any(most > top[t])) {
-                    most = fmaxf(row_max(most), top[t]);
-                    const float scale = most == -INFINITY ? 1.f : exp2f(top[t] - most);
-                    off[t] = most == -INFINITY ? 0.f : most - kWeightBias;
-                    top[t] = most;
-                    sum[t] *= scale;
+                for (int t = 0; t < QT; ++t) {
+                    float most = x[t][0];
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) o[t][d] *= scale;
+                    for (int e = 1; e < N; ++e) most = fmaxf(most, x[t][e]);
+                    if (__any(most > top[t])) {
+                        most = fmaxf(row_max(most), top[t]);
+                        const float scale = most == top[t] ? 1.f : __builtin_amdgcn_exp2f((top[t] - most) * scale_log2);
+                        off[t] = most == -INFINITY ? 0.f : most * scale_log2 - kWeightBias;
+                        top[t] = most;
+                        sum[t] *= scale;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) o[t][d] *= scale;
+                    }
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e], scale_log2, -off[t]));
+                        sum[t] += weight;
+                        w[t][e] = (T)weight;
+                    }
                 }
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float weight = __builtin_amdgcn_exp2f(x[e] - off[t]);
-                    sum[t] += weight;
-                    w[t][e] = (T)weight;
-                }
-            }
-            // A weight of zero does not keep a value out that is not finite.  Where rows see different positions of a stage, such values are
-            // taken out of the products and added to the rows that see them.
-            if (edge && r.fresh > 1) {
-                bool finite = true;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int e = 0; e < N; ++e) finite = finite && __builtin_isfinite((float)v[d][e]);
-                if (__any(!finite)) {
+                // A weight of zero does not keep a value out that is not finite.  Where rows see different positions of a stage, such values are
+                // taken out of the products and added to the rows that see them.
+                if (edge && r.fresh > 1) {
+                    bool finite = true;
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
 #pragma unroll
-                        for (int e = 0; e < N; ++e) v[d][e] = __builtin_isfinite((float)v[d][e]) ? v[d][e] : (T)0.f;
-#pragma unroll 1
-                    for (int pos = max(p, r.low); pos < min(p + STAGE, r.n); ++pos) {
-                        int page = row_table[pos >> kv.log_page];
-                        if (!page_ok(kv, page)) page = 0;
-                        const T* from = (const T*)(kv.v + (layer0 + page) * kv.page_bytes + kvh * head_bytes) +
-                                        (unsigned)((pos & page_mask) / N * dim * N) + pos % N;
-                        bool seen_here[QT];
-#pragma unroll
-                        for (int t = 0; t < QT; ++t) seen_here[t] = sees(t, pos);
+                        for (int e = 0; e < N; ++e) finite = finite && __builtin_isfinite((float)v[d][e]);
+                    if (__any(!finite)) {
 #pragma unroll
                         for (int d = 0; d < DT; ++d)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const int at_dim = 16 * d + 4 * g + j;
-                                const float value = (float)from[(FULL || at_dim < dim ? at_dim : 0) * N];
-                                const bool add = !__builtin_isfinite(value) && (FULL || at_dim < dim);
+                            for (int e = 0; e < N; ++e) v[d][e] = __builtin_isfinite((float)v[d][e]) ? v[d][e] : (T)0.f;
+#pragma unroll 1
+                        for (int pos = max(p, low_all); pos < min(p + STAGE, r.n); ++pos) {
+                            const T* from = (const T*)(v_pool + in_pool(page_at(pos))) + (unsigned)((pos & page_mask) / N * dim * N) + pos % N;
+                            bool seen_here[QT];
 #pragma unroll
-                                for (int t = 0; t < QT; ++t) o[t][d][j] += add && seen_here[t] ? value : 0.f;
-                            }
+                            for (int t = 0; t < QT; ++t) seen_here[t] = sees(t, pos);
+#pragma unroll
+                            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const int at_dim = 16 * d + 4 * g + j;
+                                    const float value = (float)from[(FULL || at_dim < dim ? at_dim : 0) * N];
+                                    const float add = __builtin_isfinite(value) || (!FULL && at_dim >= dim) ? 0.f : value;
+#pragma unroll
+                                    for (int t = 0; t < QT; ++t) o[t][d][j] += seen_here[t] ? add : 0.f;
+                                }
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+                for (int u = 0; u < M::kParts; ++u)
 #pragma unroll
-                for (int t = 0; t < QT; ++t) o[t][d] = Mat<T>::mul(v[d], w[t], o[t][d]);
-            p += STEP;
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int t = 0; t < QT; ++t) o[t][d] = M::mul(v[d], w[t], o[t][d], u);
+                if (more) load_v(v, v_next);
+                p += STEP;
+            } while (more);
         }
 
         // the waves' sums meet
-        __syncthreads();                       // (the last segment's readers are done)
+        const bool whole = s0 == 0 && s1 == steps;
+        const int part = 2 * blockIdx.x + (first_segment ? 0 : 1);
+        const int rows_here = min(16 * QT, rows - row0);
+        // four dimensions of a row of the output
+        auto finish = [&](int r0, int d, f32x4 v, float m, float total) {
+            const int2 to = out_at[r0];
+            const size_t out_row = (unsigned)to.x & 0x7fffffffu;
+            const bool none = to.x < 0 || total == 0.f;
+            const float inv = 1.f / total;
+            if (FULL || d < dim) {
+                typedef T T4 __attribute__((ext_vector_type(4)));
+                T4 y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = none ? (T)0.f : (T)(v[j] * inv);
+                *reinterpret_cast<T4*>((T*)a.out + out_row * a.out_stride + (unsigned)(to.y * dim + d)) = y;
+            }
+            if (a.lse && d == 0) a.lse[out_row * a.heads + to.y] = none ? -INFINITY : (m - kWeightBias + log2f(total)) / kLog2e;
+        };
+        char* parts = reinterpret_cast<char*>(a.parts);
+        auto part_at = [&](int slot, int r0) { return (unsigned)(((unsigned)slot * a.block_rows + r0) * ROW * 4u); };
+        if (!first_segment) __syncthreads();   // (the last segment's readers are done)
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const float total = row_sum(sum[t]);
             if (g == 0) {
-                wave_max[wv][16 * t + n] = top[t];
+                wave_max[wv][16 * t + n] = top[t] == -INFINITY ? -INFINITY : top[t] * scale_log2;
                 wave_sum_[wv][16 * t + n] = total;
+                if (wv == 0) out_at[16 * t + n] = my_out[t];
             }
         }
-        __syncthreads();
-        const bool whole = s0 == 0 && s1 == steps;
-        const int part_slot = 2 * blockIdx.x + (first_segment ? 0 : 1);
-        const int rows_here = min(16 * QT, rows - row0);
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            float most = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < kAttendWaves; ++w) most = fmaxf(most, wave_max[w][16 * t + n]);
-            const float scale = rescale(top[t], most);
 #pragma unroll
             for (int half = 0; half < HALF; ++half) {
                 if (t || half) __syncthreads();
 #pragma unroll
-                for (int d = 0; d < DT / HALF; ++d) {
-                    *reinterpret_cast<f32x4*>(&sums[wv][n][16 * d + 4 * g]) = o[t][half * (DT / HALF) + d] * scale;
-                }
+                for (int d = 0; d < DT / HALF; ++d)
+                    *reinterpret_cast<f32x4*>(&sums[wv][n][16 * d + 4 * g]) = o[t][half * (DT / HALF) + d];
                 __syncthreads();
-                // thread -> row tid / 16 of the tile, four dimensions at a time
-                const int rr = tid >> 4, row = 16 * t + rr;
-                float m = -INFINITY, total = 0.f;
+                for (int u = tid; u < 16 * (COLS / 4); u += 256) {
+                    const int rr = u / (COLS / 4), d = u % (COLS / 4) * 4, r0 = 16 * t + rr;
+                    if (r0 >= rows_here) break;
+                    float wm[kAttendWaves], wl[kAttendWaves];
+                    f32x4 wy[kAttendWaves];
 #pragma unroll
-                for (int w = 0; w < kAttendWaves; ++w) m = fmaxf(m, wave_max[w][row]);
+                    for (int w = 0; w < kAttendWaves; ++w) {
+                        wm[w] = wave_max[w][r0];
+                        wl[w] = wave_sum_[w][r0];
+                        wy[w] = *reinterpret_cast<const f32x4*>(&sums[w][rr][d]);
+                    }
+                    float m = wm[0], l = 0.f;
 #pragma unroll
-                for (int w = 0; w < kAttendWaves; ++w) total += wave_sum_[w][row] * rescale(wave_max[w][row], m);
-                if (row < rows_here) {
-                    const int abs_row = row0 + row, tok = abs_row / a.share, head = kvh * a.share + abs_row % a.share;
-                    const size_t out_row = (size_t)i * a.n_tokens + tok;
-                    const bool padding = tok >= r.fresh, none = padding || total == 0.f;
-                    const float inv = 1.f / total;
-                    for (int d = 4 * (tid & 15); d < HDP / HALF; d += 64) {
-                        f32x4 v = *reinterpret_cast<const f32x4*>(&sums[0][rr][d]);
+                    for (int e = 1; e < kAttendWaves; ++e) m = fmaxf(m, wm[e]);
+                    f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int w = 1; w < kAttendWaves; ++w) v += *reinterpret_cast<const f32x4*>(&sums[w][rr][d]);
-                        const int to_dim = half * (HDP / HALF) + d;
-                        if (whole) {
-                            if (FULL || to_dim < dim) {
-                                T* to = (T*)a.out + out_row * a.out_stride + (unsigned)(head * dim + to_dim);
+                    for (int e = 0; e < kAttendWaves; ++e) {
+                        const float f = rescale(wm[e], m);
+                        l += wl[e] * f;
+                        y += wy[e] * f;
+                    }
+                    if (whole) {
+                        finish(r0, half * COLS + d, y, m, l);
+                    } else {
+                        store_through(parts, part_at(part, r0) + (half * COLS + d) * 4, a.part_bytes, y);
+                        if (half == 0 && d == 0) store_through(parts, part_at(part, r0) + HDP * 4, a.part_bytes, f32x4{m, l, 0.f, 0.f});
+                    }
+                }
+            }
+        }
+
+        // Parts: the workgroups w0 .. w1 have steps of the item, each has left one part (its last segment, or its first if it begins in the
+        // item).  Runs of kAttendFan of them are added by the last one of the run, into the place of the run's first part, and the runs by the
+        // last run.
+        if (!whole) {
+            const int begin = at - s0, w0 = quotient(begin, run_steps), w1 = quotient(begin + steps - 1, run_steps);
+            const int count = w1 - w0 + 1, run = ((int)blockIdx.x - w0) / kAttendFan, runs = (count + kAttendFan - 1) / kAttendFan;
+            const bool begins_before = w0 * run_steps < begin;
+            auto part_of = [&](int k) { return 2 * (w0 + k) + (k == 0 && begins_before ? 1 : 0); };
+            int level = 0, from = run * kAttendFan, stride = 1, n_parts = min(kAttendFan, count - from);
+            while (true) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // this wave's stores are acknowledged,
+                __syncthreads();                                             // and those of the others
+                if (tid == 0)
+                    last = n_parts == 1 || (int)atomicInc(a.arrived + level * 2 * kAttendGroups + part_of(from), (unsigned)n_parts - 1u) == n_parts - 1;
+                __syncthreads();
+                if (!whole_wave(last)) break;
+                const bool done = level == 1 || runs == 1;
+                // Rows x four dimensions to the threads, and what is left of them shares the parts of a row.  A thread asks for kAttendAsk parts
+                // at once, those of its next rows among them.
+                constexpr int QUADS = HDP / 4, TEAMS = 256 / QUADS >= 32 ? 32 : 256 / QUADS >= 16 ? 16 : 256 / QUADS >= 8 ? 8 : 4;
+                int log_once = 0;
+                while ((1 << log_once) < TEAMS && (1 << log_once) < rows_here) ++log_once;
+                const int shares = TEAMS >> log_once, per = (n_parts + shares - 1) >> (__builtin_ctz(TEAMS) - log_once);
+                const int team = tid / QUADS, d = tid % QUADS * 4, share = team >> log_once, row_in = team & ((1 << log_once) - 1);
+                const int units = ((rows_here + (1 << log_once) - 1) >> log_once) * per;
+                auto leave = [&](int r0, f32x4 y, float m, float l) {
+                    if (done) {
+                        finish(r0, d, y, m, l);
+                    } else {
+                        const unsigned b = part_at(2 * kAttendGroups + part_of(from), r0);
+                        store_through(parts, b + d * 4, a.part_bytes, y);
+                        if (d == 0) store_through(parts, b + HDP * 4, a.part_bytes, f32x4{m, l, 0.f, 0.f});
+                    }
+                };
+                float m = -INFINITY, l = 0.f;
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
+                int r_ask = row_in, e_ask = 0, r0 = row_in, e_now = 0;           // row and part of the next one to ask for, and to add
+                for (int u0 = 0; u0 < units; u0 += kAttendAsk) {
+                    f32x2 s[kAttendAsk];
+                    f32x4 v[kAttendAsk];
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) to[j] = none ? (T)0.f : (T)(v[j] * inv);
+                    for (int e = 0; e < kAttendAsk; ++e)
+                        if (u0 + e < units) {
+                            const unsigned b = part_at(level * 2 * kAttendGroups + part_of(from + min(share * per + e_ask, n_parts - 1) * stride),
+                                                       min(r_ask, rows_here - 1));
+                            s[e] = load_through2(a.parts, b + HDP * 4, a.part_bytes);
+                            v[e] = load_through(a.parts, b + d * 4, a.part_bytes);
+                            if (++e_ask == per) {
+                                e_ask = 0;
+                                r_ask += 1 << log_once;
                             }
-                        } else {
-                            *reinterpret_cast<f32x4*>(a.parts + ((size_t)part_slot * 16 * QT + row) * HDP + to_dim) = padding ? f32x4{} : v;
+                        }
+#pragma unroll
+                    for (int e = 0; e < kAttendAsk; ++e)
+                        if (u0 + e < units) {
+                            if (share * per + e_now < n_parts) {
+                                const float most = fmaxf(m, s[e][0]), old = rescale(m, most), f = rescale(s[e][0], most);
+                                m = most;
+                                l = l * old + s[e][1] * f;
+                                y = y * old + v[e] * f;
+                            }
+                            if (++e_now == per) {
+                                if (shares == 1) {
+                                    if (team < TEAMS && r0 < rows_here) leave(r0, y, m, l);
+                                    r0 += 1 << log_once;
+                                    m = -INFINITY;
+                                    l = 0.f;
+                                    y = f32x4{0.f, 0.f, 0.f, 0.f};
+                                }
+                                e_now = 0;
+                            }
+                        }
+                }
+                if (shares > 1) {                    // (one round of rows)
+                    float* mine = &sums[0][0][0] + (team < TEAMS ? team : 0) * ROW;
+                    const bool here = team < TEAMS && r0 < rows_here;
+                    __syncthreads();
+                    if (here) {
+                        *reinterpret_cast<f32x4*>(mine + d) = y;
+                        if (d == 0) {
+                            mine[HDP] = m;
+                            mine[HDP + 1] = l;
                         }
                     }
-                    if (half == 0 && (tid & 15) == 0) {
-                        if (!whole) a.stats[(size_t)part_slot * 16 * QT + row] = padding ? make_float2(-INFINITY, 0.f) : make_float2(m, total);
-                        else if (a.lse) a.lse[out_row * a.heads + head] = none ? -INFINITY : (m - kWeightBias + log2f(total)) / kLog2e;
+                    __syncthreads();
+                    if (here && share == 0) {
+                        float most = m;
+#pragma unroll 4
+                        for (int k = 1; k < shares; ++k) most = fmaxf(most, mine[(k << log_once) * ROW + HDP]);
+                        const float f0 = rescale(m, most);
+                        l *= f0;
+                        y *= f0;
+#pragma unroll 4
+                        for (int k = 1; k < shares; ++k) {
+                            const float* theirs = mine + (k << log_once) * ROW;
+                            const float f = rescale(theirs[HDP], most);
+                            l += theirs[HDP + 1] * f;
+                            y += *reinterpret_cast<const f32x4*>(theirs + d) * f;
+                        }
+                        leave(r0, y, most, l);
                     }
                 }
+                if (done) break;
+                level = 1;
+                from = 0;
+                stride = kAttendFan;
+                n_parts = runs;
             }
         }
         at += s1 - s0;
@@ -397,89 +615,25 @@ __global__ __launch_bounds__(256, QT * HDP <= 128 ? 2 : 1) void k_kv_attend(cons
     }
 }
 
-// ---- parts of items are added ------------------------------------------------------------------------------------------------
-// grid = (rows of a batch row's items x key heads, batch), block = 256: a workgroup per output row; its waves take the parts in turn.
 template <typename T, int HDP, int QT>
-__global__ __launch_bounds__(256) void k_kv_join(const KvView kv, const AttendArgs a, int grid) {
-    constexpr int N = Vec<T>::N, STAGE = 4 * N, STEP = STAGE * kAttendWaves, PER = (HDP + 63) / 64;
-    __shared__ int first[kKvMaxSeqs + 1];
-    __shared__ int wave_tot[4];
-    __shared__ float wave_m[4], wave_l[4], acc[4][HDP];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    if (kv.st->error) return;
-    plan_steps<STAGE, STEP>(kv, a, first, wave_tot);
-    const int i = blockIdx.y, rows = a.n_tokens * a.share, kvh = blockIdx.x / rows, abs_row = blockIdx.x % rows;
-    const int rb = abs_row / (16 * QT), row = abs_row % (16 * QT);
-    const int per_row = a.kv_heads * a.row_blocks, steps = first[i + 1] - first[i];
-    const long long all = (long long)first[a.batch] * per_row;
-    const long long groups = min((long long)grid, all);
-    const long long begin = (long long)first[i] * per_row + (long long)(kvh * a.row_blocks + rb) * steps;
-    // the workgroup that has step s: the last one whose first step is not above s
-    const int w0 = (int)(((begin + 1) * groups - 1) / all), w1 = (int)(((begin + steps) * groups - 1) / all);
-    if (w0 == w1) return;                      // the item was whole
-    float m = -INFINITY, l = 0.f, o[PER];
-#pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = 0.f;
-    for (int w = w0 + wv; w <= w1; w += 4) {
-        const size_t slot = 2 * (size_t)w + (all * w / groups >= begin ? 0 : 1), at = slot * 16 * QT + row;
-        const float2 s = a.stats[at];
-        float v[PER];
-#pragma unroll
-        for (int e = 0; e < PER; ++e) v[e] = lane * PER + e < HDP ? a.parts[at * HDP + lane * PER + e] : 0.f;
-        const float most = fmaxf(m, s.x), mine = rescale(m, most), theirs = rescale(s.x, most);
-        m = most;
-        l = l * mine + s.y * theirs;
-#pragma unroll
-        for (int e = 0; e < PER; ++e) o[e] = o[e] * mine + v[e] * theirs;
+void launch_attend(const AttendArgs& a, int groups, hipStream_t s) {
+    if (a.dim == HDP) {
+        hipLaunchKernelGGL((k_kv_attend<T, HDP, true, QT>), dim3(groups), dim3(256), 0, s, a);
+    } else if constexpr (HDP != 80 && QT <= 2) {
+        hipLaunchKernelGGL((k_kv_attend<T, HDP, false, QT>), dim3(groups), dim3(256), 0, s, a);
     }
-    if (lane == 0) {
-        wave_m[wv] = m;
-        wave_l[wv] = l;
-    }
-#pragma unroll
-    for (int e = 0; e < PER; ++e)
-        if (lane * PER + e < HDP) acc[wv][lane * PER + e] = o[e];
-    __syncthreads();
-    float most = -INFINITY, total = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) most = fmaxf(most, wave_m[w]);
-    const int tok = abs_row / a.share, head = kvh * a.share + abs_row % a.share;
-    const size_t out_row = (size_t)i * a.n_tokens + tok;
-    float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float scale = rescale(wave_m[w], most);
-        total += wave_l[w] * scale;
-        if (tid < HDP) v += acc[w][tid] * scale;
-    }
-    if (tid < a.dim) ((T*)a.out)[out_row * a.out_stride + (size_t)head * a.dim + tid] = (T)(total == 0.f ? 0.f : v / total);
-    if (tid == 0 && a.lse) a.lse[out_row * a.heads + head] = total == 0.f ? -INFINITY : (most - kWeightBias + log2f(total)) / kLog2e;
 }
 
-template <typename T, int HDP, int QT>
-void launch_attend(const KvView& kv, const AttendArgs& a, int groups, hipStream_t s) {
-    if (a.dim == HDP) hipLaunchKernelGGL((k_kv_attend<T, HDP, QT, true>), dim3(groups), dim3(256), 0, s, kv, a);
-    else hipLaunchKernelGGL((k_kv_attend<T, HDP, QT, false>), dim3(groups), dim3(256), 0, s, kv, a);
-    if (groups > 1)
-        hipLaunchKernelGGL((k_kv_join<T, HDP, QT>), dim3(a.n_tokens * a.heads, a.batch), dim3(256), 0, s, kv, a, groups);
-}
-
-template <typename T, int HDP>
-void launch_attend_tiles(const KvView& kv, const AttendArgs& a, int tiles, int groups, hipStream_t s) {
-    if (tiles == 1) return launch_attend<T, HDP, 1>(kv, a, groups, s);
-    if constexpr (HDP <= 128)
-        if (tiles == 4) return launch_attend<T, HDP, 4>(kv, a, groups, s);
-    launch_attend<T, HDP, 2>(kv, a, groups, s);
-}
-
-template <typename T>
-void launch_attend_as(const KvView& kv, const AttendArgs& a, int dim_pad, int tiles, int groups, hipStream_t s) {
-    switch (dim_pad) {
-        case 32: return launch_attend_tiles<T, 32>(kv, a, tiles, groups, s);
-        case 64: return launch_attend_tiles<T, 64>(kv, a, tiles, groups, s);
-        case 96: return launch_attend_tiles<T, 96>(kv, a, tiles, groups, s);
-        case 128: return launch_attend_tiles<T, 128>(kv, a, tiles, groups, s);
-        default: return launch_attend_tiles<T, 256>(kv, a, tiles, groups, s);
+template <typename T, int QT>
+void launch_attend_tiles(const AttendArgs& a, int groups, hipStream_t s) {
+    switch (attend_dim_pad(a.dim)) {
+        case 32: return launch_attend<T, 32, QT>(a, groups, s);
+        case 64: return launch_attend<T, 64, QT>(a, groups, s);
+        case 80: return launch_attend<T, 80, QT>(a, groups, s);
+        case 96: return launch_attend<T, 96, QT>(a, groups, s);
+        case 128: return launch_attend<T, 128, QT>(a, groups, s);
+        default:
+            if constexpr (QT == 1) launch_attend<T, 256, QT>(a, groups, s);
     }
 }
 

@@ -63,6 +63,7 @@ template <bool RESET>
 __global__ __launch_bounds__(256) void k_kv_clear(const KvView kv) {
     const long long step = (long long)gridDim.x * 256, at = (long long)blockIdx.x * 256 + threadIdx.x;
     if (at == 0) *kv.st = KvState{0, 0, 0, 0};
+    for (long long i = at; i < kv.n_arrived; i += step) kv.arrived[i] = 0;
     for (long long i = at; i < kv.pages; i += step) kv.refs[i] = 0;
     for (long long i = at; i < (kv.pages + 63) / 64; i += step) kv.free_bits[i] = free_word((int)i, kv.pages);
     if (RESET) {

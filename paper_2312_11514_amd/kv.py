@@ -67,7 +67,16 @@ class KVCache:
         h = C.c_void_p()
         _b._check(self.lib.lif_kv_create(C.byref(self.cfg), C.byref(self.buf), C.byref(h)))
         self.handle = h
+        self._bind()
         self.reset()
+
+    def _bind(self):
+        """What the calls of a decode step need again and again, as plain Python values; the argument structures are filled anew per call."""
+        c, torch = self.cfg, self.torch
+        self._heads, self._kv_heads, self._dim, self._seqs, self._gpu = c.heads, c.kv_heads, c.head_dim, c.max_seqs, self.table.get_device()
+        self._int32, self._float32, self._int64 = torch.int32, torch.float32, torch.int64
+        self._rows_arg, self._query_arg = _b.LifKvRows(), _b.LifKvQuery()
+        self._rows_ref, self._query_ref = C.byref(self._rows_arg), C.byref(self._query_arg)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -80,33 +89,39 @@ class KVCache:
         except Exception:
             pass
 
-    # ---- argument checks -------------------------------------------------------------------------------------------------
+    # ---- argument checks (on the path of every layer of a step) --------------------------------------------------------------
     def _ints(self, t, count, what):
-        if t.dtype != self.torch.int32 or t.numel() != count or not t.is_contiguous() or t.device != self.table.device:
+        if t.dtype is not self._int32 or t.numel() != count or t.get_device() != self._gpu or not t.is_contiguous():
             _refuse(f"{what} must be a contiguous int32 tensor of {count} elements beside the cache")
         return t.data_ptr()
 
-    def _rows(self, t, heads, what, like=None):
-        """[batch, tokens, heads, head_dim] with contiguous heads; any stride between tokens.  Returns the stride."""
-        b, n, h, d = t.shape if t.dim() == 4 else (0, 0, 0, 0)
-        sb, sn, sh, sd = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
-        if b == 1:
-            sb = n * sn
-        if n == 1:
-            sn = sb
-        if b == 1 and n == 1:
-            sn = sb = h * d
-        if h == 1:
-            sh = d
-        if (h != heads or d != self.cfg.head_dim or t.dtype != self.tdtype or sd != 1 or sh != d or sb != n * sn or
-                t.device != self.table.device or (like is not None and (b, n) != like)):
-            _refuse(f"{what} must be [batch, tokens, {heads}, {self.cfg.head_dim}] of the cache's type, heads contiguous, tokens at one stride")
-        return sn
+    def _slots(self, slots, batch):
+        if slots is not None:
+            return self._ints(slots, batch, "slots")
+        if batch > self._seqs:
+            _refuse("more rows than slots")
+        return None
+
+    def _rows(self, t, batch, tokens, heads, what):
+        """The stride between tokens of [batch, tokens, heads, head_dim], heads contiguous."""
+        d = self._dim
+        if t.dtype is self.tdtype and t.get_device() == self._gpu and t.shape == (batch, tokens, heads, d):
+            if t.is_contiguous():
+                return heads * d
+            sb, sn, sh, sd = t.stride()
+            if batch == 1:
+                sb = tokens * sn
+            if tokens == 1:
+                sn = sb if batch > 1 else heads * d
+                sb = sn
+            if sd == 1 and (sh == d or heads == 1) and sb == tokens * sn:
+                return sn
+        _refuse(f"{what} must be [{batch}, {tokens}, {heads}, {d}] of the cache's type beside the cache, heads contiguous, tokens at one stride")
 
     def _norm(self, t, what):
         if t is None:
             return None
-        if t.dtype != self.torch.float32 or t.numel() != self.cfg.head_dim or not t.is_contiguous() or t.device != self.table.device:
+        if t.dtype is not self._float32 or t.numel() != self._dim or t.get_device() != self._gpu or not t.is_contiguous():
             _refuse(f"{what} must be a contiguous float32 tensor of head_dim elements beside the cache")
         return t.data_ptr()
 
@@ -133,37 +148,43 @@ class KVCache:
     def append(self, layer, q, k, v, q_out, norm=None, positions=None, slots=None):
         """q, q_out [batch, tokens, heads, head_dim], k, v [batch, tokens, kv_heads, head_dim].  norm: (q weight, q bias, k weight, k bias),
         each float32 [head_dim] or None."""
-        shape = tuple(q.shape[:2])
-        qw, qb, kw, kb = norm if norm is not None else (None, None, None, None)
-        rows = _b.LifKvRows(
-            q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), self._rows(q, self.cfg.heads, "q"),
-            self._rows(k, self.cfg.kv_heads, "k", shape), self._rows(v, self.cfg.kv_heads, "v", shape),
-            self._rows(q_out, self.cfg.heads, "q_out", shape), self._norm(qw, "q weight"), self._norm(qb, "q bias"), self._norm(kw, "k weight"),
-            self._norm(kb, "k bias"), self._ints(positions, shape[0] * shape[1], "positions") if positions is not None else None,
-            self._slots(slots, shape[0]), shape[0], shape[1])
-        _b._check(self.lib.lif_kv_append(self.handle, layer, C.byref(rows), _b._stream()))
+        batch, tokens = q.shape[:2]
+        a = self._rows_arg
+        a.q_stride = self._rows(q, batch, tokens, self._heads, "q")
+        a.k_stride = self._rows(k, batch, tokens, self._kv_heads, "k")
+        a.v_stride = self._rows(v, batch, tokens, self._kv_heads, "v")
+        a.q_out_stride = self._rows(q_out, batch, tokens, self._heads, "q_out")
+        a.q, a.k, a.v, a.q_out = q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr()
+        if norm is None:
+            a.q_weight = a.q_bias = a.k_weight = a.k_bias = None
+        else:
+            a.q_weight, a.q_bias, a.k_weight, a.k_bias = (self._norm(t, what) for t, what in
+                                                          zip(norm, ("q weight", "q bias", "k weight", "k bias")))
+        a.positions = self._ints(positions, batch * tokens, "positions") if positions is not None else None
+        a.slots = self._slots(slots, batch)
+        a.batch, a.n_tokens = batch, tokens
+        _b._check(self.lib.lif_kv_append(self.handle, layer, self._rows_ref, _b._stream()))
 
     def attend(self, layer, q, out, lse=None, window=0, starts=None, tree=None, slots=None):
         """q, out [batch, tokens, heads, head_dim]; lse float32 [batch, tokens, heads]; starts int32 [batch]; tree int64 [batch, tokens], a
         bit per new token that is seen; slots int32 [batch]."""
-        shape, torch = tuple(q.shape[:2]), self.torch
-        q_stride, out_stride = self._rows(q, self.cfg.heads, "q"), self._rows(out, self.cfg.heads, "out", shape)
-        if lse is not None and (lse.dtype != torch.float32 or lse.numel() != shape[0] * shape[1] * self.cfg.heads or not lse.is_contiguous() or
-                                lse.device != self.table.device):
-            _refuse("lse must be a contiguous float32 tensor [batch, tokens, heads]")
-        if tree is not None and (tree.dtype != torch.int64 or tree.numel() != shape[0] * shape[1] or not tree.is_contiguous() or
-                                 tree.device != self.table.device):
-            _refuse("tree must be a contiguous int64 tensor [batch, tokens]")
-        query = _b.LifKvQuery(q.data_ptr(), out.data_ptr(), _b._ptr(lse), q_stride, out_stride, self._slots(slots, shape[0]),
-                              self._ints(starts, shape[0], "starts") if starts is not None else None, _b._ptr(tree), shape[0], shape[1], window)
-        _b._check(self.lib.lif_kv_attend(self.handle, layer, C.byref(query), _b._stream()))
+        batch, tokens = q.shape[:2]
+        a = self._query_arg
+        a.q_stride, a.out_stride = self._rows(q, batch, tokens, self._heads, "q"), self._rows(out, batch, tokens, self._heads, "out")
+        if lse is not None and (lse.dtype is not self._float32 or lse.numel() != batch * tokens * self._heads or
+                                lse.get_device() != self._gpu or not lse.is_contiguous()):
+            _refuse("lse must be a contiguous float32 tensor [batch, tokens, heads] beside the cache")
+        if tree is not None and (tree.dtype is not self._int64 or tree.numel() != batch * tokens or tree.get_device() != self._gpu or
+                                 not tree.is_contiguous()):
+            _refuse("tree must be a contiguous int64 tensor [batch, tokens] beside the cache")
+        a.q, a.out, a.lse, a.tree = q.data_ptr(), out.data_ptr(), _b._ptr(lse), _b._ptr(tree)
+        a.slots = self._slots(slots, batch)
+        a.starts = self._ints(starts, batch, "starts") if starts is not None else None
+        a.batch, a.n_tokens, a.window = batch, tokens, window
+        _b._check(self.lib.lif_kv_attend(self.handle, layer, self._query_ref, _b._stream()))
 
-    def _slots(self, slots, batch):
-        if slots is not None:
-            return self._ints(slots, batch, "slots")
-        if batch > self.cfg.max_seqs:
-            _refuse("more rows than slots")
-        return None
+    def set_expected_tokens(self, tokens: int):
+        _b._check(self.lib.lif_kv_set_expected_tokens(self.handle, int(tokens)))
 
     # ---- introspection ---------------------------------------------------------------------------------------------------
     def state(self) -> dict:
