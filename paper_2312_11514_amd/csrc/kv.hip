@@ -67,27 +67,46 @@ struct KvLayout {
     size_t state, arrived, free_bits, moves, remap, parts, total;
 };
 
-// How the rows of an item, tokens x query heads of a key head, are dealt: blocks of 16 * tiles rows, `positions` to go through at most.
+// How the rows of an item, tokens x query heads of a key head, are dealt: blocks of 16 * tiles rows, and workgroups for each of them.
+// `positions`: of a sequence to go through, at most.
 // A workgroup reads the keys once for its block, so blocks are as large as registers allow; where there are so few that all their steps
-// run at once, the time is that of one workgroup, and smaller ones are faster.
+// run at once, the time is that of one workgroup, and smaller ones are faster (71 rows, 8 sequences of up to 2047: 9.6 us with blocks of 16,
+// 25.9 with 64).
 struct Tiling {
-    int tiles, blocks, block_rows;
-    long long steps;                     // of all items, at most
+    int tiles, blocks, block_rows, units;
+    long long steps;                     // of a block's items, at most
 };
+// The workgroups of few blocks are what fits the chip, in eights (those of one XCD share keys); of many blocks four rounds and more of
+// shorter ones, to end together; of very many blocks they are enough by themselves, and no item has parts.
+int units_of(int blocks, int resident) {
+    if (blocks == 1) return resident;
+    if (blocks <= 8) return std::max(8, resident / blocks / 8 * 8);
+    if (blocks <= 128) return (128 + blocks - 1) / blocks * 8;
+    return 1;
+}
 Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) {
     const int step = 4 * 16 / elem_bytes(c.dtype) * kAttendWaves, need = (rows + 15) / 16;
-    const long long per_item = (positions + step - 1) / step + 1;
     Tiling g;
+    g.steps = (long long)batch * c.kv_heads * ((positions + step - 1) / step + 1);
     g.tiles = std::min(attend_most_tiles(c.head_dim), need <= 1 ? 1 : need <= 2 ? 2 : 4);
-    while (g.tiles > 1 && (long long)batch * c.kv_heads * ((need + g.tiles / 2 - 1) / (g.tiles / 2)) * per_item <= kAttendFew) g.tiles /= 2;
+    while (g.tiles > 1 && g.steps * ((need + g.tiles / 2 - 1) / (g.tiles / 2)) <= kAttendFew) g.tiles /= 2;
     g.blocks = (need + g.tiles - 1) / g.tiles;
     g.block_rows = std::min(rows, 16 * g.tiles);
-    g.steps = (long long)batch * c.kv_heads * g.blocks * per_item;
+    g.units = units_of(g.blocks, kAttendUnits * attend_resident(attend_dim_pad(c.head_dim), g.tiles));
     return g;
 }
-// rows of the largest block of any call
-int most_block_rows(const lif_kv_config& c) {
-    return std::min(c.max_tokens * (c.heads / c.kv_heads), 16 * attend_most_tiles(c.head_dim));
+// floats of the parts of any call
+size_t most_part_floats(const lif_kv_config& c) {
+    const int rows = c.max_tokens * (c.heads / c.kv_heads), need = (rows + 15) / 16, pad = attend_dim_pad(c.head_dim);
+    size_t most = 0;
+    for (int tiles = 1; tiles <= attend_most_tiles(c.head_dim); tiles *= 2) {
+        // fewer rows than the largest call's make fewer blocks, and more workgroups for each: the products below are at their largest in between
+        for (int blocks = 1; blocks <= std::min(129, (need + tiles - 1) / tiles); ++blocks) {
+            const size_t groups = (size_t)blocks * units_of(blocks, kAttendUnits * attend_resident(pad, tiles));
+            if (blocks <= 128) most = std::max(most, 4 * groups * std::min(rows, 16 * tiles) * (pad + 4));
+        }
+    }
+    return most;
 }
 
 KvLayout make_layout(const lif_kv_config& c) {
@@ -96,16 +115,15 @@ KvLayout make_layout(const lif_kv_config& c) {
     L.state = off;
     off = align_up(off + sizeof(KvState), 256);
     L.arrived = off;                   // directly behind the state: a reset clears both
-    off = align_up(off + sizeof(unsigned) * 4 * kAttendGroups, 256);
+    off = align_up(off + sizeof(unsigned) * 4 * kAttendMost, 256);
     L.free_bits = off;
     off = align_up(off + sizeof(unsigned long long) * ((size_t)(c.pages + 63) / 64), 256);
     L.moves = off;
     off = align_up(off + sizeof(int2) * c.pages, 256);
     L.remap = off;
     off = align_up(off + sizeof(int32_t) * std::max(c.pages, c.max_seqs), 256);
-    const size_t rows = (size_t)4 * kAttendGroups * most_block_rows(c);
     L.parts = off;
-    off = align_up(off + sizeof(float) * rows * (attend_dim_pad(c.head_dim) + 4), 256);
+    off = align_up(off + sizeof(float) * most_part_floats(c), 256);
     L.total = off;
     return L;
 }
@@ -171,7 +189,7 @@ int lif_kv_create(const lif_kv_config* cfg, const lif_kv_buffers* buf, lif_kv** 
     v.refs = buf->refs;
     v.st = reinterpret_cast<KvState*>(w + L.state);
     v.arrived = reinterpret_cast<unsigned*>(w + L.arrived);
-    v.n_arrived = 4 * kAttendGroups;
+    v.n_arrived = 4 * kAttendMost;
     v.free_bits = reinterpret_cast<unsigned long long*>(w + L.free_bits);
     v.moves = reinterpret_cast<int2*>(w + L.moves);
     v.remap = reinterpret_cast<int32_t*>(w + L.remap);
@@ -280,22 +298,21 @@ int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* st
     const int share = c.heads / c.kv_heads, rows = query->n_tokens * share;
     const long long width = (long long)c.max_pages * c.page_tokens;
     const Tiling g = tiling(c, query->batch, rows, kv->expected ? std::min<long long>(kv->expected, width) : width);
-    const long long most = tiling(c, query->batch, rows, width).steps * 4;      // (in blocks of any size)
-    if (most >= (1ll << 31) - kAttendGroups) return fail(LIF_INVALID_ARG, "batch, heads and the width of the table are too large together");
+    if (tiling(c, query->batch, rows, width).steps >= (1ll << 31) - 4096)
+        return fail(LIF_INVALID_ARG, "batch, heads and the width of the table are too large together");
     const KvView& v = kv->view;
     const size_t layer_at = (size_t)layer * c.pages * v.page_bytes;
     AttendArgs a{static_cast<const char*>(query->q), static_cast<char*>(query->out), query->lse, query->q_stride, query->out_stride,
                  query->slots, query->starts, reinterpret_cast<const unsigned long long*>(query->tree), v.k + layer_at, v.v + layer_at, v.table,
                  v.lengths, v.fresh, &v.st->error, kv->parts, kv->arrived, (unsigned)kv->part_bytes, (unsigned)v.page_bytes,
                  (unsigned)(v.page_bytes / c.kv_heads), c.pages, c.max_seqs, c.max_pages, v.log_page, query->batch, query->n_tokens, c.heads,
-                 c.kv_heads, share, c.head_dim, query->window, g.blocks, g.block_rows, c.scale * kLog2e};
-    const int groups = (int)std::min<long long>(kAttendUnits * attend_resident(attend_dim_pad(c.head_dim), g.tiles), most);      // (at most a step for each)
+                 c.kv_heads, share, c.head_dim, query->window, g.units, g.blocks, g.block_rows, c.scale * kLog2e};
     hipStream_t s = (hipStream_t)stream;
     using Launch = void (*)(const AttendArgs&, int, hipStream_t);
     static constexpr Launch kLaunch[3][3] = {{launch_attend_f32_1, launch_attend_f32_2, launch_attend_f32_4},
                                              {launch_attend_f16_1, launch_attend_f16_2, launch_attend_f16_4},
                                              {launch_attend_bf16_1, launch_attend_bf16_2, launch_attend_bf16_4}};
-    kLaunch[c.dtype][g.tiles >> 1](a, groups, s);
+    kLaunch[c.dtype][g.tiles >> 1](a, g.blocks * g.units, s);
     return launched();
 }
 

@@ -26,7 +26,7 @@
 namespace lif {
 
 constexpr int kAttendUnits = 256;        // compute units
-constexpr int kAttendGroups = 512;       // workgroups at most: two per compute unit
+constexpr int kAttendMost = 2048;        // workgroups of a call that may leave parts
 constexpr int kAttendWaves = 4;
 constexpr int kAttendFan = 16;           // parts that one workgroup adds at most; of more, such sums are added again
 constexpr int kAttendAsk = 8;            // ... and asks for at once
@@ -49,13 +49,14 @@ struct AttendArgs {
     const int32_t* lengths;
     const int32_t* fresh;
     const int32_t* error;
-    float* parts;                          // [2][2 * kAttendGroups][rows of a block][dim_pad + 4] sums, unscaled; maximum (log2) and sum behind
+    float* parts;                          // [2][2 * workgroups][rows of a block][dim_pad + 4] sums, unscaled; maximum (log2) and sum behind
                                            // them; of the parts, and of their runs
-    unsigned* arrived;                     // [2][2 * kAttendGroups] parts written; zero between calls
+    unsigned* arrived;                     // [2][2 * workgroups] parts written; zero between calls
     unsigned part_bytes;                   // of `parts`
     unsigned page_bytes, head_bytes;       // of the keys of a page, and of one head of them
     int32_t pages, max_seqs, max_pages, log_page;
     int32_t batch, n_tokens, heads, kv_heads, share, dim, window;
+    int32_t units;                         // workgroups of a block of rows
     int32_t row_blocks, block_rows;        // blocks of 16 * tiles rows of an item; rows of a block that are there at most
     float scale_log2;                      // scale * log2 e
 };
@@ -126,9 +127,13 @@ __device__ __forceinline__ float rescale(float m, float most) { return m == most
 
 // ---- how the steps are dealt -------------------------------------------------------------------------------------------------
 // A batch row of length n, f of its tokens new, has the positions [low, n) to go through, in steps from low rounded down to a stage on; a
-// row with nothing to do has one step (it writes zeros).  Its items, key heads x blocks of rows, have the same.  The steps of all items, by
-// batch row, key head, block and position, are dealt in runs of equal length.  Every wave works this out by itself, 64 batch rows at a
-// time, one to a lane: for up to 64 that is no LDS and no barrier.
+// row with nothing to do has one step (it writes zeros).  Its items, one per key head, have the same.  The steps of all items, by
+// batch row, key head and position, are dealt to the `units` workgroups of a block of rows in runs:
+//   by items    every item in as many equal parts as it takes for none to be longer than the even share (or an eighth more), if that needs
+//               no more workgroups than there are: a workgroup then begins and ends one part.  16 sequences of 15 steps, 8 key heads, 512
+//               workgroups: 29.5 us against 31.1 with runs that go on into the next item
+//   evenly      else: runs of equal length across the items (many items, or few steps for each workgroup)
+// Every wave works this out by itself, 64 batch rows at a time, one to a lane: for up to 64 that is no LDS and no barrier.
 struct RowRange {
     int n, fresh, start, slot;             // length, new tokens, first visible position, slot
 };
@@ -209,21 +214,71 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
     if (whole_wave(error)) return;
     int total = rc.after;
     for (int c0 = 64; c0 < a.batch; c0 += 64) total = row_chunk(a, STAGE, STEP, c0, total).after;
-    const int per_row = a.kv_heads * a.row_blocks, rows = a.n_tokens * a.share;
-    const int all = total * per_row;           // (below 2^31: lif_kv_attend has seen to it)
-    const int run_steps = quotient(all + (int)gridDim.x - 1, (int)gridDim.x);
-    const int end = (int)min((unsigned)run_steps * (blockIdx.x + 1), (unsigned)all);
-    int at = (int)min((unsigned)run_steps * blockIdx.x, (unsigned)all);
+    // which block of rows, and which of its workgroups: those that read the same keys are eight apart, on one XCD
+    int block = 0, unit = blockIdx.x;
+    if (a.row_blocks > 1) {
+        if (a.units % 8 == 0) {
+            const int eights = (int)blockIdx.x >> 3, high = quotient(eights, a.row_blocks);
+            block = eights - high * a.row_blocks;
+            unit = high * 8 + ((int)blockIdx.x & 7);
+        } else {
+            block = quotient(blockIdx.x, a.units);
+            unit = (int)blockIdx.x - block * a.units;
+        }
+    }
+    const int slots0 = 2 * block * a.units;    // the block's first place for a part
+    const int rows = a.n_tokens * a.share, row0 = block * QT * 16;
+    const int all = total * a.kv_heads;        // (below 2^31: lif_kv_attend has seen to it)
+    int run_steps = quotient(all + a.units - 1, a.units);
+    // by items: parts of the lane's row, steps of each, parts of the rows before
+    int parts_of_row = 0, part_steps = 1, parts_before = 0;
+    bool by_items = false;
+    if (a.batch <= 64) {
+        for (int tries = 0; tries < 2 && !by_items; ++tries) {
+            const int most = run_steps + (tries ? run_steps / 8 : 0);
+            parts_of_row = (int)((unsigned)(rc.steps + most - 1) / (unsigned)most);
+            part_steps = max(1, (int)((unsigned)(rc.steps + parts_of_row - 1) / (unsigned)max(parts_of_row, 1)));
+            parts_of_row = (int)((unsigned)(rc.steps + part_steps - 1) / (unsigned)part_steps);
+            const int up_to = wave_inclusive_scan(parts_of_row, lane);
+            parts_before = up_to - parts_of_row;
+            const int needed = __builtin_amdgcn_readlane(up_to, 63) * a.kv_heads;
+            by_items = needed <= a.units;
+            if (by_items && unit >= needed) return;
+            if (run_steps < 8) break;
+        }
+    }
+    const int end = by_items ? 1 : (int)min((unsigned)run_steps * ((unsigned)unit + 1u), (unsigned)all);
+    int at = by_items ? 0 : (int)min((unsigned)run_steps * (unsigned)unit, (unsigned)all);
     bool first_segment = true;
 
     while (at < end) {
-        while (rc.after * per_row <= at) rc = row_chunk(a, STAGE, STEP, rc.first + 64, rc.after);
-        // the last row that begins at or before the step (rows behind the batch have no steps, and begin behind it)
-        const int il = __popcll(__ballot(rc.before * per_row <= at && rc.steps > 0)) - 1, i = rc.first + il;
-        const int before = __builtin_amdgcn_readlane(rc.before, il), steps = __builtin_amdgcn_readlane(rc.steps, il);
+        int il, s0, s1, steps, kvh, w0, count;             // lane of the batch row, steps, key head, workgroups that share the item
+        bool begins_before = false;                        // the first of them has steps of another item before
+        if (by_items) {
+            il = __popcll(__ballot(parts_before * a.kv_heads <= unit && rc.steps > 0)) - 1;
+            steps = __builtin_amdgcn_readlane(rc.steps, il);
+            count = __builtin_amdgcn_readlane(parts_of_row, il);
+            const int in_row = unit - __builtin_amdgcn_readlane(parts_before, il) * a.kv_heads, each = __builtin_amdgcn_readlane(part_steps, il);
+            kvh = quotient(in_row, count);
+            w0 = unit - (in_row - kvh * count);
+            s0 = (unit - w0) * each;
+            s1 = min(steps, s0 + each);
+        } else {
+            while (rc.after * a.kv_heads <= at) rc = row_chunk(a, STAGE, STEP, rc.first + 64, rc.after);
+            // the last row that begins at or before the step (rows behind the batch have no steps, and begin behind it)
+            il = __popcll(__ballot(rc.before * a.kv_heads <= at && rc.steps > 0)) - 1;
+            steps = __builtin_amdgcn_readlane(rc.steps, il);
+            const int in_row = at - __builtin_amdgcn_readlane(rc.before, il) * a.kv_heads;
+            kvh = quotient(in_row, steps);
+            s0 = in_row - kvh * steps;
+            s1 = min(steps, s0 + end - at);
+            const int begin = at - s0;
+            w0 = quotient(begin, run_steps);
+            count = quotient(begin + steps - 1, run_steps) - w0 + 1;
+            begins_before = w0 * run_steps < begin;
+        }
+        const int i = rc.first + il;
         const RowRange r = of_lane(rc.range, il);
-        const int in_row = at - before * per_row, item = quotient(in_row, steps), s0 = in_row - item * steps, s1 = min(steps, s0 + end - at);
-        const int kvh = a.row_blocks == 1 ? item : quotient(item, a.row_blocks), row0 = (item - kvh * a.row_blocks) * QT * 16;
         const int base = r.n - r.fresh, low_all = low_of(r, 0, a.window);
 
         // the lane's rows: first position it sees, last new token and which of those it sees, query
@@ -432,7 +487,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
 
         // the waves' sums meet
         const bool whole = s0 == 0 && s1 == steps;
-        const int part = 2 * blockIdx.x + (first_segment ? 0 : 1);
+        const int part = slots0 + 2 * unit + (first_segment ? 0 : 1);
         const int rows_here = min(16 * QT, rows - row0);
         // four dimensions of a row of the output
         auto finish = [&](int r0, int d, f32x4 v, float m, float total) {
@@ -501,20 +556,17 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
             }
         }
 
-        // Parts: the workgroups w0 .. w1 have steps of the item, each has left one part (its last segment, or its first if it begins in the
-        // item).  Runs of kAttendFan of them are added by the last one of the run, into the place of the run's first part, and the runs by the
+        // Parts: each of the `count` workgroups from w0 on has left one (the first of them its last segment, if it began before the item).  Runs of kAttendFan of them are added by the last one of the run, into the place of the run's first part, and the runs by the
         // last run.
         if (!whole) {
-            const int begin = at - s0, w0 = quotient(begin, run_steps), w1 = quotient(begin + steps - 1, run_steps);
-            const int count = w1 - w0 + 1, run = ((int)blockIdx.x - w0) / kAttendFan, runs = (count + kAttendFan - 1) / kAttendFan;
-            const bool begins_before = w0 * run_steps < begin;
-            auto part_of = [&](int k) { return 2 * (w0 + k) + (k == 0 && begins_before ? 1 : 0); };
+            const int run = (unit - w0) / kAttendFan, runs = (count + kAttendFan - 1) / kAttendFan, level2 = 2 * (int)gridDim.x;
+            auto part_of = [&](int k) { return slots0 + 2 * (w0 + k) + (k == 0 && begins_before ? 1 : 0); };
             int level = 0, from = run * kAttendFan, stride = 1, n_parts = min(kAttendFan, count - from);
             while (true) {
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // this wave's stores are acknowledged,
                 __syncthreads();                                             // and those of the others
                 if (tid == 0)
-                    last = n_parts == 1 || (int)atomicInc(a.arrived + level * 2 * kAttendGroups + part_of(from), (unsigned)n_parts - 1u) == n_parts - 1;
+                    last = n_parts == 1 || (int)atomicInc(a.arrived + level * level2 + part_of(from), (unsigned)n_parts - 1u) == n_parts - 1;
                 __syncthreads();
                 if (!whole_wave(last)) break;
                 const bool done = level == 1 || runs == 1;
@@ -530,7 +582,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                     if (done) {
                         finish(r0, d, y, m, l);
                     } else {
-                        const unsigned b = part_at(2 * kAttendGroups + part_of(from), r0);
+                        const unsigned b = part_at(level2 + part_of(from), r0);
                         store_through(parts, b + d * 4, a.part_bytes, y);
                         if (d == 0) store_through(parts, b + HDP * 4, a.part_bytes, f32x4{m, l, 0.f, 0.f});
                     }
@@ -544,7 +596,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
 #pragma unroll
                     for (int e = 0; e < kAttendAsk; ++e)
                         if (u0 + e < units) {
-                            const unsigned b = part_at(level * 2 * kAttendGroups + part_of(from + min(share * per + e_ask, n_parts - 1) * stride),
+                            const unsigned b = part_at(level * level2 + part_of(from + min(share * per + e_ask, n_parts - 1) * stride),
                                                        min(r_ask, rows_here - 1));
                             s[e] = load_through2(a.parts, b + HDP * 4, a.part_bytes);
                             v[e] = load_through(a.parts, b + d * 4, a.part_bytes);
@@ -610,6 +662,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                 n_parts = runs;
             }
         }
+        if (by_items) break;
         at += s1 - s0;
         first_segment = false;
     }
