@@ -30,6 +30,7 @@ namespace {
 
 constexpr long long kMaxPositions = 1 << 24;     // of a sequence: the steps of 1024 of them are counted in 32 bits
 constexpr int kAttendFew = 1024;                 // steps that run at once, or nearly
+constexpr int kAppendGroups = 2048;              // workgroups for queries and keys that fill the chip
 constexpr int kMoveBlocks = 2048;                // 8 workgroups of copies per compute unit
 constexpr int kCopyBlocks = 256;                 // ... behind lif_kv_reserve, which has a page to copy once in a while
 
@@ -269,19 +270,22 @@ int lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* rows, void* stre
     LIF_TRY(stride_ok(kv, rows->v_stride, c.kv_heads));
     AppendArgs a{static_cast<const char*>(rows->q), static_cast<const char*>(rows->k), static_cast<const char*>(rows->v),
                  static_cast<char*>(rows->q_out), rows->q_stride, rows->k_stride, rows->v_stride, rows->q_out_stride,
-                 rows->q_weight, rows->q_bias, rows->k_weight, rows->k_bias, kv->frequencies, rows->positions, rows->slots,
-                 rows->n_tokens, c.heads, c.kv_heads, c.head_dim, layer, c.rotary_dim, c.norm, 0, c.norm_eps, c.rotary_scale};
-    const int count = rows->batch * rows->n_tokens, all = c.heads + 2 * c.kv_heads;
-    const int at_once = 256 / lanes_of_head(c.head_dim, 16 / elem_bytes(c.dtype));
-    // few rows: a workgroup per heads_at_once heads, to have the whole chip at it; many: all heads of a row by one, angles computed once
-    const int wanted = std::max(1, 2048 / count), blocks = std::min((all + at_once - 1) / at_once, wanted);
+                 rows->q_weight, rows->q_bias, rows->k_weight, rows->k_bias, kv->frequencies, rows->positions, rows->slots, rows->batch,
+                 rows->n_tokens, c.heads, c.kv_heads, c.head_dim, layer, c.rotary_dim, c.norm, 0, 0, 0, 0, 0, c.norm_eps, c.rotary_scale};
+    const int count = rows->batch * rows->n_tokens, all = c.heads + c.kv_heads, n = 16 / elem_bytes(c.dtype);
+    while ((n << a.log_lanes) < c.head_dim) ++a.log_lanes;
+    const int at_once = 256 >> a.log_lanes;
+    // few tokens: a workgroup for as many heads as it takes at once, to have the whole chip at it; many: more heads each, angles once for them
+    const int wanted = std::max(1, kAppendGroups / count), blocks = std::min((all + at_once - 1) / at_once, wanted);
     a.heads_per_block = ((all + blocks - 1) / blocks + at_once - 1) / at_once * at_once;
-    const int grid = (all + a.heads_per_block - 1) / a.heads_per_block;
+    a.head_blocks = (all + a.heads_per_block - 1) / a.heads_per_block;
+    a.pieces = (rows->n_tokens + n - 2) / n + 1;
+    a.value_blocks = (c.kv_heads * c.head_dim * elem_bytes(c.dtype) / 4 + 255) / 256;
     const bool interleaved = c.rotary == LIF_ROTARY_INTERLEAVED;
     hipStream_t s = (hipStream_t)stream;
-    if (c.dtype == LIF_F32) launch_append_f32(kv->view, a, interleaved, count, grid, s);
-    else if (c.dtype == LIF_F16) launch_append_f16(kv->view, a, interleaved, count, grid, s);
-    else launch_append_bf16(kv->view, a, interleaved, count, grid, s);
+    if (c.dtype == LIF_F32) launch_append_f32(kv->view, a, interleaved, s);
+    else if (c.dtype == LIF_F16) launch_append_f16(kv->view, a, interleaved, s);
+    else launch_append_bf16(kv->view, a, interleaved, s);
     return launched();
 }
 

@@ -1,7 +1,5 @@
 #include "lif_kv_append.h"
 
 namespace lif {
-void launch_append_bf16(const KvView& kv, const AppendArgs& a, bool interleaved, int rows, int blocks, hipStream_t s) {
-    launch_append_as<__bf16>(kv, a, interleaved, rows, blocks, s);
-}
+void launch_append_bf16(const KvView& kv, const AppendArgs& a, bool interleaved, hipStream_t s) { launch_append_as<__bf16>(kv, a, interleaved, s); }
 }  // namespace lif

@@ -4,10 +4,13 @@
 //   (x, y) -> (x cos a - y sin a, x sin a + y cos a) * magnitude with a = position * frequency.
 //
 // What bounds it: for a few tokens the chain slot -> length -> table entry -> store (three dependent round trips) and the launch; for
-// prompts the bytes, each read and written once.  A lane holds 16 bytes of a head, a power of two of lanes a head, so the sums of a norm
-// are a few lane exchanges; the other half of a pair (half layout) is a second 16-byte load of the same line and not an exchange,
-// since it is normalised with other weights anyway.  The angles belong to the lane's dimensions and the token, not to the head: a wave
-// computes them once and goes through its heads with them.
+// prompts the bytes, each read and written once.
+// Queries and keys: a workgroup has one token, and computes its angles once, one pair to a thread, for all heads.  A lane holds 16 bytes of
+// a head, a power of two of lanes a head, so the sums of a norm are a few lane exchanges; the other half of a pair (half layout) is a second
+// 16-byte load of the same line and not an exchange, since it is normalised with other weights anyway.
+// Values: the cache keeps N consecutive tokens of a dimension in 16 bytes.  Written token by token, from workgroups on different XCDs,
+// those are N writes of a part of a line each; a workgroup takes the N tokens of a piece together and writes it whole where it has all of them
+// (32 prompts of up to 64 tokens, 64 heads of 64: 66.0 us before, with angles per lane).
 #pragma once
 
 #include "lif_kv.h"
@@ -20,6 +23,8 @@ template <> struct Vec<__bf16> {
     static constexpr int N = 8;
 };
 
+constexpr int kAppendAhead = 4;           // heads that a thread asks for at once
+
 struct AppendArgs {
     const char *q, *k, *v;
     char* q_out;
@@ -28,27 +33,41 @@ struct AppendArgs {
     const double* frequencies;
     const int32_t* positions;
     const int32_t* slots;
-    int32_t n_tokens, heads, kv_heads, dim, layer, rotary_dim, norm, heads_per_block;
+    int32_t batch, n_tokens, heads, kv_heads, dim, layer, rotary_dim, norm;
+    int32_t log_lanes;                         // lanes that share a head: the pieces of 16 bytes, rounded up to a power of two
+    int32_t head_blocks, heads_per_block;      // workgroups of a token for its queries and keys, and heads of each
+    int32_t pieces, value_blocks;              // pieces of N positions that a batch row's new tokens may lie in, workgroups of a piece
     float eps, magnitude;
 };
 
-void launch_append_f16(const KvView& kv, const AppendArgs& a, bool interleaved, int rows, int blocks, hipStream_t s);
-void launch_append_bf16(const KvView& kv, const AppendArgs& a, bool interleaved, int rows, int blocks, hipStream_t s);
-void launch_append_f32(const KvView& kv, const AppendArgs& a, bool interleaved, int rows, int blocks, hipStream_t s);
+void launch_append_f16(const KvView& kv, const AppendArgs& a, bool interleaved, hipStream_t s);
+void launch_append_bf16(const KvView& kv, const AppendArgs& a, bool interleaved, hipStream_t s);
+void launch_append_f32(const KvView& kv, const AppendArgs& a, bool interleaved, hipStream_t s);
 
-// lanes that share a head: the pieces of 16 bytes, rounded up to a power of two
-__host__ __device__ __forceinline__ int lanes_of_head(int dim, int per_piece) {
-    int lanes = 1;
-    while (lanes * per_piece < dim) lanes *= 2;
-    return lanes;
-}
-
+// sum over groups of `lanes` lanes (the same number everywhere), in every one of them: register moves, no round trips through the LDS
 __device__ __forceinline__ float group_sum(float v, int lanes) {
-    for (int m = 1; m < lanes; m *= 2) v += __shfl_xor(v, m);
+    if (lanes >= 2) v += dpp_from<0xb1, 0xf>(v);               // pairs swapped
+    if (lanes >= 4) v += dpp_from<0x4e, 0xf>(v);               // pairs of pairs
+    if (lanes >= 8) v += from_xor<4>(v);
+    if (lanes >= 16) v += from_xor<8>(v);
+    if (lanes >= 32) v = swap_add<16>(v, v);
+    if (lanes >= 64) v = swap_add<32>(v, v);
     return v;
 }
 
-// cos and sin of 2 pi * position * frequency / (2 pi): reduced in fp64, where position * frequency is good to 2^-52 of itself
+// N floats at any float's address
+template <int N>
+__device__ __forceinline__ void load_floats(const float* from, float (&to)[N]) {
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+        const f4 v = *reinterpret_cast<const f4*>(from + e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[e + j] = v[j];
+    }
+}
+
+// cos and sin of position * frequency: reduced in fp64, where the product is good to 2^-52 of itself
 __device__ __forceinline__ void turn(double position, double frequency, float magnitude, float& c, float& s) {
     const double half_turns = position * frequency * 0.31830988618379067154;       // angle / pi
     const double rest = half_turns - 2.0 * __builtin_rint(0.5 * half_turns);       // -1 .. 1
@@ -57,84 +76,165 @@ __device__ __forceinline__ void turn(double position, double frequency, float ma
     s *= magnitude;
 }
 
-// grid = (rows, blocks of heads), block = 256.  Heads are numbered queries, keys, values; a workgroup takes heads_per_block of them.
-template <typename T, bool INTERLEAVED>
+// new tokens of batch row i: slot, length, how many
+struct NewTokens {
+    int slot, length, fresh;
+};
+__device__ __forceinline__ NewTokens new_tokens(const KvView& kv, const AppendArgs& a, int i) {
+    NewTokens t{a.slots ? a.slots[i] : i, 0, 0};
+    if ((unsigned)t.slot < (unsigned)kv.max_seqs) {
+        t.length = length_of(kv, t.slot);
+        t.fresh = min(max(kv.fresh[t.slot], 0), t.length);
+    }
+    return t;
+}
+
+// Values of the positions N p .. N p + N - 1 of a batch row, p counted from the piece of its first new token on; 256 threads, each
+// 4 bytes of a token at a time.
+template <typename T>
+__device__ __forceinline__ void append_values(const KvView& kv, const AppendArgs& a, int i, int unit) {
+    using V = typename Vec<T>::type;
+    constexpr int N = Vec<T>::N, W = 4 / (int)sizeof(T);       // dimensions in 4 bytes
+    const int p = (int)((unsigned)unit / (unsigned)a.value_blocks), block = unit - p * a.value_blocks;
+    const int error = kv.st->error;
+    const NewTokens n = new_tokens(kv, a, i);
+    const int first = n.length - n.fresh, low = (first / N + p) * N;                  // position of the piece's first token
+    if (error || n.fresh == 0 || low >= min(n.length, first + a.n_tokens)) return;
+    const int page = kv.table[(size_t)n.slot * kv.max_pages + (low >> kv.log_page)], width = a.kv_heads * a.dim;
+    if (!page_ok(kv, page)) return;
+    const int t0 = low - first, t_end = min(n.fresh, a.n_tokens);                     // token of the piece's first position; negative: an older one
+    const T* from = (const T*)a.v + ((long long)i * a.n_tokens + t0) * a.v_stride;
+    T* page_at = (T*)kv.v + (((size_t)a.layer * kv.pages + page) * a.kv_heads << kv.log_page) * a.dim;
+    const int piece = (low & ((1 << kv.log_page) - 1)) / N;
+    for (int c = (block * 256 + (int)threadIdx.x) * W; c < width; c += a.value_blocks * 256 * W) {
+        const int h = (int)((unsigned)c / (unsigned)a.dim), d = c - h * a.dim;
+        T* to = page_at + ((size_t)h << kv.log_page) * a.dim + (size_t)(piece * a.dim + d) * N;
+        unsigned w[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[e] = t0 + e >= 0 && t0 + e < t_end ? *reinterpret_cast<const unsigned*>(from + e * a.v_stride + c) : 0u;
+        V out[W];
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                if constexpr (W == 1) out[j][e] = __builtin_bit_cast(T, w[e]);
+                else out[j][e] = __builtin_bit_cast(T, (unsigned short)(w[e] >> (16 * j)));
+            }
+        if (t0 >= 0 && t0 + N <= t_end) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) *reinterpret_cast<V*>(to + j * N) = out[j];
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (t0 + e >= 0 && t0 + e < t_end) {
+#pragma unroll
+                    for (int j = 0; j < W; ++j) to[j * N + e] = out[j][e];
+                }
+        }
+    }
+}
+
+// grid = (n_tokens * head_blocks workgroups for queries and keys, then pieces * value_blocks for values; batch), block = 256
+template <typename T, bool INTERLEAVED, bool NORM>
 __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const AppendArgs a) {
     using V = typename Vec<T>::type;
     constexpr int N = Vec<T>::N;
-    const int row = blockIdx.x, i = row / a.n_tokens, t = row % a.n_tokens;
-    const int error = kv.st->error;
-    const int slot = a.slots ? a.slots[i] : i;
-    int length = 0, fresh = 0;
-    if ((unsigned)slot < (unsigned)kv.max_seqs) {
-        length = length_of(kv, slot);
-        fresh = min(max(kv.fresh[slot], 0), length);
+    __shared__ float cosine[128], sine[128];                   // of the token's pairs
+    const int unit = blockIdx.x, i = blockIdx.y;
+    if (unit >= a.n_tokens * a.head_blocks) {
+        append_values<T>(kv, a, i, unit - a.n_tokens * a.head_blocks);
+        return;
     }
-    if (error) return;
-    const bool there = t < fresh;
-    const int at = there ? length - fresh + t : 0;
-    int page = -1;
-    if (there) page = kv.table[(size_t)slot * kv.max_pages + (at >> kv.log_page)];
-    const int offset = at & ((1 << kv.log_page) - 1);
-    const bool store = there && page_ok(kv, page);
-
-    const int lanes = lanes_of_head(a.dim, N), lane = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = 256 / lanes;
-    const int d0 = lane * N, half = a.rotary_dim / 2;
+    const int t = a.head_blocks == 1 ? unit : (int)((unsigned)unit / (unsigned)a.head_blocks), row = i * a.n_tokens + t, half = a.rotary_dim / 2;
+    const int lanes = 1 << a.log_lanes, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.log_lanes, groups = 256 >> a.log_lanes;
+    const int d0 = lane * N;
     const bool mine = d0 < a.dim;
     // half layout: all of the lane's dimensions turn or none, all on one side of their pairs
     const bool turns = mine && d0 < a.rotary_dim, upper = !INTERLEAVED && d0 >= half;
     const int d1 = !turns || INTERLEAVED ? d0 : upper ? d0 - half : d0 + half;
+    const int first = (unit - t * a.head_blocks) * a.heads_per_block, last = min(first + a.heads_per_block, a.heads + a.kv_heads);
+    // The lane's dimensions of its next heads, and those they are paired with; the first ones are asked for before it is known whether the
+    // token is there.
+    const T *q_row = (const T*)a.q + (size_t)row * a.q_stride, *k_row = (const T*)a.k + (size_t)row * a.k_stride;
+    T* q_to = (T*)a.q_out + (size_t)row * a.q_out_stride + d0;
+    V own[kAppendAhead], other[kAppendAhead];
+    auto ask = [&](int base) {
+#pragma unroll
+        for (int u = 0; u < kAppendAhead; ++u) {
+            const int head = base + u * groups + group;
+            own[u] = other[u] = V{};
+            if (head < last && mine) {
+                const T* from = (head < a.heads ? q_row : k_row) + (unsigned)((head < a.heads ? head : head - a.heads) * a.dim);
+                own[u] = *reinterpret_cast<const V*>(from + d0);
+                if (!INTERLEAVED && half) other[u] = *reinterpret_cast<const V*>(from + d1);
+            }
+        }
+    };
+    ask(first);
+
+    const int error = kv.st->error;
+    const NewTokens n = new_tokens(kv, a, i);
+    if (error) return;
+    const bool there = t < n.fresh;
+    const int at = there ? n.length - n.fresh + t : 0, offset = at & ((1 << kv.log_page) - 1);
+    int page = -1;
+    if (there) page = kv.table[(size_t)n.slot * kv.max_pages + (at >> kv.log_page)];
+    if (there && (int)threadIdx.x < half)
+        turn(a.positions ? a.positions[row] : at, a.frequencies[threadIdx.x], a.magnitude, cosine[threadIdx.x], sine[threadIdx.x]);
+    __syncthreads();
+    if (!there) {                                              // (the whole workgroup)
+        for (int head = first + group; head < min(last, a.heads); head += groups)
+            if (mine) *reinterpret_cast<V*>(q_to + (unsigned)(head * a.dim)) = V{};
+        return;
+    }
+    const bool store = page_ok(kv, page);
+    T* k_to = (T*)kv.k + (((((size_t)a.layer * kv.pages + (store ? page : 0)) * a.kv_heads) << kv.log_page) + offset) * a.dim + d0;
     constexpr int PAIRS = INTERLEAVED ? N / 2 : N;
     float c[PAIRS], s[PAIRS];
-    if (turns) {
-        const double position = a.positions ? a.positions[row] : at;
 #pragma unroll
-        for (int e = 0; e < PAIRS; ++e) {
-            const int pair = INTERLEAVED ? d0 / 2 + e : (upper ? d1 : d0) + e;
-            c[e] = 1.f;
-            s[e] = 0.f;
-            if (pair < half) turn(position, a.frequencies[pair], a.magnitude, c[e], s[e]);
-        }
+    for (int e = 0; e < PAIRS; ++e) {
+        const int pair = INTERLEAVED ? d0 / 2 + e : (upper ? d1 : d0) + e;
+        const bool there_is = turns && pair < half;
+        c[e] = there_is ? cosine[pair] : 1.f;
+        s[e] = there_is ? sine[pair] : 0.f;
     }
-    const int first = blockIdx.y * a.heads_per_block, last = min(first + a.heads_per_block, a.heads + 2 * a.kv_heads);
-    for (int base = first; base < last; base += groups) {
-        const int head = base + group;
-        const bool ok = head < last && mine;
-        const int kind = head < a.heads ? 0 : head < a.heads + a.kv_heads ? 1 : 2;
-        const int h = kind == 0 ? head : kind == 1 ? head - a.heads : head - a.heads - a.kv_heads;
-        if (!there) {                                          // (the whole workgroup)
-            if (ok && kind == 0)
-                *reinterpret_cast<V*>((T*)a.q_out + (size_t)row * a.q_out_stride + (size_t)h * a.dim + d0) = V{};
-            continue;
-        }
-        const T* x = kind == 0 ? (const T*)a.q + (size_t)row * a.q_stride
-                               : kind == 1 ? (const T*)a.k + (size_t)row * a.k_stride : (const T*)a.v + (size_t)row * a.v_stride;
-        x += (size_t)h * a.dim;
-        V own = {}, other = {};
-        if (ok) {
-            own = *reinterpret_cast<const V*>(x + d0);
-            if (!INTERLEAVED && kind != 2) other = *reinterpret_cast<const V*>(x + d1);
-        }
-        if (kind == 2) {                                       // (lanes of one head go one way; the exchanges below stay inside it)
-            if (ok && store) {
-                T* to = (T*)kv.v + ((((size_t)a.layer * kv.pages + page) * a.kv_heads + h) << kv.log_page) * a.dim +
-                        ((size_t)(offset / N) * a.dim + d0) * N + offset % N;
+    float w[N], b[N], w1[N], b1[N];                            // of the lane's dimensions, and of those they are paired with
+    int weights_of = -1;                                       // queries, keys
+    for (int base = first;;) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) to[e * N] = own[e];
-            }
-            continue;
-        }
-        float f[N], g[N];                                      // the lane's dimensions, and those they are paired with
+      for (int u = 0; u < kAppendAhead; ++u) {
+        if (base + u * groups >= last) return;                 // (the whole workgroup)
+        const int head = base + u * groups + group;
+        const bool ok = head < last && mine, key = head >= a.heads;
+        float f[N], g[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            f[e] = (float)own[e];
-            g[e] = (float)other[e];
+            f[e] = (float)own[u][e];
+            g[e] = (float)other[u][e];
         }
-        if (a.norm) {
+        if constexpr (NORM) {
+            if (weights_of != (int)key) {
+                weights_of = key;
+                const float* weight = key ? a.k_weight : a.q_weight;
+                const float* bias = a.norm == 2 ? (key ? a.k_bias : a.q_bias) : nullptr;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    w[e] = w1[e] = 1.f;
+                    b[e] = b1[e] = 0.f;
+                }
+                if (mine && weight) {
+                    load_floats(weight + d0, w);
+                    if (!INTERLEAVED) load_floats(weight + d1, w1);
+                }
+                if (mine && bias) {
+                    load_floats(bias + d0, b);
+                    if (!INTERLEAVED) load_floats(bias + d1, b1);
+                }
+            }
             float mean = 0.f;
             if (a.norm == 2) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) mean += f[e];
+                for (int e = 0; e < N; ++e) mean += mine ? f[e] : 0.f;
                 mean = group_sum(mean, lanes) / a.dim;
             }
             float square = 0.f;
@@ -144,14 +244,10 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
                 square += v * v;
             }
             const float inv = 1.f / sqrtf(group_sum(square, lanes) / a.dim + a.eps);
-            const float* w = kind == 0 ? a.q_weight : a.k_weight;
-            const float* b = a.norm == 2 ? (kind == 0 ? a.q_bias : a.k_bias) : nullptr;
-            if (mine) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    f[e] = (f[e] - mean) * inv * (w ? w[d0 + e] : 1.f) + (b ? b[d0 + e] : 0.f);
-                    if (!INTERLEAVED) g[e] = (g[e] - mean) * inv * (w ? w[d1 + e] : 1.f) + (b ? b[d1 + e] : 0.f);
-                }
+            for (int e = 0; e < N; ++e) {
+                f[e] = (f[e] - mean) * inv * w[e] + b[e];
+                if (!INTERLEAVED) g[e] = (g[e] - mean) * inv * w1[e] + b1[e];
             }
         }
         V out;
@@ -171,17 +267,23 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
             }
         }
         if (!ok) continue;
-        if (kind == 0)
-            *reinterpret_cast<V*>((T*)a.q_out + (size_t)row * a.q_out_stride + (size_t)h * a.dim + d0) = out;
+        if (!key)
+            *reinterpret_cast<V*>(q_to + (unsigned)(head * a.dim)) = out;
         else if (store)
-            *reinterpret_cast<V*>((T*)kv.k + (((((size_t)a.layer * kv.pages + page) * a.kv_heads + h) << kv.log_page) + offset) * a.dim + d0) = out;
+            *reinterpret_cast<V*>(k_to + (unsigned)(((head - a.heads) * a.dim) << kv.log_page)) = out;
+      }
+      base += kAppendAhead * groups;
+      if (base >= last) return;
+      ask(base);
     }
 }
 
 template <typename T>
-void launch_append_as(const KvView& kv, const AppendArgs& a, bool interleaved, int rows, int blocks, hipStream_t s) {
-    if (interleaved) hipLaunchKernelGGL((k_kv_append<T, true>), dim3(rows, blocks), dim3(256), 0, s, kv, a);
-    else hipLaunchKernelGGL((k_kv_append<T, false>), dim3(rows, blocks), dim3(256), 0, s, kv, a);
+void launch_append_as(const KvView& kv, const AppendArgs& a, bool interleaved, hipStream_t s) {
+    const dim3 grid(a.n_tokens * a.head_blocks + a.pieces * a.value_blocks, a.batch);
+    auto kernel = a.norm ? (interleaved ? k_kv_append<T, true, true> : k_kv_append<T, false, true>)
+                         : (interleaved ? k_kv_append<T, true, false> : k_kv_append<T, false, false>);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, kv, a);
 }
 
 }  // namespace lif
