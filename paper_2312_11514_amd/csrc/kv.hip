@@ -134,6 +134,8 @@ int launched() {
     return e == hipSuccess ? LIF_OK : fail(LIF_HIP_ERROR, "launch: %s", hipGetErrorString(e));
 }
 
+int plan_threads(const lif_kv* kv) { return kv->cfg.max_seqs <= kKvPlanFew ? kKvPlanFew : kKvMaxSeqs; }
+
 int batch_ok(const lif_kv* kv, int32_t layer, int32_t batch, int32_t n_tokens) {
     if (layer < 0 || layer >= kv->cfg.layers) return fail(LIF_INVALID_ARG, "layer out of range");
     if (batch < 1 || batch > kKvMaxSeqs) return fail(LIF_INVALID_ARG, "batch must be in 1..1024");
@@ -230,7 +232,9 @@ int lif_kv_adopt(lif_kv* kv, void* stream) {
 
 int lif_kv_reserve(lif_kv* kv, const int32_t* counts_dev, void* stream) {
     if (!kv || !counts_dev) return fail(LIF_INVALID_ARG, "null pointer");
-    hipLaunchKernelGGL(k_kv_reserve, dim3(1), dim3(kKvPlanThreads), 0, (hipStream_t)stream, kv->view, counts_dev);
+    const int threads = plan_threads(kv);
+    hipLaunchKernelGGL(threads == kKvPlanFew ? k_kv_reserve<kKvPlanFew> : k_kv_reserve<kKvMaxSeqs>, dim3(1), dim3(threads), 0, (hipStream_t)stream,
+                       kv->view, counts_dev);
     hipLaunchKernelGGL((k_kv_move<KV_COPY>), dim3(kCopyBlocks), dim3(256), 0, (hipStream_t)stream, kv->view, nullptr, nullptr, 0);
     return launched();
 }
@@ -244,14 +248,18 @@ int lif_kv_truncate(lif_kv* kv, const int32_t* lengths_dev, void* stream) {
 int lif_kv_fork(lif_kv* kv, const int32_t* src_dev, const int32_t* dst_dev, int32_t n, void* stream) {
     if (!kv || !src_dev || !dst_dev) return fail(LIF_INVALID_ARG, "null pointer");
     if (n < 1 || n > kv->cfg.max_seqs) return fail(LIF_INVALID_ARG, "n must be in 1..max_seqs");
-    hipLaunchKernelGGL(k_kv_fork, dim3(1), dim3(kKvPlanThreads), 0, (hipStream_t)stream, kv->view, src_dev, dst_dev, n);
+    const int threads = plan_threads(kv);
+    hipLaunchKernelGGL(threads == kKvPlanFew ? k_kv_fork<kKvPlanFew> : k_kv_fork<kKvMaxSeqs>, dim3(1), dim3(threads), 0, (hipStream_t)stream,
+                       kv->view, src_dev, dst_dev, n);
     hipLaunchKernelGGL((k_kv_move<KV_FORK>), dim3(n + kMoveBlocks), dim3(256), 0, (hipStream_t)stream, kv->view, src_dev, dst_dev, n);
     return launched();
 }
 
 int lif_kv_compact(lif_kv* kv, void* stream) {
     if (!kv) return fail(LIF_INVALID_ARG, "null handle");
-    hipLaunchKernelGGL(k_kv_compact, dim3(1), dim3(kKvPlanThreads), 0, (hipStream_t)stream, kv->view);
+    const int threads = plan_threads(kv);
+    hipLaunchKernelGGL(threads == kKvPlanFew ? k_kv_compact<kKvPlanFew> : k_kv_compact<kKvMaxSeqs>, dim3(1), dim3(threads), 0, (hipStream_t)stream,
+                       kv->view);
     hipLaunchKernelGGL((k_kv_move<KV_COMPACT>), dim3(kv->cfg.max_seqs + kMoveBlocks), dim3(256), 0, (hipStream_t)stream, kv->view, nullptr, nullptr,
                        kv->cfg.max_seqs);
     return launched();
@@ -271,7 +279,7 @@ int lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* rows, void* stre
     AppendArgs a{static_cast<const char*>(rows->q), static_cast<const char*>(rows->k), static_cast<const char*>(rows->v),
                  static_cast<char*>(rows->q_out), rows->q_stride, rows->k_stride, rows->v_stride, rows->q_out_stride,
                  rows->q_weight, rows->q_bias, rows->k_weight, rows->k_bias, kv->frequencies, rows->positions, rows->slots, rows->batch,
-                 rows->n_tokens, c.heads, c.kv_heads, c.head_dim, layer, c.rotary_dim, c.norm, 0, 0, 0, 0, 0, c.norm_eps, c.rotary_scale};
+                 rows->n_tokens, c.heads, c.kv_heads, c.head_dim, layer, c.rotary_dim, c.norm, 0, 0, 0, 0, 0, c.norm_eps, c.rotary_scale, 1.f / c.head_dim};
     const int count = rows->batch * rows->n_tokens, all = c.heads + c.kv_heads, n = 16 / elem_bytes(c.dtype);
     while ((n << a.log_lanes) < c.head_dim) ++a.log_lanes;
     const int at_once = 256 >> a.log_lanes;

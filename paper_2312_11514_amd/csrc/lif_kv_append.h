@@ -37,7 +37,7 @@ struct AppendArgs {
     int32_t log_lanes;                         // lanes that share a head: the pieces of 16 bytes, rounded up to a power of two
     int32_t head_blocks, heads_per_block;      // workgroups of a token for its queries and keys, and heads of each
     int32_t pieces, value_blocks;              // pieces of N positions that a batch row's new tokens may lie in, workgroups of a piece
-    float eps, magnitude;
+    float eps, magnitude, inv_dim;
 };
 
 void launch_append_f16(const KvView& kv, const AppendArgs& a, bool interleaved, hipStream_t s);
@@ -153,8 +153,9 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
     const bool turns = mine && d0 < a.rotary_dim, upper = !INTERLEAVED && d0 >= half;
     const int d1 = !turns || INTERLEAVED ? d0 : upper ? d0 - half : d0 + half;
     const int first = (unit - t * a.head_blocks) * a.heads_per_block, last = min(first + a.heads_per_block, a.heads + a.kv_heads);
-    // The lane's dimensions of its next heads, and those they are paired with; the first ones are asked for before it is known whether the
-    // token is there.
+    // The lane's dimensions of its next heads, and those they are paired with.  Of single tokens the first ones are asked for before it is
+    // known whether the token is there; of several many may not be, and reading all of them costs more than the wait (25.9 us against 22 in
+    // the case above, where half are padding).
     const T *q_row = (const T*)a.q + (size_t)row * a.q_stride, *k_row = (const T*)a.k + (size_t)row * a.k_stride;
     T* q_to = (T*)a.q_out + (size_t)row * a.q_out_stride + d0;
     V own[kAppendAhead], other[kAppendAhead];
@@ -170,7 +171,28 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
             }
         }
     };
-    ask(first);
+    if (a.n_tokens == 1) ask(first);
+    float w[N], b[N], w1[N], b1[N];                            // norm: weights of these dimensions, of queries or of keys
+    bool weights_of = false;
+    auto ask_weights = [&](bool key) {
+        weights_of = key;
+        const float* weight = key ? a.k_weight : a.q_weight;
+        const float* bias = a.norm == 2 ? (key ? a.k_bias : a.q_bias) : nullptr;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            w[e] = w1[e] = 1.f;
+            b[e] = b1[e] = 0.f;
+        }
+        if (mine && weight) {
+            load_floats(weight + d0, w);
+            if (!INTERLEAVED) load_floats(weight + d1, w1);
+        }
+        if (mine && bias) {
+            load_floats(bias + d0, b);
+            if (!INTERLEAVED) load_floats(bias + d1, b1);
+        }
+    };
+    if constexpr (NORM) ask_weights(first + group >= a.heads);
 
     const int error = kv.st->error;
     const NewTokens n = new_tokens(kv, a, i);
@@ -187,6 +209,7 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
             if (mine) *reinterpret_cast<V*>(q_to + (unsigned)(head * a.dim)) = V{};
         return;
     }
+    if (a.n_tokens > 1) ask(first);
     const bool store = page_ok(kv, page);
     T* k_to = (T*)kv.k + (((((size_t)a.layer * kv.pages + (store ? page : 0)) * a.kv_heads) << kv.log_page) + offset) * a.dim + d0;
     constexpr int PAIRS = INTERLEAVED ? N / 2 : N;
@@ -198,8 +221,6 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
         c[e] = there_is ? cosine[pair] : 1.f;
         s[e] = there_is ? sine[pair] : 0.f;
     }
-    float w[N], b[N], w1[N], b1[N];                            // of the lane's dimensions, and of those they are paired with
-    int weights_of = -1;                                       // queries, keys
     for (int base = first;;) {
 #pragma unroll
       for (int u = 0; u < kAppendAhead; ++u) {
@@ -213,29 +234,12 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
             g[e] = (float)other[u][e];
         }
         if constexpr (NORM) {
-            if (weights_of != (int)key) {
-                weights_of = key;
-                const float* weight = key ? a.k_weight : a.q_weight;
-                const float* bias = a.norm == 2 ? (key ? a.k_bias : a.q_bias) : nullptr;
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    w[e] = w1[e] = 1.f;
-                    b[e] = b1[e] = 0.f;
-                }
-                if (mine && weight) {
-                    load_floats(weight + d0, w);
-                    if (!INTERLEAVED) load_floats(weight + d1, w1);
-                }
-                if (mine && bias) {
-                    load_floats(bias + d0, b);
-                    if (!INTERLEAVED) load_floats(bias + d1, b1);
-                }
-            }
+            if (weights_of != key) ask_weights(key);
             float mean = 0.f;
             if (a.norm == 2) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) mean += mine ? f[e] : 0.f;
-                mean = group_sum(mean, lanes) / a.dim;
+                mean = group_sum(mean, lanes) * a.inv_dim;
             }
             float square = 0.f;
 #pragma unroll
@@ -243,7 +247,7 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
                 const float v = mine ? f[e] - mean : 0.f;
                 square += v * v;
             }
-            const float inv = 1.f / sqrtf(group_sum(square, lanes) / a.dim + a.eps);
+            const float inv = __builtin_amdgcn_rsqf(group_sum(square, lanes) * a.inv_dim + a.eps);      // (good to one unit in the last place)
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 f[e] = (f[e] - mean) * inv * w[e] + b[e];

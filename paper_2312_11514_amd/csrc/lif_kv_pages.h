@@ -9,32 +9,38 @@
 
 namespace lif {
 
-constexpr int kKvPlanThreads = 1024;     // of the planning workgroup: one per slot
+// threads of the planning workgroup, one per slot: 256 or 1024 (max_seqs).  A barrier among 16 waves costs more than one among 4.
+constexpr int kKvPlanFew = 256;
 
 // Walks the set bits of the words [w0, w1) in ascending order by the whole workgroup: emit(rank, page) for those of rank < total, and
 // keep(word index, word, taken bits) for every word that had one of them.  select(word index, word) picks the bits that count.  A thread
 // counts the bits of a word; a word with bits that are wanted is then dealt to a wave, one bit to a lane: pages come in runs, and
 // one thread that goes through 64 bits by itself is what the others wait for.
 // Returns the bits seen (all of them if total is not reached).  Every thread of the workgroup has to call it.
+// `ahead`: the word of the thread in the first pass.
+template <int THREADS>
 struct WalkScratch {
-    int wave_tot[kKvPlanThreads / 64];
-    unsigned long long word[kKvPlanThreads];
-    int before[kKvPlanThreads];
+    int wave_tot[THREADS / 64];
+    unsigned long long word[THREADS];
+    int before[THREADS];
 };
-template <typename Select, typename Emit, typename Keep>
-__device__ __forceinline__ int walk_bits(const unsigned long long* bits, int w0, int w1, int total, WalkScratch& ws, Select select, Emit emit,
-                                         Keep keep) {
+__device__ __forceinline__ unsigned long long word_ahead(const unsigned long long* bits, int w0, int w1) {
+    return w0 + (int)threadIdx.x < w1 ? bits[w0 + threadIdx.x] : 0ull;
+}
+template <int THREADS, typename Select, typename Emit, typename Keep>
+__device__ __forceinline__ int walk_bits(const unsigned long long* bits, int w0, int w1, int total, unsigned long long ahead, WalkScratch<THREADS>& ws,
+                                         Select select, Emit emit, Keep keep) {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     int seen = 0;
-    for (int base = w0; base < w1 && seen < total; base += kKvPlanThreads) {
+    for (int base = w0; base < w1 && seen < total; base += THREADS) {
         const int at = base + tid;
-        const unsigned long long w = at < w1 ? select(at, bits[at]) : 0ull;
+        const unsigned long long w = at < w1 ? select(at, base == w0 ? ahead : bits[at]) : 0ull;
         int all;
-        const int before = block_exclusive_scan<kKvPlanThreads / 64>(__popcll(w), ws.wave_tot, &all);
+        const int before = block_exclusive_scan<THREADS / 64>(__popcll(w), ws.wave_tot, &all);
         ws.word[tid] = w;
         ws.before[tid] = seen + before;
         __syncthreads();
-        for (int i = wv; i < kKvPlanThreads; i += kKvPlanThreads / 64) {
+        for (int i = wv; i < min(THREADS, w1 - base); i += THREADS / 64) {
             const unsigned long long word = ws.word[i];
             const int first = ws.before[i];
             if (first >= total) break;
@@ -62,7 +68,7 @@ __device__ __forceinline__ unsigned long long free_word(int w, int pages) {
 template <bool RESET>
 __global__ __launch_bounds__(256) void k_kv_clear(const KvView kv) {
     const long long step = (long long)gridDim.x * 256, at = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (at == 0) *kv.st = KvState{0, 0, 0, 0};
+    if (at == 0) *kv.st = KvState{0, 0, 0, 0, 0};
     for (long long i = at; i < kv.n_arrived; i += step) kv.arrived[i] = 0;
     for (long long i = at; i < kv.pages; i += step) kv.refs[i] = 0;
     for (long long i = at; i < (kv.pages + 63) / 64; i += step) kv.free_bits[i] = free_word((int)i, kv.pages);
@@ -90,6 +96,8 @@ __global__ __launch_bounds__(256) void k_kv_adopt(const KvView kv) {
         } else if (atomicAdd(&kv.refs[page], 1) == 0) {
             atomicAnd(&kv.free_bits[page >> 6], ~(1ull << (page & 63)));
             ++used;
+        } else {
+            kv.st->shares = 1;
         }
     }
     if (used) atomicAdd(&kv.st->used, used);
@@ -98,12 +106,14 @@ __global__ __launch_bounds__(256) void k_kv_adopt(const KvView kv) {
 
 // ---- reserve: one workgroup -------------------------------------------------------------------------------------------------
 
-__global__ __launch_bounds__(kKvPlanThreads) void k_kv_reserve(const KvView kv, const int32_t* __restrict__ counts) {
-    __shared__ WalkScratch ws;
-    __shared__ int first[kKvPlanThreads], had_of[kKvPlanThreads], copy_of[kKvPlanThreads];
-    const int slot = threadIdx.x;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_reserve(const KvView kv, const int32_t* __restrict__ counts) {
+    __shared__ WalkScratch<THREADS> ws;
+    __shared__ int first[THREADS], had_of[THREADS], copy_of[THREADS];
+    const int slot = threadIdx.x, words = (kv.pages + 63) / 64;
     KvState* st = kv.st;
-    const int error = st->error, used = st->used;
+    const int error = st->error, used = st->used, shares = st->shares;
+    const unsigned long long ahead = word_ahead(kv.free_bits, 0, words);
     int length = 0, count = 0;
     if (slot < kv.max_seqs) {
         length = length_of(kv, slot);
@@ -116,14 +126,15 @@ __global__ __launch_bounds__(kKvPlanThreads) void k_kv_reserve(const KvView kv, 
     int32_t* row = kv.table + (size_t)(slot < kv.max_seqs ? slot : 0) * kv.max_pages;
     // tokens that go behind others into a page that is not this sequence's alone: a copy of it
     int shared = -1;
-    if (fits && count > 0 && (length & ((1 << kv.log_page) - 1))) {
+    if (shares && fits && count > 0 && (length & ((1 << kv.log_page) - 1))) {
         const int page = row[had - 1];
         if (page_ok(kv, page) && kv.refs[page] > 1) shared = page;
     }
     const int need = fits ? pages_of(end, kv.log_page) - had + (shared >= 0) : 0;
     int total, copies;
-    const int rank0 = block_exclusive_scan<kKvPlanThreads / 64>(need, ws.wave_tot, &total);
-    const int copy0 = block_exclusive_scan<kKvPlanThreads / 64>(shared >= 0, ws.wave_tot, &copies);
+    const int rank0 = block_exclusive_scan<THREADS / 64>(need, ws.wave_tot, &total);
+    int copy0 = copies = 0;
+    if (shares) copy0 = block_exclusive_scan<THREADS / 64>(shared >= 0, ws.wave_tot, &copies);
     first[slot] = rank0;
     had_of[slot] = had - (shared >= 0);
     copy_of[slot] = shared >= 0 ? copy0 : -1;
@@ -136,9 +147,9 @@ __global__ __launch_bounds__(kKvPlanThreads) void k_kv_reserve(const KvView kv, 
     }
     if (total > 0) {
         walk_bits(
-            kv.free_bits, 0, (kv.pages + 63) / 64, total, ws, [](int, unsigned long long w) { return w; },
+            kv.free_bits, 0, words, total, ahead, ws, [](int, unsigned long long w) { return w; },
             [&](int rank, int page) {
-                const int s = last_not_above(first, kKvPlanThreads, rank), j = rank - first[s];
+                const int s = last_not_above(first, min(THREADS, kv.max_seqs), rank), j = rank - first[s];
                 int32_t* at = kv.table + (size_t)s * kv.max_pages + had_of[s] + j;
                 if (j == 0 && copy_of[s] >= 0) kv.moves[copy_of[s]] = make_int2(*at, page);
                 *at = page;
@@ -146,12 +157,12 @@ __global__ __launch_bounds__(kKvPlanThreads) void k_kv_reserve(const KvView kv, 
             },
             [&](int w, unsigned long long taken) { kv.free_bits[w] &= ~taken; });
     }
-    int freed = 0;
+    int all_freed = 0, freed = 0;
     if (shared >= 0 && atomicSub(&kv.refs[shared], 1) == 1) {        // (everyone who held it has a copy)
         atomicOr(&kv.free_bits[shared >> 6], 1ull << (shared & 63));
         freed = 1;
     }
-    const int all_freed = __syncthreads_count(freed);
+    if (shares) all_freed = __syncthreads_count(freed);
     if (slot < kv.max_seqs) {
         kv.lengths[slot] = (int)end;
         kv.fresh[slot] = count;
@@ -191,13 +202,13 @@ __global__ __launch_bounds__(256) void k_kv_truncate(const KvView kv, const int3
 
 // ---- fork: one workgroup plans, k_kv_move does ------------------------------------------------------------------------------
 
-__global__ __launch_bounds__(kKvPlanThreads) void k_kv_fork(const KvView kv, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
-                                                            int n) {
-    __shared__ WalkScratch ws;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_fork(const KvView kv, const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int n) {
+    __shared__ WalkScratch<THREADS> ws;
     __shared__ unsigned named[kKvMaxSeqs / 32];
-    __shared__ int first[kKvPlanThreads];
-    const int i = threadIdx.x;
+    const int i = threadIdx.x, words = (kv.pages + 63) / 64;
     KvState* st = kv.st;
+    const unsigned long long ahead = word_ahead(kv.free_bits, 0, words);
     const int error = st->error, used = st->used;
     if (i < kKvMaxSeqs / 32) named[i] = 0;
     __syncthreads();
@@ -214,8 +225,7 @@ __global__ __launch_bounds__(kKvPlanThreads) void k_kv_fork(const KvView kv, con
     }
     const bool partial = i < n && !bad && (length & ((1 << kv.log_page) - 1));
     int total;
-    const int rank0 = block_exclusive_scan<kKvPlanThreads / 64>(partial, ws.wave_tot, &total);
-    first[i] = rank0;
+    const int rank0 = block_exclusive_scan<THREADS / 64>(partial, ws.wave_tot, &total);
     const bool any_bad = __syncthreads_or(bad);
     if (error || any_bad || total > kv.pages - used) {
         if (i == 0) {
@@ -230,7 +240,7 @@ __global__ __launch_bounds__(kKvPlanThreads) void k_kv_fork(const KvView kv, con
     // the page of rank r is the copy of the last page of the r-th pair that has a partly filled one
     if (total > 0)
         walk_bits(
-            kv.free_bits, 0, (kv.pages + 63) / 64, total, ws, [](int, unsigned long long w) { return w; },
+            kv.free_bits, 0, words, total, ahead, ws, [](int, unsigned long long w) { return w; },
             [&](int rank, int page) {
                 kv.moves[rank].y = page;
                 kv.refs[page] = 1;
@@ -250,13 +260,15 @@ __global__ __launch_bounds__(kKvPlanThreads) void k_kv_fork(const KvView kv, con
         st->used = used + total;
         st->n_moves = total;
         st->ok = 1;
+        st->shares = 1;
     }
 }
 
 // ---- compact: one workgroup plans -------------------------------------------------------------------------------------------
 
-__global__ __launch_bounds__(kKvPlanThreads) void k_kv_compact(const KvView kv) {
-    __shared__ WalkScratch ws;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_compact(const KvView kv) {
+    __shared__ WalkScratch<THREADS> ws;
     KvState* st = kv.st;
     const int error = st->error, used = st->used, words = (kv.pages + 63) / 64, edge = used >> 6;
     if (error) {
@@ -266,24 +278,24 @@ __global__ __launch_bounds__(kKvPlanThreads) void k_kv_compact(const KvView kv) 
     auto below = [&](int w) { return w < edge ? ~0ull : w > edge ? 0ull : (1ull << (used & 63)) - 1ull; };   // pages < used
     auto nothing = [](int, unsigned long long) {};
     const int holes = walk_bits(
-        kv.free_bits, 0, min(edge + 1, words), 0x7fffffff, ws, [&](int w, unsigned long long v) { return v & below(w); },
+        kv.free_bits, 0, min(edge + 1, words), 0x7fffffff, word_ahead(kv.free_bits, 0, words), ws, [&](int w, unsigned long long v) { return v & below(w); },
         [&](int rank, int page) { kv.moves[rank].y = page; }, nothing);
     if (holes > 0) {
         // as many used pages lie at or above `used` as free ones below; the highest goes to the lowest hole
         const int movers = walk_bits(
-            kv.free_bits, edge, words, holes, ws, [&](int w, unsigned long long v) { return ~v & ~below(w) & free_word(w, kv.pages); },
+            kv.free_bits, edge, words, holes, word_ahead(kv.free_bits, edge, words), ws, [&](int w, unsigned long long v) { return ~v & ~below(w) & free_word(w, kv.pages); },
             [&](int rank, int page) { kv.moves[holes - 1 - rank].x = page; }, nothing);
         if (movers < holes) {                            // (counts that do not belong together: the state was written over)
             if (threadIdx.x == 0) st->error = 2 /* LIF_BAD_STATE */;
             return;
         }
-        for (int j = threadIdx.x; j < holes; j += kKvPlanThreads) {
+        for (int j = threadIdx.x; j < holes; j += THREADS) {
             const int2 m = kv.moves[j];
             kv.refs[m.y] = kv.refs[m.x];
             kv.refs[m.x] = 0;
             kv.remap[m.x] = m.y;
         }
-        for (int w = threadIdx.x; w < words; w += kKvPlanThreads) kv.free_bits[w] = free_word(w, kv.pages) & ~below(w);
+        for (int w = threadIdx.x; w < words; w += THREADS) kv.free_bits[w] = free_word(w, kv.pages) & ~below(w);
     }
     if (threadIdx.x == 0) {
         st->n_moves = holes;
