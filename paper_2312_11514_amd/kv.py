@@ -9,9 +9,14 @@
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 from . import binding as _b
 from .binding import LIF_INVALID_ARG, LifError
+
+# lif_kv_rows and lif_kv_query, filled in one go: setting the fields of a ctypes structure one by one is a third of the cost of a call
+_ROWS, _QUERY = struct.Struct("@4P4q6P2i"), struct.Struct("@3P2q3P3i4x")
+assert _ROWS.size == C.sizeof(_b.LifKvRows) and _QUERY.size == C.sizeof(_b.LifKvQuery)
 
 _DTYPES = {"f32": _b.LIF_F32, "f16": _b.LIF_F16, "bf16": _b.LIF_BF16}
 
@@ -75,6 +80,7 @@ class KVCache:
         c, torch = self.cfg, self.torch
         self._heads, self._kv_heads, self._dim, self._seqs, self._gpu = c.heads, c.kv_heads, c.head_dim, c.max_seqs, self.table.get_device()
         self._int32, self._float32, self._int64 = torch.int32, torch.float32, torch.int64
+        self._append_call, self._attend_call = self.lib.lif_kv_append, self.lib.lif_kv_attend
         self._rows_arg, self._query_arg = _b.LifKvRows(), _b.LifKvQuery()
         self._rows_ref, self._query_ref = C.byref(self._rows_arg), C.byref(self._query_arg)
 
@@ -100,12 +106,12 @@ class KVCache:
             return self._ints(slots, batch, "slots")
         if batch > self._seqs:
             _refuse("more rows than slots")
-        return None
+        return 0
 
-    def _rows(self, t, batch, tokens, heads, what):
+    def _rows(self, t, shape, what):
         """The stride between tokens of [batch, tokens, heads, head_dim], heads contiguous."""
-        d = self._dim
-        if t.dtype is self.tdtype and t.get_device() == self._gpu and t.shape == (batch, tokens, heads, d):
+        if t.dtype is self.tdtype and t.get_device() == self._gpu and t.shape == shape:
+            batch, tokens, heads, d = shape
             if t.is_contiguous():
                 return heads * d
             sb, sn, sh, sd = t.stride()
@@ -116,11 +122,11 @@ class KVCache:
                 sb = sn
             if sd == 1 and (sh == d or heads == 1) and sb == tokens * sn:
                 return sn
-        _refuse(f"{what} must be [{batch}, {tokens}, {heads}, {d}] of the cache's type beside the cache, heads contiguous, tokens at one stride")
+        _refuse(f"{what} must be {list(shape)} of the cache's type beside the cache, heads contiguous, tokens at one stride")
 
     def _norm(self, t, what):
         if t is None:
-            return None
+            return 0
         if t.dtype is not self._float32 or t.numel() != self._dim or t.get_device() != self._gpu or not t.is_contiguous():
             _refuse(f"{what} must be a contiguous float32 tensor of head_dim elements beside the cache")
         return t.data_ptr()
@@ -148,40 +154,43 @@ class KVCache:
     def append(self, layer, q, k, v, q_out, norm=None, positions=None, slots=None):
         """q, q_out [batch, tokens, heads, head_dim], k, v [batch, tokens, kv_heads, head_dim].  norm: (q weight, q bias, k weight, k bias),
         each float32 [head_dim] or None."""
-        batch, tokens = q.shape[:2]
-        a = self._rows_arg
-        a.q_stride = self._rows(q, batch, tokens, self._heads, "q")
-        a.k_stride = self._rows(k, batch, tokens, self._kv_heads, "k")
-        a.v_stride = self._rows(v, batch, tokens, self._kv_heads, "v")
-        a.q_out_stride = self._rows(q_out, batch, tokens, self._heads, "q_out")
-        a.q, a.k, a.v, a.q_out = q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr()
-        if norm is None:
-            a.q_weight = a.q_bias = a.k_weight = a.k_bias = None
-        else:
-            a.q_weight, a.q_bias, a.k_weight, a.k_bias = (self._norm(t, what) for t, what in
-                                                          zip(norm, ("q weight", "q bias", "k weight", "k bias")))
-        a.positions = self._ints(positions, batch * tokens, "positions") if positions is not None else None
-        a.slots = self._slots(slots, batch)
-        a.batch, a.n_tokens = batch, tokens
-        _b._check(self.lib.lif_kv_append(self.handle, layer, self._rows_ref, _b._stream()))
+        if q.dim() != 4:
+            _refuse("q must be [batch, tokens, heads, head_dim]")
+        batch, tokens, _, _ = q.shape
+        of_q, of_k = (batch, tokens, self._heads, self._dim), (batch, tokens, self._kv_heads, self._dim)
+        q_stride, k_stride, v_stride = self._rows(q, of_q, "q"), self._rows(k, of_k, "k"), self._rows(v, of_k, "v")
+        out_stride = self._rows(q_out, of_q, "q_out")
+        qw = qb = kw = kb = 0
+        if norm is not None:
+            qw, qb, kw, kb = (self._norm(t, what) for t, what in zip(norm, ("q weight", "q bias", "k weight", "k bias")))
+        _ROWS.pack_into(self._rows_arg, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), q_stride, k_stride, v_stride, out_stride,
+                        qw, qb, kw, kb, self._ints(positions, batch * tokens, "positions") if positions is not None else 0,
+                        self._slots(slots, batch), batch, tokens)
+        rc = self._append_call(self.handle, layer, self._rows_ref, _b._stream())
+        if rc:
+            _b._check(rc)
 
     def attend(self, layer, q, out, lse=None, window=0, starts=None, tree=None, slots=None):
         """q, out [batch, tokens, heads, head_dim]; lse float32 [batch, tokens, heads]; starts int32 [batch]; tree int64 [batch, tokens], a
         bit per new token that is seen; slots int32 [batch]."""
-        batch, tokens = q.shape[:2]
-        a = self._query_arg
-        a.q_stride, a.out_stride = self._rows(q, batch, tokens, self._heads, "q"), self._rows(out, batch, tokens, self._heads, "out")
+        if q.dim() != 4:
+            _refuse("q must be [batch, tokens, heads, head_dim]")
+        shape = batch, tokens, _, _ = q.shape
+        if shape[2] != self._heads or shape[3] != self._dim:
+            _refuse(f"q must be [batch, tokens, {self._heads}, {self._dim}]")
+        q_stride, out_stride = self._rows(q, shape, "q"), self._rows(out, shape, "out")
         if lse is not None and (lse.dtype is not self._float32 or lse.numel() != batch * tokens * self._heads or
                                 lse.get_device() != self._gpu or not lse.is_contiguous()):
             _refuse("lse must be a contiguous float32 tensor [batch, tokens, heads] beside the cache")
         if tree is not None and (tree.dtype is not self._int64 or tree.numel() != batch * tokens or tree.get_device() != self._gpu or
                                  not tree.is_contiguous()):
             _refuse("tree must be a contiguous int64 tensor [batch, tokens] beside the cache")
-        a.q, a.out, a.lse, a.tree = q.data_ptr(), out.data_ptr(), _b._ptr(lse), _b._ptr(tree)
-        a.slots = self._slots(slots, batch)
-        a.starts = self._ints(starts, batch, "starts") if starts is not None else None
-        a.batch, a.n_tokens, a.window = batch, tokens, window
-        _b._check(self.lib.lif_kv_attend(self.handle, layer, self._query_ref, _b._stream()))
+        _QUERY.pack_into(self._query_arg, 0, q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else 0, q_stride, out_stride,
+                         self._slots(slots, batch), self._ints(starts, batch, "starts") if starts is not None else 0,
+                         tree.data_ptr() if tree is not None else 0, batch, tokens, window)
+        rc = self._attend_call(self.handle, layer, self._query_ref, _b._stream())
+        if rc:
+            _b._check(rc)
 
     def set_expected_tokens(self, tokens: int):
         _b._check(self.lib.lif_kv_set_expected_tokens(self.handle, int(tokens)))
