@@ -49,7 +49,7 @@ struct AttendArgs {
     const int32_t* lengths;
     const int32_t* fresh;
     const int32_t* error;
-    float* parts;                          // [2][2 * workgroups][rows of a block][dim_pad + 4] sums, unscaled; maximum (log2) and sum behind
+    float* parts;                          // [2][2 * workgroups][rows of a block][dim_pad + 4] sums, unscaled; maximum and sum behind
                                            // them; of the parts, and of their runs
     unsigned* arrived;                     // [2][2 * workgroups] parts written; zero between calls
     unsigned part_bytes;                   // of `parts`
@@ -122,8 +122,12 @@ __device__ __forceinline__ float row_sum(float v) {
     return swap_add<32>(w, w);
 }
 
-// factor on sums over the maximum m for the larger maximum `most`: with nothing visible (m = -inf) the sums are zeros, or NaN, which stays
-__device__ __forceinline__ float rescale(float m, float most) { return m == most ? 1.f : __builtin_amdgcn_exp2f(m - most); }
+// factor on sums over the maximum m for the larger maximum `most`: with nothing visible (m = -inf) the sums are zeros, or NaN, which stays.
+// Maxima are kept as the products give them and scaled after the subtraction, which is exact: of large scores the scaled ones would differ by
+// more than their rounding.
+__device__ __forceinline__ float rescale(float m, float most, float scale_log2) {
+    return m == most ? 1.f : __builtin_amdgcn_exp2f((m - most) * scale_log2);
+}
 
 // ---- how the steps are dealt -------------------------------------------------------------------------------------------------
 // A batch row of length n, f of its tokens new, has the positions [low, n) to go through, in steps from low rounded down to a stage on; a
@@ -316,11 +320,11 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
         }
         const float scale_log2 = a.scale_log2;
         f32x4 o[QT][DT];
-        float top[QT], off[QT], sum[QT];       // running maximum, what is taken from the exponents, sum of the lane's weights
+        float top[QT], ref[QT], sum[QT];       // running maximum, the same or 0 where there is none, sum of the lane's weights
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             top[t] = -INFINITY;
-            off[t] = sum[t] = 0.f;
+            ref[t] = sum[t] = 0.f;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -437,8 +441,8 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                     for (int e = 1; e < N; ++e) most = fmaxf(most, x[t][e]);
                     if (__any(most > top[t])) {
                         most = fmaxf(row_max(most), top[t]);
-                        const float scale = most == top[t] ? 1.f : __builtin_amdgcn_exp2f((top[t] - most) * scale_log2);
-                        off[t] = most == -INFINITY ? 0.f : most * scale_log2 - kWeightBias;
+                        const float scale = rescale(top[t], most, scale_log2);
+                        ref[t] = most == -INFINITY ? 0.f : most;
                         top[t] = most;
                         sum[t] *= scale;
 #pragma unroll
@@ -446,7 +450,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                     }
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e], scale_log2, -off[t]));
+                        const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e] - ref[t], scale_log2, kWeightBias));
                         sum[t] += weight;
                         w[t][e] = (T)weight;
                     }
@@ -511,7 +515,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                 for (int j = 0; j < 4; ++j) y[j] = none ? (T)0.f : (T)(v[j] * inv);
                 *reinterpret_cast<T4*>((T*)a.out + out_row * a.out_stride + (unsigned)(to.y * dim + d)) = y;
             }
-            if (a.lse && d == 0) a.lse[out_row * a.heads + to.y] = none ? -INFINITY : (m - kWeightBias + log2f(total)) / kLog2e;
+            if (a.lse && d == 0) a.lse[out_row * a.heads + to.y] = none ? -INFINITY : (m * a.scale_log2 - kWeightBias + log2f(total)) / kLog2e;
         };
         char* parts = reinterpret_cast<char*>(a.parts);
         auto part_at = [&](int slot, int r0) { return (unsigned)(((unsigned)slot * a.block_rows + r0) * ROW * 4u); };
@@ -520,7 +524,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
         for (int t = 0; t < QT; ++t) {
             const float total = row_sum(sum[t]);
             if (g == 0) {
-                wave_max[wv][16 * t + n] = top[t] == -INFINITY ? -INFINITY : top[t] * scale_log2;
+                wave_max[wv][16 * t + n] = top[t];
                 wave_sum_[wv][16 * t + n] = total;
                 if (wv == 0) out_at[16 * t + n] = my_out[t];
             }
@@ -551,7 +555,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int e = 0; e < kAttendWaves; ++e) {
-                        const float f = rescale(wm[e], m);
+                        const float f = rescale(wm[e], m, scale_log2);
                         l += wl[e] * f;
                         y += wy[e] * f;
                     }
@@ -618,7 +622,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                     for (int e = 0; e < kAttendAsk; ++e)
                         if (u0 + e < units) {
                             if (share * per + e_now < n_parts) {
-                                const float most = fmaxf(m, s[e][0]), old = rescale(m, most), f = rescale(s[e][0], most);
+                                const float most = fmaxf(m, s[e][0]), old = rescale(m, most, scale_log2), f = rescale(s[e][0], most, scale_log2);
                                 m = most;
                                 l = l * old + s[e][1] * f;
                                 y = y * old + v[e] * f;
@@ -651,13 +655,13 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                         float most = m;
 #pragma unroll 4
                         for (int k = 1; k < shares; ++k) most = fmaxf(most, mine[(k << log_once) * ROW + HDP]);
-                        const float f0 = rescale(m, most);
+                        const float f0 = rescale(m, most, scale_log2);
                         l *= f0;
                         y *= f0;
 #pragma unroll 4
                         for (int k = 1; k < shares; ++k) {
                             const float* theirs = mine + (k << log_once) * ROW;
-                            const float f = rescale(theirs[HDP], most);
+                            const float f = rescale(theirs[HDP], most, scale_log2);
                             l += theirs[HDP + 1] * f;
                             y += *reinterpret_cast<const f32x4*>(theirs + d) * f;
                         }

@@ -292,3 +292,30 @@ def test_more_new_tokens_than_the_call_has_rows_for():
     kv.attend(1, q, all_six)
     kv.attend(1, q[:, :4], four)
     assert torch.allclose(all_six[:, :4], four, atol=1e-5, rtol=0)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("size", [30.0, 3e3, 6e4])
+def test_scores_of_any_size(dtype, size):
+    """Queries and keys as large as the type holds: scores up to 10^10, whose differences decide.  Per sequence one key wins by far, and the result is
+    its value; lengths that go through several waves, workgroups and rescalings."""
+    lengths, d, heads = [40, 700, 3000], 64, 4
+    kv, rows = build(lengths, [1] * 3, kv_heads=2, head_dim=d, page=16, dtype=dtype, seed=8, heads=heads)
+    from tests.kv_harness import put
+    rng = np.random.default_rng(9)
+    q = torch.from_numpy(np.sign(rng.standard_normal((3, 1, heads, d))) * size).to(DTYPES[dtype]).cuda()
+    want = np.zeros((3, 1, heads, d))
+    for i, n in enumerate(lengths):
+        keys = rng.uniform(-0.5, 0.5, (2, n, d)) * size
+        for g in range(2):                                 # the two query heads of a key head have the same direction
+            q[i, 0, 2 * g + 1] = q[i, 0, 2 * g]
+            at = int(rng.integers(n))
+            keys[g, at] = np.sign(q[i, 0, 2 * g].float().cpu().numpy()) * size
+            want[i, 0, 2 * g:2 * g + 2] = rows[i][1][g, at]
+        put(kv, 1, kv.table[i, :-(-n // 16)].tolist(), torch.from_numpy(keys).to(DTYPES[dtype]), torch.from_numpy(rows[i][1]).to(DTYPES[dtype]))
+    out, lse = torch.empty_like(q), torch.empty(3, 1, heads, device="cuda")
+    kv.attend(1, q, out, lse=lse)
+    # the winner's score is 64 size^2 / 8, the others' are at most half of it in size: 3600 behind for the smallest size, weights of e^-3600
+    assert np.abs(out.double().cpu().numpy() - want).max() <= UNIT[dtype] * np.abs(want).max()
+    score = float(torch.tensor(size).to(DTYPES[dtype])) ** 2 * d * float(np.float32(d ** -0.5))
+    assert np.abs(lse.double().cpu().numpy() - score).max() <= score * (d + 4) * 2.0 ** -24 + 1e-5

@@ -162,3 +162,34 @@ def test_oracle_pages():
     o.truncate([0, 0, -1])
     o.compact()
     assert o.tables == [[], [], [0, 1]] and o.content[1] == ("initial", 1) and o.used() == 2
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.125])
+def test_scales_that_are_not_positive(b, scale):
+    cfg = _config(b, scale=scale)
+    assert b.load_library().lif_kv_workspace_bytes(C.byref(cfg)) == 0
+
+
+def test_the_hint(b):
+    lib, cfg = b.load_library(), _config(b)
+    rc, h = _create(b, cfg, _buffers(b, cfg))
+    assert rc == b.LIF_OK
+    assert lib.lif_kv_set_expected_tokens(None, 5) == lib.lif_kv_set_expected_tokens(h, -1) == b.LIF_INVALID_ARG
+    assert lib.lif_kv_set_expected_tokens(h, 0) == lib.lif_kv_set_expected_tokens(h, 1 << 30) == b.LIF_OK
+    lib.lif_kv_destroy(h)
+
+
+def test_a_page_of_two_gib(b):
+    assert b.load_library().lif_kv_workspace_bytes(C.byref(_config(b, heads=65536, kv_heads=65536, head_dim=256, page_tokens=256, dtype=0))) == 0
+
+
+def test_too_many_steps(b):
+    """1024 sequences of 2^24 positions, 64 key heads: more steps than 32 bits count"""
+    lib = b.load_library()
+    cfg = _config(b, heads=64, kv_heads=64, max_seqs=1024, max_pages=1 << 20)
+    rc, h = _create(b, cfg, _buffers(b, cfg))
+    assert rc == b.LIF_OK
+    p = 1 << 32
+    query = b.LifKvQuery(q=p, out=p, q_stride=4096, out_stride=4096, batch=1024, n_tokens=1)
+    assert lib.lif_kv_attend(h, 0, C.byref(query), None) == b.LIF_INVALID_ARG and b"together" in lib.lif_last_error_string()
+    lib.lif_kv_destroy(h)
