@@ -85,17 +85,25 @@ int units_of(int blocks, int resident) {
     if (blocks <= 128) return (128 + blocks - 1) / blocks * 8;
     return 1;
 }
+int resident_of(const lif_kv_config& c, int tiles) {
+    const int pad = attend_dim_pad(c.head_dim);
+    return kAttendUnits * attend_resident(pad, pad == c.head_dim, tiles, elem_bytes(c.dtype));
+}
 Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) {
-    const int step = 4 * 16 / elem_bytes(c.dtype) * kAttendWaves, need = (rows + 15) / 16;
+    const int bytes = elem_bytes(c.dtype), pad = attend_dim_pad(c.head_dim), need = (rows + 15) / 16;
+    auto steps_of = [&](int waves) {
+        const int step = 4 * 16 / bytes * waves;
+        return (long long)batch * c.kv_heads * ((positions + step - 1) / step + 1);
+    };
     Tiling g;
-    g.steps = (long long)batch * c.kv_heads * ((positions + step - 1) / step + 1);
     g.tiles = std::min(attend_most_tiles(c.head_dim), need <= 1 ? 1 : need <= 2 ? 2 : 4);
-    while (g.tiles > 1 && g.steps * ((need + g.tiles / 2 - 1) / (g.tiles / 2)) <= kAttendFew) g.tiles /= 2;
+    while (g.tiles > 1 && steps_of(4) * ((need + g.tiles / 2 - 1) / (g.tiles / 2)) <= kAttendFew) g.tiles /= 2;
     // of several blocks the last one may be mostly empty: 71 rows, 8 x 16000 positions, heads of 64: 33.5 us in two blocks of 64
     while (g.tiles > 1 && need > g.tiles && 4 * ((need + g.tiles - 1) / g.tiles * g.tiles) > 5 * need) g.tiles /= 2;
+    g.steps = steps_of(attend_waves(pad, pad == c.head_dim, g.tiles, bytes));
     g.blocks = (need + g.tiles - 1) / g.tiles;
     g.block_rows = std::min(rows, 16 * g.tiles);
-    g.units = units_of(g.blocks, kAttendUnits * attend_resident(attend_dim_pad(c.head_dim), g.tiles));
+    g.units = units_of(g.blocks, resident_of(c, g.tiles));
     return g;
 }
 // floats of the parts of any call
@@ -105,7 +113,7 @@ size_t most_part_floats(const lif_kv_config& c) {
     for (int tiles = 1; tiles <= attend_most_tiles(c.head_dim); tiles *= 2) {
         // fewer rows than the largest call's make fewer blocks, and more workgroups for each: the products below are at their largest in between
         for (int blocks = 1; blocks <= std::min(129, (need + tiles - 1) / tiles); ++blocks) {
-            const size_t groups = (size_t)blocks * units_of(blocks, kAttendUnits * attend_resident(pad, tiles));
+            const size_t groups = (size_t)blocks * units_of(blocks, resident_of(c, tiles));
             if (blocks <= 128) most = std::max(most, 4 * groups * std::min(rows, 16 * tiles) * (pad + 4));
         }
     }

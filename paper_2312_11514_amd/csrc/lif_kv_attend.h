@@ -27,7 +27,6 @@ namespace lif {
 
 constexpr int kAttendUnits = 256;        // compute units
 constexpr int kAttendMost = 2048;        // workgroups of a call that may leave parts
-constexpr int kAttendWaves = 4;
 constexpr int kAttendFan = 16;           // parts that one workgroup adds at most; of more, such sums are added again
 constexpr int kAttendAsk = 8;            // ... and asks for at once
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -105,8 +104,18 @@ __device__ __forceinline__ f32x2 load_through2(const float* base, unsigned off, 
                                          __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, (int)bytes, kFlags), (int)off, 0, kPast));
 }
 
-// workgroups of four waves that fit a compute unit
-__host__ __device__ constexpr int attend_resident(int dim_pad, int tiles) { return dim_pad * tiles <= 128 ? 2 : 1; }
+// whether a wave has 256 registers for its tiles, so that a compute unit has room for eight
+__host__ __device__ constexpr bool attend_lean(int dim_pad, bool exact, int tiles, int bytes) {
+    return exact ? dim_pad <= 128 && dim_pad * tiles * bytes <= 512 : dim_pad * tiles <= 128;
+}
+// waves of a workgroup
+__host__ __device__ constexpr int attend_waves(int dim_pad, bool exact, int tiles, int bytes) {
+    return attend_lean(dim_pad, exact, tiles, bytes) && tiles > 1 ? 8 : 4;
+}
+// workgroups that fit a compute unit
+__host__ __device__ constexpr int attend_resident(int dim_pad, bool exact, int tiles, int bytes) {
+    return attend_lean(dim_pad, exact, tiles, bytes) ? 8 / attend_waves(dim_pad, exact, tiles, bytes) : 1;
+}
 
 // max and sum over the four lanes of a row (16 and 32 apart); every one of them gets the result
 __device__ __forceinline__ float row_max(float v) {
@@ -206,9 +215,10 @@ __device__ __forceinline__ RowChunk row_chunk(const AttendArgs& a, int stage, in
 // ---- the pass over keys and values -------------------------------------------------------------------------------------------
 // grid = groups, block = 256.  HDP: head_dim rounded up (FULL: head_dim itself).  QT: tiles of 16 rows of a wave.
 template <typename T, int HDP, bool FULL, int QT>
-__global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(const AttendArgs a) {
+__global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend_lean(HDP, FULL, QT, sizeof(T)) ? 2 : 1) void k_kv_attend(const AttendArgs a) {
     using V = typename Vec<T>::type;
     using M = Mat<T>;
+    constexpr int WAVES = attend_waves(HDP, FULL, QT, sizeof(T)), THREADS = 64 * WAVES;
     constexpr int N = Vec<T>::N;               // elements of 16 bytes; positions of a lane in the second products
     constexpr int TILES = N / 4;               // K tiles of a stage
     constexpr int STAGE = 4 * N;
@@ -218,11 +228,18 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
     constexpr int COLS = HDP / HALF, PITCH = COLS + 4;
     constexpr int ROW = HDP + 4;               // floats of a row of a part
     __shared__ int last;
-    __shared__ float wave_max[kAttendWaves][16 * QT], wave_sum_[kAttendWaves][16 * QT];
-    __shared__ int2 out_at[16 * QT];          // of a row of the block: row of `out` (negative: padding), head
-    __shared__ float sums[kAttendWaves][16][PITCH];
+    __shared__ float wave_max[WAVES][16 * QT], wave_sum_[WAVES][16 * QT];
+    __shared__ float sums[WAVES][16][PITCH];
+    // What a wave needs of its rows only now and then is not kept in registers: their place in `out` (a row, negative for padding, and the
+    // head), of the first segment and of later ones; first position, last new token, and which of those they see.  Queries of several
+    // tiles neither: 128 dimensions by 32 rows fit 256 registers then, and two workgroups a compute unit.
+    constexpr bool QLDS = QT > 1 && attend_lean(HDP, FULL, QT, sizeof(T));
+    __shared__ int2 out_at[2][16 * QT], sees_at[WAVES][16 * QT];
+    __shared__ unsigned long long seen_at[WAVES][16 * QT];
+    __shared__ V q_at[QLDS ? WAVES : 1][QLDS ? QT : 1][QLDS ? CH : 1][64];
+    __shared__ int4 join_of[WAVES][2];         // parts to add behind the loop: w0, count, begins_before
     const int tid = threadIdx.x, lane = tid & 63, wv = whole_wave(tid >> 6), n = lane & 15, g = lane >> 4, dim = FULL ? HDP : a.dim;
-    constexpr int STEP = STAGE * kAttendWaves;
+    constexpr int STEP = STAGE * WAVES;
     const int error = *a.error;
     RowChunk rc = row_chunk(a, STAGE, STEP, 0, 0);
     if (whole_wave(error)) return;
@@ -263,6 +280,38 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
     const int end = by_items ? 1 : (int)min((unsigned)run_steps * ((unsigned)unit + 1u), (unsigned)all);
     int at = by_items ? 0 : (int)min((unsigned)run_steps * (unsigned)unit, (unsigned)all);
     bool first_segment = true;
+    bool arrived = false;                      // the first segment's part was the last of its run to be left
+    int joins = 0;                             // bits of the segments that are parts
+    const float scale_log2 = a.scale_log2;
+    const int rows_here = min(16 * QT, rows - row0);
+    // four dimensions of a row of the output
+    auto finish = [&](int seg, int r0, int d, f32x4 v, float m, float total) {
+        const int2 to = out_at[seg][r0];
+        const size_t out_row = (unsigned)to.x & 0x7fffffffu;
+        const bool none = to.x < 0 || total == 0.f;
+        const float inv = 1.f / total;
+        if (FULL || d < dim) {
+            typedef T T4 __attribute__((ext_vector_type(4)));
+            T4 y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = none ? (T)0.f : (T)(v[j] * inv);
+            *reinterpret_cast<T4*>((T*)a.out + out_row * a.out_stride + (unsigned)(to.y * dim + d)) = y;
+        }
+        if (a.lse && d == 0) a.lse[out_row * a.heads + to.y] = none ? -INFINITY : (m * scale_log2 - kWeightBias + log2f(total)) / kLog2e;
+    };
+    char* parts = reinterpret_cast<char*>(a.parts);
+    const int level2 = 2 * (int)gridDim.x;     // places of parts; those of runs are behind them
+    // place of the k-th part of an item whose first workgroup is w0
+    auto part_of = [&](int w0, bool begins_before, int k) { return slots0 + 2 * (w0 + k) + (k == 0 && begins_before ? 1 : 0); };
+    // whether this workgroup is the last of `n` to have left its part; `place`: of the first of them
+    auto arrive = [&](int level, int place, int n) -> bool {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                     // this wave's stores are acknowledged,
+        __syncthreads();                                                     // and those of the others
+        if (tid == 0) last = n == 1 || (int)atomicInc(a.arrived + level * level2 + place, (unsigned)n - 1u) == n - 1;
+        __syncthreads();
+        return whole_wave(last);
+    };
+    auto part_at = [&](int slot, int r0) { return (unsigned)(((unsigned)slot * a.block_rows + r0) * ROW * 4u); };
 
     while (at < end) {
         int il, s0, s1, steps, kvh, w0, count;             // lane of the batch row, steps, key head, workgroups that share the item
@@ -294,31 +343,37 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
         const RowRange r = of_lane(rc.range, il);
         const int base = r.n - r.fresh, low_all = low_of(r, 0, a.window);
 
-        // the lane's rows: first position it sees, last new token and which of those it sees, query
-        int low[QT], newest[QT];
-        int2 my_out[QT];
-        unsigned long long seen[QT];
-        V q[QT][CH];
+        const int seg = first_segment ? 0 : 1;
+        if (!first_segment) lds_barrier();     // (the last segment's readers are done)
+        V q[QLDS ? 1 : QT][CH];
+        int2 my_sees;
+        unsigned long long my_seen;
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const int row = row0 + 16 * t + n;
             const int tok = (int)((unsigned)row / (unsigned)a.share), head = kvh * a.share + row - tok * a.share;
             const bool ok = row < rows && tok < r.fresh;
-            my_out[t] = make_int2((i * a.n_tokens + tok) | (ok ? 0 : 1 << 31), head);
-            low[t] = ok ? low_of(r, tok, a.window) : 0x7fffffff;
-            newest[t] = a.tree ? 63 : tok;
-            seen[t] = ~0ull;
-            if (ok && a.tree) seen[t] = a.tree[(size_t)i * a.n_tokens + tok];
+            if (g == 0) {
+                if (wv == 0) out_at[seg][16 * t + n] = make_int2((i * a.n_tokens + tok) | (ok ? 0 : 1 << 31), head);
+                if (QT > 1) sees_at[wv][16 * t + n] = make_int2(ok ? low_of(r, tok, a.window) : 0x7fffffff, a.tree ? 63 : tok);
+                if (QT > 1) seen_at[wv][16 * t + n] = ok && a.tree ? a.tree[(size_t)i * a.n_tokens + tok] : ~0ull;
+            }
+            if (QT == 1) {
+                my_sees = make_int2(ok ? low_of(r, tok, a.window) : 0x7fffffff, a.tree ? 63 : tok);
+                my_seen = ~0ull;
+                if (ok && a.tree) my_seen = a.tree[(size_t)i * a.n_tokens + tok];
+            }
             const T* from = (const T*)a.q + ((size_t)i * a.n_tokens + (ok ? tok : 0)) * a.q_stride + (unsigned)((ok ? head : 0) * dim);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {             // (a row that is not there computes with one that is, and is not looked at)
                 const bool sure_in = FULL && (4 * c + 4) * N <= HDP;
                 const int d = (4 * c + g) * N;
-                q[t][c] = *reinterpret_cast<const V*>(from + (sure_in || d < dim ? d : 0));
-                if (!sure_in && d >= dim) q[t][c] = V{};
+                V held = *reinterpret_cast<const V*>(from + (sure_in || d < dim ? d : 0));
+                if (!sure_in && d >= dim) held = V{};
+                if constexpr (QLDS) q_at[wv][t][c][lane] = held;
+                else q[t][c] = held;
             }
         }
-        const float scale_log2 = a.scale_log2;
         f32x4 o[QT][DT];
         float top[QT], ref[QT], sum[QT];       // running maximum, the same or 0 where there is none, sum of the lane's weights
 #pragma unroll
@@ -339,9 +394,9 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
         const char* v_pool = a.v + kvh * (size_t)a.head_bytes;
         const int page_mask = (1 << a.log_page) - 1;
         // whether the lane's row of tile t sees a position
-        auto sees = [&](int t, int pos) -> bool {
+        auto sees = [&](int2 at, unsigned long long seen, int pos) -> bool {
             const int own = pos - base;
-            return (int)(pos >= low[t]) & (int)(pos < r.n) & ((int)(own < 0) | ((int)(own <= newest[t]) & (int)(seen[t] >> (own & 63) & 1ull)));
+            return (int)(pos >= at.x) & (int)(pos < r.n) & ((int)(own < 0) | ((int)(own <= at.y) & (int)(seen >> (own & 63) & 1ull)));
         };
         auto page_at = [&](int pos) { return row_table[min(pos, p_last) >> a.log_page]; };
         auto in_pool = [&](int page) { return (size_t)((unsigned)page < (unsigned)a.pages ? page : 0) * a.page_bytes; };
@@ -382,6 +437,8 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
             bool more;
             do {
                 more = p + STEP < p_end;
+                int here = lane;
+                if constexpr (QLDS) asm volatile("" : "+v"(here));       // (read anew every time, and not kept in registers after all)
                 float x[QT][N];
                 {
                     // (two sums where one chain of products would be long)
@@ -394,13 +451,20 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
 #pragma unroll
                             for (int h = 0; h < CHAINS; ++h) s[t][e][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int c = 0; c < CH; ++c)
+                    for (int c = 0; c < CH; ++c) {
+                        V qc[QT];
+#pragma unroll
+                        for (int t = 0; t < QT; ++t) {
+                            if constexpr (QLDS) qc[t] = q_at[wv][t][c][here];
+                            else qc[t] = q[t][c];
+                        }
 #pragma unroll
                         for (int u = 0; u < M::kParts; ++u)
 #pragma unroll
                             for (int e = 0; e < TILES; ++e)
 #pragma unroll
-                                for (int t = 0; t < QT; ++t) s[t][e][u % CHAINS] = M::mul(k[e][c], q[t][c], s[t][e][u % CHAINS], u);
+                                for (int t = 0; t < QT; ++t) s[t][e][u % CHAINS] = M::mul(k[e][c], qc[t], s[t][e][u % CHAINS], u);
+                    }
 #pragma unroll
                     for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -418,9 +482,12 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                 const bool edge = p < sure || p + STAGE > sure_end;
                 if (edge) {
 #pragma unroll
-                    for (int t = 0; t < QT; ++t)
+                    for (int t = 0; t < QT; ++t) {
+                        const int2 at = QT == 1 ? my_sees : sees_at[wv][16 * t + n];
+                        const unsigned long long seen = QT == 1 ? my_seen : seen_at[wv][16 * t + n];
 #pragma unroll
-                        for (int e = 0; e < N; ++e) x[t][e] = sees(t, vp + e) ? x[t][e] : -INFINITY;
+                        for (int e = 0; e < N; ++e) x[t][e] = sees(at, seen, vp + e) ? x[t][e] : -INFINITY;
+                    }
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {          // what no row may see is not there, whatever it holds
                         auto in = [&](int e) { return vp + e >= low_all && vp + e < r.n; };
@@ -473,7 +540,7 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                             const T* from = (const T*)(v_pool + in_pool(page_at(pos))) + (unsigned)((pos & page_mask) / N * dim * N) + pos % N;
                             bool seen_here[QT];
 #pragma unroll
-                            for (int t = 0; t < QT; ++t) seen_here[t] = sees(t, pos);
+                            for (int t = 0; t < QT; ++t) seen_here[t] = QT == 1 ? sees(my_sees, my_seen, pos) : sees(sees_at[wv][16 * t + n], seen_at[wv][16 * t + n], pos);
 #pragma unroll
                             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -500,33 +567,13 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
 
         // the waves' sums meet
         const bool whole = s0 == 0 && s1 == steps;
-        const int part = slots0 + 2 * unit + (first_segment ? 0 : 1);
-        const int rows_here = min(16 * QT, rows - row0);
-        // four dimensions of a row of the output
-        auto finish = [&](int r0, int d, f32x4 v, float m, float total) {
-            const int2 to = out_at[r0];
-            const size_t out_row = (unsigned)to.x & 0x7fffffffu;
-            const bool none = to.x < 0 || total == 0.f;
-            const float inv = 1.f / total;
-            if (FULL || d < dim) {
-                typedef T T4 __attribute__((ext_vector_type(4)));
-                T4 y;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = none ? (T)0.f : (T)(v[j] * inv);
-                *reinterpret_cast<T4*>((T*)a.out + out_row * a.out_stride + (unsigned)(to.y * dim + d)) = y;
-            }
-            if (a.lse && d == 0) a.lse[out_row * a.heads + to.y] = none ? -INFINITY : (m * a.scale_log2 - kWeightBias + log2f(total)) / kLog2e;
-        };
-        char* parts = reinterpret_cast<char*>(a.parts);
-        auto part_at = [&](int slot, int r0) { return (unsigned)(((unsigned)slot * a.block_rows + r0) * ROW * 4u); };
-        if (!first_segment) __syncthreads();   // (the last segment's readers are done)
+        const int part = slots0 + 2 * unit + seg;
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const float total = row_sum(sum[t]);
             if (g == 0) {
                 wave_max[wv][16 * t + n] = top[t];
                 wave_sum_[wv][16 * t + n] = total;
-                if (wv == 0) out_at[16 * t + n] = my_out[t];
             }
         }
 #pragma unroll
@@ -538,29 +585,29 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
                 for (int d = 0; d < DT / HALF; ++d)
                     *reinterpret_cast<f32x4*>(&sums[wv][n][16 * d + 4 * g]) = o[t][half * (DT / HALF) + d];
                 __syncthreads();
-                for (int u = tid; u < 16 * (COLS / 4); u += 256) {
+                for (int u = tid; u < 16 * (COLS / 4); u += THREADS) {
                     const int rr = u / (COLS / 4), d = u % (COLS / 4) * 4, r0 = 16 * t + rr;
                     if (r0 >= rows_here) break;
-                    float wm[kAttendWaves], wl[kAttendWaves];
-                    f32x4 wy[kAttendWaves];
+                    float wm[WAVES], wl[WAVES];
+                    f32x4 wy[WAVES];
 #pragma unroll
-                    for (int w = 0; w < kAttendWaves; ++w) {
+                    for (int w = 0; w < WAVES; ++w) {
                         wm[w] = wave_max[w][r0];
                         wl[w] = wave_sum_[w][r0];
                         wy[w] = *reinterpret_cast<const f32x4*>(&sums[w][rr][d]);
                     }
                     float m = wm[0], l = 0.f;
 #pragma unroll
-                    for (int e = 1; e < kAttendWaves; ++e) m = fmaxf(m, wm[e]);
+                    for (int e = 1; e < WAVES; ++e) m = fmaxf(m, wm[e]);
                     f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int e = 0; e < kAttendWaves; ++e) {
+                    for (int e = 0; e < WAVES; ++e) {
                         const float f = rescale(wm[e], m, scale_log2);
                         l += wl[e] * f;
                         y += wy[e] * f;
                     }
                     if (whole) {
-                        finish(r0, half * COLS + d, y, m, l);
+                        finish(seg, r0, half * COLS + d, y, m, l);
                     } else {
                         store_through(parts, part_at(part, r0) + (half * COLS + d) * 4, a.part_bytes, y);
                         if (half == 0 && d == 0) store_through(parts, part_at(part, r0) + HDP * 4, a.part_bytes, f32x4{m, l, 0.f, 0.f});
@@ -569,124 +616,134 @@ __global__ __launch_bounds__(256, attend_resident(HDP, QT)) void k_kv_attend(con
             }
         }
 
-        // Parts: each of the `count` workgroups from w0 on has left one (the first of them its last segment, if it began before the item).  Runs of kAttendFan of them are added by the last one of the run, into the place of the run's first part, and the runs by the
-        // last run.
         if (!whole) {
-            const int run = (unit - w0) / kAttendFan, runs = (count + kAttendFan - 1) / kAttendFan, level2 = 2 * (int)gridDim.x;
-            auto part_of = [&](int k) { return slots0 + 2 * (w0 + k) + (k == 0 && begins_before ? 1 : 0); };
-            int level = 0, from = run * kAttendFan, stride = 1, n_parts = min(kAttendFan, count - from);
-            while (true) {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // this wave's stores are acknowledged,
-                __syncthreads();                                             // and those of the others
-                if (tid == 0)
-                    last = n_parts == 1 || (int)atomicInc(a.arrived + level * level2 + part_of(from), (unsigned)n_parts - 1u) == n_parts - 1;
-                __syncthreads();
-                if (!whole_wave(last)) break;
-                const bool done = level == 1 || runs == 1;
-                // Rows x four dimensions to the threads, and what is left of them shares the parts of a row.  A thread asks for kAttendAsk parts
-                // at once, those of its next rows among them.
-                constexpr int QUADS = HDP / 4, TEAMS = 256 / QUADS >= 32 ? 32 : 256 / QUADS >= 16 ? 16 : 256 / QUADS >= 8 ? 8 : 4;
-                int log_once = 0;
-                while ((1 << log_once) < TEAMS && (1 << log_once) < rows_here) ++log_once;
-                const int shares = TEAMS >> log_once, per = (n_parts + shares - 1) >> (__builtin_ctz(TEAMS) - log_once);
-                const int team = tid / QUADS, d = tid % QUADS * 4, share = team >> log_once, row_in = team & ((1 << log_once) - 1);
-                const int units = ((rows_here + (1 << log_once) - 1) >> log_once) * per;
-                auto leave = [&](int r0, f32x4 y, float m, float l) {
-                    if (done) {
-                        finish(r0, d, y, m, l);
-                    } else {
-                        const unsigned b = part_at(level2 + part_of(from), r0);
-                        store_through(parts, b + d * 4, a.part_bytes, y);
-                        if (d == 0) store_through(parts, b + HDP * 4, a.part_bytes, f32x4{m, l, 0.f, 0.f});
-                    }
-                };
-                float m = -INFINITY, l = 0.f;
-                f32x4 y = {0.f, 0.f, 0.f, 0.f};
-                int r_ask = row_in, e_ask = 0, r0 = row_in, e_now = 0;           // row and part of the next one to ask for, and to add
-                for (int u0 = 0; u0 < units; u0 += kAttendAsk) {
-                    f32x2 s[kAttendAsk];
-                    f32x4 v[kAttendAsk];
-#pragma unroll
-                    for (int e = 0; e < kAttendAsk; ++e)
-                        if (u0 + e < units) {
-                            const unsigned b = part_at(level * level2 + part_of(from + min(share * per + e_ask, n_parts - 1) * stride),
-                                                       min(r_ask, rows_here - 1));
-                            s[e] = load_through2(a.parts, b + HDP * 4, a.part_bytes);
-                            v[e] = load_through(a.parts, b + d * 4, a.part_bytes);
-                            if (++e_ask == per) {
-                                e_ask = 0;
-                                r_ask += 1 << log_once;
-                            }
-                        }
-#pragma unroll
-                    for (int e = 0; e < kAttendAsk; ++e)
-                        if (u0 + e < units) {
-                            if (share * per + e_now < n_parts) {
-                                const float most = fmaxf(m, s[e][0]), old = rescale(m, most, scale_log2), f = rescale(s[e][0], most, scale_log2);
-                                m = most;
-                                l = l * old + s[e][1] * f;
-                                y = y * old + v[e] * f;
-                            }
-                            if (++e_now == per) {
-                                if (shares == 1) {
-                                    if (team < TEAMS && r0 < rows_here) leave(r0, y, m, l);
-                                    r0 += 1 << log_once;
-                                    m = -INFINITY;
-                                    l = 0.f;
-                                    y = f32x4{0.f, 0.f, 0.f, 0.f};
-                                }
-                                e_now = 0;
-                            }
-                        }
-                }
-                if (shares > 1) {                    // (one round of rows)
-                    float* mine = &sums[0][0][0] + (team < TEAMS ? team : 0) * ROW;
-                    const bool here = team < TEAMS && r0 < rows_here;
-                    __syncthreads();
-                    if (here) {
-                        *reinterpret_cast<f32x4*>(mine + d) = y;
-                        if (d == 0) {
-                            mine[HDP] = m;
-                            mine[HDP + 1] = l;
-                        }
-                    }
-                    __syncthreads();
-                    if (here && share == 0) {
-                        float most = m;
-#pragma unroll 4
-                        for (int k = 1; k < shares; ++k) most = fmaxf(most, mine[(k << log_once) * ROW + HDP]);
-                        const float f0 = rescale(m, most, scale_log2);
-                        l *= f0;
-                        y *= f0;
-#pragma unroll 4
-                        for (int k = 1; k < shares; ++k) {
-                            const float* theirs = mine + (k << log_once) * ROW;
-                            const float f = rescale(theirs[HDP], most, scale_log2);
-                            l += theirs[HDP + 1] * f;
-                            y += *reinterpret_cast<const f32x4*>(theirs + d) * f;
-                        }
-                        leave(r0, y, most, l);
-                    }
-                }
-                if (done) break;
-                level = 1;
-                from = 0;
-                stride = kAttendFan;
-                n_parts = runs;
-            }
+            joins |= 1 << seg;
+            if (lane == 0) join_of[wv][seg] = make_int4(w0, count, begins_before, 0);
         }
         if (by_items) break;
         at += s1 - s0;
+        if (!whole && at < end) {              // (others may be waiting for this one's first part)
+            const int from = (unit - w0) / kAttendFan * kAttendFan;
+            arrived = arrive(0, part_of(w0, begins_before, from), min(kAttendFan, count - from));
+            joins = arrived ? 1 : 0;
+        }
         first_segment = false;
+    }
+
+    // Parts: each of the `count` workgroups from w0 on has left one (the first of them its last segment, if it began before the item).
+    // Runs of kAttendFan of them are added by the last one of the run, into the place of the run's first part, and the runs by the last run.
+    // (Behind the loop: inside, what this needs of registers would be kept through the pass over the keys.)
+#pragma unroll 1
+    for (int seg = 0; seg < 2; ++seg) {
+        if (!(joins >> seg & 1)) continue;
+        const int4 of = join_of[wv][seg];
+        const int w0 = whole_wave(of.x), count = whole_wave(of.y), runs = (count + kAttendFan - 1) / kAttendFan;
+        const bool begins_before = whole_wave(of.z);
+        int level = 0, from = (unit - w0) / kAttendFan * kAttendFan, stride = 1, n_parts = min(kAttendFan, count - from);
+        while (true) {
+            if (!arrived && !arrive(level, part_of(w0, begins_before, from), n_parts)) break;
+            arrived = false;
+            const bool done = level == 1 || runs == 1;
+            // Rows x four dimensions to the threads, and what is left of them shares the parts of a row.  A thread asks for kAttendAsk parts
+            // at once, those of its next rows among them.
+            constexpr int QUADS = HDP / 4, TEAMS = THREADS / QUADS >= 32 ? 32 : THREADS / QUADS >= 16 ? 16 : THREADS / QUADS >= 8 ? 8 : 4;
+            int log_once = 0;
+            while ((1 << log_once) < TEAMS && (1 << log_once) < rows_here) ++log_once;
+            const int shares = TEAMS >> log_once, per = (n_parts + shares - 1) >> (__builtin_ctz(TEAMS) - log_once);
+            const int team = tid / QUADS, d = tid % QUADS * 4, share = team >> log_once, row_in = team & ((1 << log_once) - 1);
+            const int units = ((rows_here + (1 << log_once) - 1) >> log_once) * per;
+            auto leave = [&](int r0, f32x4 y, float m, float l) {
+                if (done) {
+                    finish(seg, r0, d, y, m, l);
+                } else {
+                    const unsigned b = part_at(level2 + part_of(w0, begins_before, from), r0);
+                    store_through(parts, b + d * 4, a.part_bytes, y);
+                    if (d == 0) store_through(parts, b + HDP * 4, a.part_bytes, f32x4{m, l, 0.f, 0.f});
+                }
+            };
+            float m = -INFINITY, l = 0.f;
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+            int r_ask = row_in, e_ask = 0, r0 = row_in, e_now = 0;           // row and part of the next one to ask for, and to add
+            for (int u0 = 0; u0 < units; u0 += kAttendAsk) {
+                f32x2 s[kAttendAsk];
+                f32x4 v[kAttendAsk];
+#pragma unroll
+                for (int e = 0; e < kAttendAsk; ++e)
+                    if (u0 + e < units) {
+                        const unsigned b = part_at(level * level2 + part_of(w0, begins_before, from + min(share * per + e_ask, n_parts - 1) * stride),
+                                                   min(r_ask, rows_here - 1));
+                        s[e] = load_through2(a.parts, b + HDP * 4, a.part_bytes);
+                        v[e] = load_through(a.parts, b + d * 4, a.part_bytes);
+                        if (++e_ask == per) {
+                            e_ask = 0;
+                            r_ask += 1 << log_once;
+                        }
+                    }
+#pragma unroll
+                for (int e = 0; e < kAttendAsk; ++e)
+                    if (u0 + e < units) {
+                        if (share * per + e_now < n_parts) {
+                            const float most = fmaxf(m, s[e][0]), old = rescale(m, most, scale_log2), f = rescale(s[e][0], most, scale_log2);
+                            m = most;
+                            l = l * old + s[e][1] * f;
+                            y = y * old + v[e] * f;
+                        }
+                        if (++e_now == per) {
+                            if (shares == 1) {
+                                if (team < TEAMS && r0 < rows_here) leave(r0, y, m, l);
+                                r0 += 1 << log_once;
+                                m = -INFINITY;
+                                l = 0.f;
+                                y = f32x4{0.f, 0.f, 0.f, 0.f};
+                            }
+                            e_now = 0;
+                        }
+                    }
+            }
+            if (shares > 1) {                    // (one round of rows)
+                float* mine = &sums[0][0][0] + (team < TEAMS ? team : 0) * ROW;
+                const bool here = team < TEAMS && r0 < rows_here;
+                __syncthreads();
+                if (here) {
+                    *reinterpret_cast<f32x4*>(mine + d) = y;
+                    if (d == 0) {
+                        mine[HDP] = m;
+                        mine[HDP + 1] = l;
+                    }
+                }
+                __syncthreads();
+                if (here && share == 0) {
+                    float most = m;
+#pragma unroll 4
+                    for (int k = 1; k < shares; ++k) most = fmaxf(most, mine[(k << log_once) * ROW + HDP]);
+                    const float f0 = rescale(m, most, scale_log2);
+                    l *= f0;
+                    y *= f0;
+#pragma unroll 4
+                    for (int k = 1; k < shares; ++k) {
+                        const float* theirs = mine + (k << log_once) * ROW;
+                        const float f = rescale(theirs[HDP], most, scale_log2);
+                        l += theirs[HDP + 1] * f;
+                        y += *reinterpret_cast<const f32x4*>(theirs + d) * f;
+                    }
+                    leave(r0, y, most, l);
+                }
+            }
+            if (done) break;
+            level = 1;
+            from = 0;
+            stride = kAttendFan;
+            n_parts = runs;
+        }
     }
 }
 
 template <typename T, int HDP, int QT>
 void launch_attend(const AttendArgs& a, int groups, hipStream_t s) {
     if (a.dim == HDP) {
-        hipLaunchKernelGGL((k_kv_attend<T, HDP, true, QT>), dim3(groups), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_kv_attend<T, HDP, true, QT>), dim3(groups), dim3(64 * attend_waves(HDP, true, QT, sizeof(T))), 0, s, a);
     } else if constexpr (HDP != 80 && QT <= 2) {
-        hipLaunchKernelGGL((k_kv_attend<T, HDP, false, QT>), dim3(groups), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_kv_attend<T, HDP, false, QT>), dim3(groups), dim3(64 * attend_waves(HDP, false, QT, sizeof(T))), 0, s, a);
     }
 }
 
