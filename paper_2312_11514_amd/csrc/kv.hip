@@ -29,7 +29,7 @@ struct lif_kv {
 namespace {
 
 constexpr long long kMaxPositions = 1 << 24;     // of a sequence: the steps of 1024 of them are counted in 32 bits
-constexpr int kAttendFew = 1024;                 // steps that run at once, or nearly
+constexpr int kAttendFew = 4096;                 // steps that run at once, or nearly
 constexpr int kAppendGroups = 2048;              // workgroups for queries and keys that fill the chip
 constexpr int kMoveBlocks = 2048;                // 8 workgroups of copies per compute unit
 constexpr int kCopyBlocks = 256;                 // ... behind lif_kv_reserve, which has a page to copy once in a while
@@ -71,14 +71,17 @@ struct KvLayout {
 // How the rows of an item, tokens x query heads of a key head, are dealt: blocks of 16 * tiles rows, and workgroups for each of them.
 // `positions`: of a sequence to go through, at most.
 // A workgroup reads the keys once for its block, so blocks are as large as registers allow; where there are so few that all their steps
-// run at once, the time is that of one workgroup, and smaller ones are faster (71 rows, 8 sequences of up to 2047: 9.6 us with blocks of 16,
-// 25.9 with 64).
+// run at once, or nearly, the time is that of one workgroup with its parts, and smaller ones are faster (16 tokens of 2 sequences of 4000, 32
+// heads of 128 on 8: 22.2 us in blocks of 16 rows, 45.2 in ones of 64).
 struct Tiling {
-    int tiles, blocks, block_rows, units;
+    int tiles, blocks, block_rows, units, round_units, round_steps;
     long long steps;                     // of a block's items, at most
 };
 // The workgroups of few blocks are what fits the chip, in eights (those of one XCD share keys); of many blocks four rounds and more of
-// shorter ones, to end together; of very many blocks they are enough by themselves, and no item has parts.
+// shorter ones, in eights too; of very many blocks they are enough by themselves, and no item has parts.  What a workgroup costs beside its
+// steps is worth about five of them, so rounds of short ones are slow (20 tokens of 32 sequences of 2000, 71 heads of 64 on one: 162 us): of
+// fewer steps than 16 per workgroup (64 if nine tenths of the chip have work) only one round of them is in use (73 us; 20 tokens
+// of 64 sequences of 8000 467 -> 383 us).
 int units_of(int blocks, int resident) {
     if (blocks == 1) return resident;
     if (blocks <= 8) return std::max(8, resident / blocks / 8 * 8);
@@ -96,7 +99,7 @@ Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) 
         return (long long)batch * c.kv_heads * ((positions + step - 1) / step + 1);
     };
     Tiling g;
-    g.tiles = std::min(attend_most_tiles(c.head_dim), need <= 1 ? 1 : need <= 2 ? 2 : 4);
+    g.tiles = std::min(attend_most_tiles(c.head_dim), need <= (pad > 128 ? 2 : 1) ? 1 : need <= 2 ? 2 : 4);
     while (g.tiles > 1 && steps_of(4) * ((need + g.tiles / 2 - 1) / (g.tiles / 2)) <= kAttendFew) g.tiles /= 2;
     // of several blocks the last one may be mostly empty: 71 rows, 8 x 16000 positions, heads of 64: 33.5 us in two blocks of 64
     while (g.tiles > 1 && need > g.tiles && 4 * ((need + g.tiles - 1) / g.tiles * g.tiles) > 5 * need) g.tiles /= 2;
@@ -104,6 +107,9 @@ Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) 
     g.blocks = (need + g.tiles - 1) / g.tiles;
     g.block_rows = std::min(rows, 16 * g.tiles);
     g.units = units_of(g.blocks, resident_of(c, g.tiles));
+    const int at_once = resident_of(c, g.tiles);
+    g.round_units = g.blocks <= 8 ? g.units : std::min(g.units, std::max(1, at_once / g.blocks));
+    g.round_steps = g.blocks <= 8 ? 0 : g.units * (10 * g.round_units * g.blocks >= 9 * at_once ? 64 : 16);
     return g;
 }
 // floats of the parts of any call
@@ -328,7 +334,7 @@ int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* st
                  query->slots, query->starts, reinterpret_cast<const unsigned long long*>(query->tree), v.k + layer_at, v.v + layer_at, v.table,
                  v.lengths, v.fresh, &v.st->error, kv->parts, kv->arrived, (unsigned)kv->part_bytes, (unsigned)v.page_bytes,
                  (unsigned)(v.page_bytes / c.kv_heads), c.pages, c.max_seqs, c.max_pages, v.log_page, query->batch, query->n_tokens, c.heads,
-                 c.kv_heads, share, c.head_dim, query->window, g.units, g.blocks, g.block_rows, c.scale * kLog2e};
+                 c.kv_heads, share, c.head_dim, query->window, g.units, g.round_units, g.round_steps, g.blocks, g.block_rows, c.scale * kLog2e};
     hipStream_t s = (hipStream_t)stream;
     using Launch = void (*)(const AttendArgs&, int, hipStream_t);
     static constexpr Launch kLaunch[3][3] = {{launch_attend_f32_1, launch_attend_f32_2, launch_attend_f32_4},

@@ -56,6 +56,7 @@ struct AttendArgs {
     int32_t pages, max_seqs, max_pages, log_page;
     int32_t batch, n_tokens, heads, kv_heads, share, dim, window;
     int32_t units;                         // workgroups of a block of rows
+    int32_t round_units, round_steps;      // of them, so many that all blocks' run at once; steps of a block below which only those work
     int32_t row_blocks, block_rows;        // blocks of 16 * tiles rows of an item; rows of a block that are there at most
     float scale_log2;                      // scale * log2 e
 };
@@ -76,7 +77,7 @@ __host__ __device__ __forceinline__ int attend_dim_pad(int dim) {
     return dim <= 32 ? 32 : dim <= 64 ? 64 : dim == 80 ? 80 : dim <= 96 ? 96 : dim <= 128 ? 128 : 256;
 }
 // most tiles of 16 rows that a wave has registers for: dimensions that are not the compiled ones take some for their bounds
-__host__ __device__ __forceinline__ int attend_most_tiles(int dim) { return dim > 128 ? 1 : dim == attend_dim_pad(dim) ? 4 : 2; }
+__host__ __device__ __forceinline__ int attend_most_tiles(int dim) { return dim == 256 ? 2 : dim > 128 ? 1 : dim == attend_dim_pad(dim) ? 4 : 2; }
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend
     // What a wave needs of its rows only now and then is not kept in registers: their place in `out` (a row, negative for padding, and the
     // head), of the first segment and of later ones; first position, last new token, and which of those they see.  Queries of several
     // tiles neither: 128 dimensions by 32 rows fit 256 registers then, and two workgroups a compute unit.
-    constexpr bool QLDS = QT > 1 && attend_lean(HDP, FULL, QT, sizeof(T));
+    constexpr bool QLDS = QT > 1 && (attend_lean(HDP, FULL, QT, sizeof(T)) || (HDP == 256 && CH <= 8));
     __shared__ int2 out_at[2][16 * QT], sees_at[WAVES][16 * QT];
     __shared__ unsigned long long seen_at[WAVES][16 * QT];
     __shared__ V q_at[QLDS ? WAVES : 1][QLDS ? QT : 1][QLDS ? CH : 1][64];
@@ -245,10 +246,16 @@ __global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend
     if (whole_wave(error)) return;
     int total = rc.after;
     for (int c0 = 64; c0 < a.batch; c0 += 64) total = row_chunk(a, STAGE, STEP, c0, total).after;
+    const int all = total * a.kv_heads;        // (below 2^31: lif_kv_attend has seen to it)
     // which block of rows, and which of its workgroups: those that read the same keys are eight apart, on one XCD
-    int block = 0, unit = blockIdx.x;
+    int block = 0, unit = blockIdx.x, units = a.units;
     if (a.row_blocks > 1) {
-        if (a.units % 8 == 0) {
+        if (all < a.round_steps) {             // all blocks' at once, each workgroup with more steps
+            units = a.round_units;
+            block = quotient(blockIdx.x, units);
+            if (block >= a.row_blocks) return;
+            unit = (int)blockIdx.x - block * units;
+        } else if (a.units % 8 == 0) {
             const int eights = (int)blockIdx.x >> 3, high = quotient(eights, a.row_blocks);
             block = eights - high * a.row_blocks;
             unit = high * 8 + ((int)blockIdx.x & 7);
@@ -259,8 +266,7 @@ __global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend
     }
     const int slots0 = 2 * block * a.units;    // the block's first place for a part
     const int rows = a.n_tokens * a.share, row0 = block * QT * 16;
-    const int all = total * a.kv_heads;        // (below 2^31: lif_kv_attend has seen to it)
-    int run_steps = quotient(all + a.units - 1, a.units);
+    int run_steps = quotient(all + units - 1, units);
     // by items: parts of the lane's row, steps of each, parts of the rows before
     int parts_of_row = 0, part_steps = 1, parts_before = 0;
     bool by_items = false;
@@ -272,7 +278,7 @@ __global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend
             const int up_to = wave_inclusive_scan(parts_of_row, lane);
             parts_before = up_to - parts_of_row;
             const int needed = __builtin_amdgcn_readlane(up_to, 63) * a.kv_heads;
-            by_items = needed <= a.units;
+            by_items = needed <= units;
             if (by_items && unit >= needed) return;
             if (run_steps < 8) break;
         }
@@ -580,11 +586,11 @@ __global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend
         for (int t = 0; t < QT; ++t) {
 #pragma unroll
             for (int half = 0; half < HALF; ++half) {
-                if (t || half) __syncthreads();
+                if (t || half) lds_barrier();
 #pragma unroll
                 for (int d = 0; d < DT / HALF; ++d)
                     *reinterpret_cast<f32x4*>(&sums[wv][n][16 * d + 4 * g]) = o[t][half * (DT / HALF) + d];
-                __syncthreads();
+                lds_barrier();
                 for (int u = tid; u < 16 * (COLS / 4); u += THREADS) {
                     const int rr = u / (COLS / 4), d = u % (COLS / 4) * 4, r0 = 16 * t + rr;
                     if (r0 >= rows_here) break;
@@ -742,7 +748,7 @@ template <typename T, int HDP, int QT>
 void launch_attend(const AttendArgs& a, int groups, hipStream_t s) {
     if (a.dim == HDP) {
         hipLaunchKernelGGL((k_kv_attend<T, HDP, true, QT>), dim3(groups), dim3(64 * attend_waves(HDP, true, QT, sizeof(T))), 0, s, a);
-    } else if constexpr (HDP != 80 && QT <= 2) {
+    } else if constexpr (HDP != 80 && QT <= (HDP == 256 ? 1 : 2)) {
         hipLaunchKernelGGL((k_kv_attend<T, HDP, false, QT>), dim3(groups), dim3(64 * attend_waves(HDP, false, QT, sizeof(T))), 0, s, a);
     }
 }
@@ -756,7 +762,7 @@ void launch_attend_tiles(const AttendArgs& a, int groups, hipStream_t s) {
         case 96: return launch_attend<T, 96, QT>(a, groups, s);
         case 128: return launch_attend<T, 128, QT>(a, groups, s);
         default:
-            if constexpr (QT == 1) launch_attend<T, 256, QT>(a, groups, s);
+            if constexpr (QT <= 2) launch_attend<T, 256, QT>(a, groups, s);
     }
 }
 

@@ -16,7 +16,7 @@ def ints(values):
 
 
 def build(lengths, fresh, *, kv_heads, head_dim, page, dtype, seed, heads=None, layers=2, layer=1, spare=3, garbage=float("nan"), max_tokens=None,
-          slots=None, max_seqs=None, **more):
+          slots=None, max_seqs=None, max_pages=0, **more):
     """A cache whose sequences (batch row i in slot slots[i]) hold random keys and values in layer `layer`, pages scattered over the pool,
     and `garbage` everywhere else: in free pages, in other layers, behind the last token of a page.
     Returns the cache and the fp64 keys and values per row, [kv_heads, n, head_dim]."""
@@ -24,11 +24,11 @@ def build(lengths, fresh, *, kv_heads, head_dim, page, dtype, seed, heads=None, 
     rng = np.random.default_rng(seed)
     per = [-(-n // page) for n in lengths]
     slots = list(range(len(lengths))) if slots is None else slots
-    max_seqs = max_seqs or max(slots) + 1
+    max_seqs, max_pages = max_seqs or max(slots) + 1, max(per + [1, max_pages])
     kv = lif.KVCache(layers=layers, heads=heads or kv_heads, kv_heads=kv_heads, head_dim=head_dim, page_tokens=page, pages=sum(per) + spare,
-                     max_seqs=max_seqs, max_pages=max(per + [1]), max_tokens=max_tokens or max(list(fresh) + [1]), dtype=dtype, **more)
+                     max_seqs=max_seqs, max_pages=max_pages, max_tokens=max_tokens or max(list(fresh) + [1]), dtype=dtype, **more)
     order = rng.permutation(sum(per) + spare).tolist()
-    table = np.full((max_seqs, max(per + [1])), -1, np.int32)
+    table = np.full((max_seqs, max_pages), -1, np.int32)
     n_of, f_of = np.zeros(max_seqs, np.int32), np.zeros(max_seqs, np.int32)
     kv.k.fill_(garbage)
     kv.v.fill_(garbage)

@@ -28,9 +28,9 @@ def _check(out, lse, ref, dtype, n, d, tag):
 
 
 def _run(lengths, fresh, *, heads, kv_heads, head_dim, page, dtype, tokens, window=0, starts=None, tree=None, seed=1, slots=None, peaked=1.0,
-         max_seqs=None, change=None, stride=0):
+         max_seqs=None, max_pages=0, change=None, stride=0):
     kv, rows = build(lengths, fresh, kv_heads=kv_heads, head_dim=head_dim, page=page, dtype=dtype, seed=seed, heads=heads, max_tokens=tokens,
-                     slots=slots, max_seqs=max_seqs)
+                     slots=slots, max_seqs=max_seqs, max_pages=max_pages)
     rng = np.random.default_rng(seed + 1)
     b = len(lengths)
     wide = torch.from_numpy(peaked * rng.standard_normal((b, tokens, heads * head_dim + stride), dtype=np.float32)).to(DTYPES[dtype]).cuda()
@@ -99,6 +99,31 @@ def test_many_tokens(dtype, heads, kv_heads, head_dim, tokens):
          tokens=tokens)
 
 
+# How many rows a workgroup takes together goes by the rows and by what a full table would make of steps: the same calls with wide tables.
+LARGE = [("f16", 8, 1, 128), ("bf16", 8, 2, 128), ("f32", 8, 1, 128), ("f16", 9, 1, 64), ("f32", 8, 2, 64), ("bf16", 6, 1, 80), ("f32", 9, 1, 80),
+         ("f16", 8, 1, 96), ("f32", 8, 1, 96), ("bf16", 8, 1, 32), ("f32", 8, 1, 32), ("f16", 8, 1, 256), ("f32", 8, 1, 256), ("bf16", 8, 1, 112),
+         ("f32", 9, 1, 40), ("f16", 8, 1, 200), ("f16", 9, 1, 24)]
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,head_dim", LARGE)
+@pytest.mark.parametrize("tokens", [4, 11])
+def test_rows_together(dtype, heads, kv_heads, head_dim, tokens):
+    lengths, fresh = [tokens, 700, 0, 150, 33, 2100], [tokens, tokens, 0, tokens - 1, 2, tokens]
+    kw = dict(heads=heads, kv_heads=kv_heads, head_dim=head_dim, page=16, dtype=dtype, tokens=tokens, max_pages=1 << 17)
+    _run(lengths, fresh, **kw)
+    rng = np.random.default_rng(tokens)
+    tree = [[int(w) | 1 << j if j else 1 for j, w in enumerate(rng.integers(0, 1 << tokens, tokens))] for _ in lengths]
+    _run(lengths, fresh, tree=tree, window=600, starts=[0, 5, 0, 149, 1, 40], **kw)
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,head_dim,tokens", [("f16", 71, 1, 64, 20), ("f32", 40, 1, 32, 30), ("bf16", 40, 2, 128, 40),
+                                                                  ("bf16", 71, 1, 64, 256)])
+@pytest.mark.parametrize("max_pages", [0, 1 << 17])
+def test_many_blocks_of_rows(dtype, heads, kv_heads, head_dim, tokens, max_pages):
+    _run([tokens + 130, 0, tokens, 1200], [tokens, 0, tokens // 2, tokens], heads=heads, kv_heads=kv_heads, head_dim=head_dim, page=16, dtype=dtype,
+         tokens=tokens, max_pages=max_pages)
+
+
 @pytest.mark.parametrize("batch", [1, 70, 300, 1024])
 def test_batches(batch):
     rng = np.random.default_rng(batch)
@@ -135,9 +160,10 @@ def test_many_small_weights_beside_a_large_one(dtype):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_what_a_token_does_not_see_never_reaches_it(dtype, bad):
+@pytest.mark.parametrize("max_pages", [0, 1 << 18])
+def test_what_a_token_does_not_see_never_reaches_it(dtype, bad, max_pages):
     """Keys and values that are not finite at positions before `starts`, behind a window, of later tokens and of other branches of a tree."""
-    for heads, kv_heads, d in ((2, 1, 64), (4, 1, 128), (24, 1, 40)):
+    for heads, kv_heads, d in ((2, 1, 64), (4, 1, 128), (24, 1, 40), (6, 1, 128), (10, 1, 64)):
         tree = [[1, 3, 5, 11, 21]]
         spots = [(0, 36), (0, 38), (0, 39)]                       # the second, fourth and fifth of five new tokens, among others
 
@@ -155,7 +181,7 @@ def test_what_a_token_does_not_see_never_reaches_it(dtype, bad):
 
         for starts, window in (([13], 0), (None, 24)):
             for t in (None, tree):
-                kv, rows = build([40], [5], kv_heads=kv_heads, head_dim=d, page=16, dtype=dtype, seed=4, heads=heads)
+                kv, rows = build([40], [5], kv_heads=kv_heads, head_dim=d, page=16, dtype=dtype, seed=4, heads=heads, max_pages=max_pages)
                 change(kv, rows, None)
                 q = torch.randn(1, 5, heads, d, device="cuda").to(DTYPES[dtype])
                 out, lse = torch.empty_like(q), torch.empty(1, 5, heads, device="cuda")
@@ -176,12 +202,12 @@ def test_what_a_token_does_not_see_never_reaches_it(dtype, bad):
 
 def test_a_value_that_is_not_finite_reaches_the_rows_that_see_it():
     """... with its sign, and only its own dimension"""
-    for dtype in ("f16", "f32"):
-        kv, rows = build([40], [3], kv_heads=1, head_dim=64, page=16, dtype=dtype, seed=4, heads=2)
+    for dtype, heads, max_pages in (("f16", 2, 0), ("f32", 2, 0), ("f16", 9, 1 << 18), ("f32", 17, 1 << 18)):
+        kv, rows = build([40], [3], kv_heads=1, head_dim=64, page=16, dtype=dtype, seed=4, heads=heads, max_pages=max_pages)
         page, e = int(kv.table[0, 2]), kv.v.shape[5]
         j = 38                                                     # the second of three new tokens
         kv.v[1, page, 0, j % 16 // e, 11, j % 16 % e] = -float("inf")
-        q = torch.randn(1, 3, 2, 64, device="cuda").to(DTYPES[dtype])
+        q = torch.randn(1, 3, heads, 64, device="cuda").to(DTYPES[dtype])
         out = torch.empty_like(q)
         kv.attend(1, q, out)
         others = [d for d in range(64) if d != 11]
