@@ -32,7 +32,7 @@ constexpr long long kMaxPositions = 1 << 24;     // of a sequence: the steps of 
 constexpr int kAttendFew = 4096;                 // steps that run at once, or nearly
 constexpr int kAppendGroups = 2048;              // workgroups for queries and keys that fill the chip
 constexpr int kMoveBlocks = 2048;                // 8 workgroups of copies per compute unit
-constexpr int kCopyBlocks = 256;                 // ... behind lif_kv_reserve, which has a page to copy once in a while
+constexpr int kCopyBlocks = 128;                 // workgroups of lif_kv_reserve, which has a page to copy once in a while
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 int elem_bytes(int dtype) { return dtype == LIF_F32 ? 4 : 2; }
@@ -249,9 +249,8 @@ int lif_kv_adopt(lif_kv* kv, void* stream) {
 int lif_kv_reserve(lif_kv* kv, const int32_t* counts_dev, void* stream) {
     if (!kv || !counts_dev) return fail(LIF_INVALID_ARG, "null pointer");
     const int threads = plan_threads(kv);
-    hipLaunchKernelGGL(threads == kKvPlanFew ? k_kv_reserve<kKvPlanFew> : k_kv_reserve<kKvMaxSeqs>, dim3(1), dim3(threads), 0, (hipStream_t)stream,
-                       kv->view, counts_dev);
-    hipLaunchKernelGGL((k_kv_move<KV_COPY>), dim3(kCopyBlocks), dim3(256), 0, (hipStream_t)stream, kv->view, nullptr, nullptr, 0);
+    hipLaunchKernelGGL(threads == kKvPlanFew ? k_kv_reserve<kKvPlanFew> : k_kv_reserve<kKvMaxSeqs>, dim3(kCopyBlocks), dim3(threads), 0,
+                       (hipStream_t)stream, kv->view, counts_dev);
     return launched();
 }
 

@@ -13,6 +13,7 @@ struct KvState {
     int32_t n_moves;         // pages to copy by the launch that follows a plan
     int32_t ok;              // whether the plan of a fork or a compaction stands
     int32_t shares;          // whether a page may have several holders: since a fork, or tables that were adopted so
+    unsigned planned;        // workgroups of a reservation that have planned; zero between calls
 };
 
 // What the kernels know of a cache.

@@ -2,7 +2,8 @@
 //
 // A page is free iff refs[page] == 0.  The same as one bit per page, set where it is free, is what the calls look for pages in: 64
 // pages a word, so that one workgroup sees 65536 pages per pass.  The plans (which page goes where) are made by one workgroup, whose
-// time is a few dependent memory round trips; the copies that follow from them by a launch over the whole chip (k_kv_move).
+// time is a few dependent memory round trips; the copies that follow from them by a launch over the whole chip (k_kv_move).  A reservation,
+// which every step of a program makes, is a single launch.
 #pragma once
 
 #include "lif_kv.h"
@@ -104,15 +105,46 @@ __global__ __launch_bounds__(256) void k_kv_adopt(const KvView kv) {
     if (bad) atomicExch(&kv.st->error, 2 /* LIF_BAD_STATE */);
 }
 
-// ---- reserve: one workgroup -------------------------------------------------------------------------------------------------
+// ---- copies of pages ------------------------------------------------------------------------------------------------------------
+// kKvPiece bytes of one page of one layer at a time by 256 threads: 16-byte loads, four in flight per thread, neighbouring workgroups on
+// neighbouring pieces; the pieces first, first + step, ..
+constexpr int kKvPiece = 256 * 16 * 4;
 
+__device__ __forceinline__ void copy_pages(const KvView& kv, const int2* moves, int n_moves, unsigned first, unsigned step) {
+    const unsigned pieces = (unsigned)((kv.page_bytes + kKvPiece - 1) / kKvPiece), per_move = pieces * 2u * (unsigned)kv.layers;
+    const unsigned long long units = (unsigned long long)n_moves * per_move;
+    for (unsigned long long u = first; u < units; u += step) {
+        const unsigned move = (unsigned)(u / per_move), rest = (unsigned)(u % per_move), piece = rest % pieces, part = rest / pieces;
+        const int2 m = moves[move];
+        char* pool = (part & 1) ? kv.v : kv.k;
+        const size_t layer = (size_t)(part >> 1) * kv.pages;
+        const char* from = pool + (layer + m.x) * kv.page_bytes;
+        char* to = pool + (layer + m.y) * kv.page_bytes;
+        const size_t at = (size_t)piece * kKvPiece + (size_t)(threadIdx.x & 255) * 16;
+        f32x4 held[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (at + q * 4096 < kv.page_bytes) held[q] = *reinterpret_cast<const f32x4*>(from + at + q * 4096);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (at + q * 4096 < kv.page_bytes) *reinterpret_cast<f32x4*>(to + at + q * 4096) = held[q];
+    }
+}
+
+// ---- reserve: grid = the first workgroup, and those that copy if there may be something to ----------------------------------------
+// Without sharing the first workgroup does everything.  With it every workgroup works out the same plan for itself, and copies its
+// part of the pages; nothing that the plan follows from may change before all of them have read it, so it is the last one to have
+// planned that writes it down.  One launch, and no workgroup waits for another (reserve + truncate of 65 slots, called one after the other:
+// 8.8 us a pair; 12.2 with the copies in a launch of their own).
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_kv_reserve(const KvView kv, const int32_t* __restrict__ counts) {
     __shared__ WalkScratch<THREADS> ws;
-    __shared__ int first[THREADS], had_of[THREADS], copy_of[THREADS];
+    __shared__ int first[THREADS], had_of[THREADS], copy_of[THREADS], last;
+    __shared__ int2 moves[THREADS];                      // the copies
     const int slot = threadIdx.x, words = (kv.pages + 63) / 64;
     KvState* st = kv.st;
     const int error = st->error, used = st->used, shares = st->shares;
+    if (blockIdx.x > 0 && !shares) return;
     const unsigned long long ahead = word_ahead(kv.free_bits, 0, words);
     int length = 0, count = 0;
     if (slot < kv.max_seqs) {
@@ -139,20 +171,35 @@ __global__ __launch_bounds__(THREADS) void k_kv_reserve(const KvView kv, const i
     had_of[slot] = had - (shared >= 0);
     copy_of[slot] = shared >= 0 ? copy0 : -1;
     if (__syncthreads_or(!fits) || total > kv.pages - used) {
-        if (slot == 0) {
-            st->error = 3 /* LIF_CAPACITY */;
+        if (slot == 0 && blockIdx.x == 0) {
+            st->error = 3 /* LIF_CAPACITY */;            // (who reads it before the counts comes to the same end)
             st->n_moves = 0;
         }
         return;
+    }
+    const int slots = min(THREADS, kv.max_seqs);
+    if (shares) {
+        if (shared >= 0) moves[copy0].x = shared;
+        if (copies > 0)
+            walk_bits(
+                kv.free_bits, 0, words, total, ahead, ws, [](int, unsigned long long w) { return w; },
+                [&](int rank, int page) {
+                    const int s = last_not_above(first, slots, rank);
+                    if (rank == first[s] && copy_of[s] >= 0) moves[copy_of[s]].y = page;
+                },
+                [](int, unsigned long long) {});
+        __syncthreads();                                 // (what this workgroup read has arrived)
+        if (slot == 0) last = atomicInc(&st->planned, gridDim.x - 1) == gridDim.x - 1;
+        __syncthreads();
+        copy_pages(kv, moves, copies, blockIdx.x * (THREADS / 256) + threadIdx.x / 256, gridDim.x * (THREADS / 256));
+        if (!last) return;
     }
     if (total > 0) {
         walk_bits(
             kv.free_bits, 0, words, total, ahead, ws, [](int, unsigned long long w) { return w; },
             [&](int rank, int page) {
-                const int s = last_not_above(first, min(THREADS, kv.max_seqs), rank), j = rank - first[s];
-                int32_t* at = kv.table + (size_t)s * kv.max_pages + had_of[s] + j;
-                if (j == 0 && copy_of[s] >= 0) kv.moves[copy_of[s]] = make_int2(*at, page);
-                *at = page;
+                const int s = last_not_above(first, slots, rank), j = rank - first[s];
+                kv.table[(size_t)s * kv.max_pages + had_of[s] + j] = page;
                 kv.refs[page] = 1;
             },
             [&](int w, unsigned long long taken) { kv.free_bits[w] &= ~taken; });
@@ -304,10 +351,8 @@ __global__ __launch_bounds__(THREADS) void k_kv_compact(const KvView kv) {
 }
 
 // ---- what the plans leave to the whole chip ---------------------------------------------------------------------------------
-// The first `table_blocks` workgroups bring the tables in line, the others copy pages, kKvPiece bytes of one page of one layer at a time:
-// 16-byte loads, four in flight per thread, neighbouring workgroups on neighbouring pieces.
-enum { KV_COPY = 0, KV_FORK = 1, KV_COMPACT = 2 };
-constexpr int kKvPiece = 256 * 16 * 4;
+// The first `table_blocks` workgroups bring the tables in line, the others copy pages.
+enum { KV_FORK = 1, KV_COMPACT = 2 };
 
 template <int JOB>
 __global__ __launch_bounds__(256) void k_kv_move(const KvView kv, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
@@ -316,7 +361,7 @@ __global__ __launch_bounds__(256) void k_kv_move(const KvView kv, const int32_t*
     const int n_moves = st->n_moves;
     if (st->error || !st->ok) return;
     const int tid = threadIdx.x;
-    if (JOB != KV_COPY && (int)blockIdx.x < table_blocks) {
+    if ((int)blockIdx.x < table_blocks) {
         if constexpr (JOB == KV_FORK) {                  // a pair: full pages shared, the copy behind them
             const int i = blockIdx.x, copy = kv.remap[i], held = pages_of(length_of(kv, dst[i]), kv.log_page);
             const int32_t* from = kv.table + (size_t)src[i] * kv.max_pages;
@@ -341,24 +386,7 @@ __global__ __launch_bounds__(256) void k_kv_move(const KvView kv, const int32_t*
         }
         return;
     }
-    const unsigned pieces = (unsigned)((kv.page_bytes + kKvPiece - 1) / kKvPiece), per_move = pieces * 2u * (unsigned)kv.layers;
-    const unsigned long long units = (unsigned long long)n_moves * per_move, step = gridDim.x - table_blocks;
-    for (unsigned long long u = blockIdx.x - table_blocks; u < units; u += step) {
-        const unsigned move = (unsigned)(u / per_move), rest = (unsigned)(u % per_move), piece = rest % pieces, part = rest / pieces;
-        const int2 m = kv.moves[move];
-        char* pool = (part & 1) ? kv.v : kv.k;
-        const size_t layer = (size_t)(part >> 1) * kv.pages;
-        const char* from = pool + (layer + m.x) * kv.page_bytes;
-        char* to = pool + (layer + m.y) * kv.page_bytes;
-        const size_t at = (size_t)piece * kKvPiece + (size_t)tid * 16;
-        f32x4 held[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (at + q * 4096 < kv.page_bytes) held[q] = *reinterpret_cast<const f32x4*>(from + at + q * 4096);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (at + q * 4096 < kv.page_bytes) *reinterpret_cast<f32x4*>(to + at + q * 4096) = held[q];
-    }
+    copy_pages(kv, kv.moves, n_moves, blockIdx.x - table_blocks, gridDim.x - table_blocks);
 }
 
 }  // namespace lif
