@@ -194,6 +194,7 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
     };
     if constexpr (NORM) ask_weights(first + group >= a.heads);
 
+    const double frequency = (int)threadIdx.x < half ? a.frequencies[threadIdx.x] : 0.;
     const int error = kv.st->error;
     const NewTokens n = new_tokens(kv, a, i);
     if (error) return;
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
     int page = -1;
     if (there) page = kv.table[(size_t)n.slot * kv.max_pages + (at >> kv.log_page)];
     if (there && (int)threadIdx.x < half)
-        turn(a.positions ? a.positions[row] : at, a.frequencies[threadIdx.x], a.magnitude, cosine[threadIdx.x], sine[threadIdx.x]);
+        turn(a.positions ? a.positions[row] : at, frequency, a.magnitude, cosine[threadIdx.x], sine[threadIdx.x]);
     __syncthreads();
     if (!there) {                                              // (the whole workgroup)
         for (int head = first + group; head < min(last, a.heads); head += groups)
