@@ -74,7 +74,7 @@ struct KvLayout {
 // run at once, or nearly, the time is that of one workgroup with its parts, and smaller ones are faster (16 tokens of 2 sequences of 4000, 32
 // heads of 128 on 8: 22.2 us in blocks of 16 rows, 45.2 in ones of 64).
 struct Tiling {
-    int tiles, blocks, block_rows, units, round_units, round_steps;
+    int tiles, waves, blocks, block_rows, units, round_units, round_steps;
     long long steps;                     // of a block's items, at most
 };
 // The workgroups of few blocks are what fits the chip, in eights (those of one XCD share keys); of many blocks four rounds and more of
@@ -88,9 +88,9 @@ int units_of(int blocks, int resident) {
     if (blocks <= 128) return (128 + blocks - 1) / blocks * 8;
     return 1;
 }
-int resident_of(const lif_kv_config& c, int tiles) {
+bool lean(const lif_kv_config& c, int tiles) {
     const int pad = attend_dim_pad(c.head_dim);
-    return kAttendUnits * attend_resident(pad, pad == c.head_dim, tiles, elem_bytes(c.dtype));
+    return attend_lean(pad, pad == c.head_dim, tiles, elem_bytes(c.dtype));
 }
 Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) {
     const int bytes = elem_bytes(c.dtype), pad = attend_dim_pad(c.head_dim), need = (rows + 15) / 16;
@@ -103,11 +103,17 @@ Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) 
     while (g.tiles > 1 && steps_of(4) * ((need + g.tiles / 2 - 1) / (g.tiles / 2)) <= kAttendFew) g.tiles /= 2;
     // of several blocks the last one may be mostly empty: 71 rows, 8 x 16000 positions, heads of 64: 33.5 us in two blocks of 64
     while (g.tiles > 1 && need > g.tiles && 4 * ((need + g.tiles - 1) / g.tiles * g.tiles) > 5 * need) g.tiles /= 2;
-    g.steps = steps_of(attend_waves(pad, pad == c.head_dim, g.tiles, bytes));
     g.blocks = (need + g.tiles - 1) / g.tiles;
     g.block_rows = std::min(rows, 16 * g.tiles);
-    g.units = units_of(g.blocks, resident_of(c, g.tiles));
-    const int at_once = resident_of(c, g.tiles);
+    // Eight waves share a part, or four: the larger parts are fewer to add, the smaller ones fill the chip sooner, and two workgroups of them hide
+    // each other's beginnings and ends.  Larger ones pay where a part has some rows, and where no workgroup goes through more than one item (4 tokens of
+    // 4 sequences of up to 4000, 32 heads on 8: 20.8 us with four, 14.2 with eight; 64 sequences of one: 144.5 and 149.3).
+    const long long items = (long long)batch * c.kv_heads * g.blocks;
+    const bool fits = lean(c, g.tiles), some = g.block_rows >= 4 && (positions > (g.block_rows >= 16 ? 1024 : 2048) || items >= kAttendUnits / 2);
+    g.waves = fits && (g.tiles > 1 || (some && items <= kAttendUnits)) ? 8 : 4;
+    g.steps = steps_of(4);
+    const int at_once = kAttendUnits * attend_resident(fits, g.waves);
+    g.units = units_of(g.blocks, at_once);
     g.round_units = g.blocks <= 8 ? g.units : std::min(g.units, std::max(1, at_once / g.blocks));
     g.round_steps = g.blocks <= 8 ? 0 : g.units * (10 * g.round_units * g.blocks >= 9 * at_once ? 64 : 16);
     return g;
@@ -119,7 +125,7 @@ size_t most_part_floats(const lif_kv_config& c) {
     for (int tiles = 1; tiles <= attend_most_tiles(c.head_dim); tiles *= 2) {
         // fewer rows than the largest call's make fewer blocks, and more workgroups for each: the products below are at their largest in between
         for (int blocks = 1; blocks <= std::min(129, (need + tiles - 1) / tiles); ++blocks) {
-            const size_t groups = (size_t)blocks * units_of(blocks, resident_of(c, tiles));
+            const size_t groups = (size_t)blocks * units_of(blocks, kAttendUnits * attend_resident(lean(c, tiles), tiles > 1 ? 8 : 4));
             if (blocks <= 128) most = std::max(most, 4 * groups * std::min(rows, 16 * tiles) * (pad + 4));
         }
     }
@@ -335,11 +341,11 @@ int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* st
                  (unsigned)(v.page_bytes / c.kv_heads), c.pages, c.max_seqs, c.max_pages, v.log_page, query->batch, query->n_tokens, c.heads,
                  c.kv_heads, share, c.head_dim, query->window, g.units, g.round_units, g.round_steps, g.blocks, g.block_rows, c.scale * kLog2e};
     hipStream_t s = (hipStream_t)stream;
-    using Launch = void (*)(const AttendArgs&, int, hipStream_t);
+    using Launch = void (*)(const AttendArgs&, int, int, hipStream_t);
     static constexpr Launch kLaunch[3][3] = {{launch_attend_f32_1, launch_attend_f32_2, launch_attend_f32_4},
                                              {launch_attend_f16_1, launch_attend_f16_2, launch_attend_f16_4},
                                              {launch_attend_bf16_1, launch_attend_bf16_2, launch_attend_bf16_4}};
-    kLaunch[c.dtype][g.tiles >> 1](a, g.blocks * g.units, s);
+    kLaunch[c.dtype][g.tiles >> 1](a, g.blocks * g.units, g.waves, s);
     return launched();
 }
 

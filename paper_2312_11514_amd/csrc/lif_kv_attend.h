@@ -62,15 +62,15 @@ struct AttendArgs {
 };
 
 // per element type and tiles of 16 rows that a wave takes over the same keys
-void launch_attend_f16_1(const AttendArgs& a, int groups, hipStream_t s);
-void launch_attend_f16_2(const AttendArgs& a, int groups, hipStream_t s);
-void launch_attend_f16_4(const AttendArgs& a, int groups, hipStream_t s);
-void launch_attend_bf16_1(const AttendArgs& a, int groups, hipStream_t s);
-void launch_attend_bf16_2(const AttendArgs& a, int groups, hipStream_t s);
-void launch_attend_bf16_4(const AttendArgs& a, int groups, hipStream_t s);
-void launch_attend_f32_1(const AttendArgs& a, int groups, hipStream_t s);
-void launch_attend_f32_2(const AttendArgs& a, int groups, hipStream_t s);
-void launch_attend_f32_4(const AttendArgs& a, int groups, hipStream_t s);
+void launch_attend_f16_1(const AttendArgs& a, int groups, int waves, hipStream_t s);
+void launch_attend_f16_2(const AttendArgs& a, int groups, int waves, hipStream_t s);
+void launch_attend_f16_4(const AttendArgs& a, int groups, int waves, hipStream_t s);
+void launch_attend_bf16_1(const AttendArgs& a, int groups, int waves, hipStream_t s);
+void launch_attend_bf16_2(const AttendArgs& a, int groups, int waves, hipStream_t s);
+void launch_attend_bf16_4(const AttendArgs& a, int groups, int waves, hipStream_t s);
+void launch_attend_f32_1(const AttendArgs& a, int groups, int waves, hipStream_t s);
+void launch_attend_f32_2(const AttendArgs& a, int groups, int waves, hipStream_t s);
+void launch_attend_f32_4(const AttendArgs& a, int groups, int waves, hipStream_t s);
 
 // head_dim rounded up to what the kernels are compiled for
 __host__ __device__ __forceinline__ int attend_dim_pad(int dim) {
@@ -109,14 +109,8 @@ __device__ __forceinline__ f32x2 load_through2(const float* base, unsigned off, 
 __host__ __device__ constexpr bool attend_lean(int dim_pad, bool exact, int tiles, int bytes) {
     return exact ? dim_pad <= 128 && dim_pad * tiles * bytes <= 512 : dim_pad * tiles <= 128;
 }
-// waves of a workgroup
-__host__ __device__ constexpr int attend_waves(int dim_pad, bool exact, int tiles, int bytes) {
-    return attend_lean(dim_pad, exact, tiles, bytes) && tiles > 1 ? 8 : 4;
-}
 // workgroups that fit a compute unit
-__host__ __device__ constexpr int attend_resident(int dim_pad, bool exact, int tiles, int bytes) {
-    return attend_lean(dim_pad, exact, tiles, bytes) ? 8 / attend_waves(dim_pad, exact, tiles, bytes) : 1;
-}
+__host__ __device__ constexpr int attend_resident(bool lean, int waves) { return lean ? 8 / waves : 1; }
 
 // max and sum over the four lanes of a row (16 and 32 apart); every one of them gets the result
 __device__ __forceinline__ float row_max(float v) {
@@ -214,12 +208,12 @@ __device__ __forceinline__ RowChunk row_chunk(const AttendArgs& a, int stage, in
 }
 
 // ---- the pass over keys and values -------------------------------------------------------------------------------------------
-// grid = groups, block = 256.  HDP: head_dim rounded up (FULL: head_dim itself).  QT: tiles of 16 rows of a wave.
-template <typename T, int HDP, bool FULL, int QT>
-__global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend_lean(HDP, FULL, QT, sizeof(T)) ? 2 : 1) void k_kv_attend(const AttendArgs a) {
+// grid = groups, block = 64 * WAVES.  HDP: head_dim rounded up (FULL: head_dim itself).  QT: tiles of 16 rows of a wave.
+template <typename T, int HDP, bool FULL, int QT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ? 2 : 1) void k_kv_attend(const AttendArgs a) {
     using V = typename Vec<T>::type;
     using M = Mat<T>;
-    constexpr int WAVES = attend_waves(HDP, FULL, QT, sizeof(T)), THREADS = 64 * WAVES;
+    constexpr int THREADS = 64 * WAVES;
     constexpr int N = Vec<T>::N;               // elements of 16 bytes; positions of a lane in the second products
     constexpr int TILES = N / 4;               // K tiles of a stage
     constexpr int STAGE = 4 * N;
@@ -707,6 +701,7 @@ __global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend
                     }
             }
             if (shares > 1) {                    // (one round of rows)
+                const int taken = small_ceil(n_parts, per);              // shares that have parts
                 float* mine = &sums[0][0][0] + (team < TEAMS ? team : 0) * ROW;
                 const bool here = team < TEAMS && r0 < rows_here;
                 __syncthreads();
@@ -721,12 +716,12 @@ __global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend
                 if (here && share == 0) {
                     float most = m;
 #pragma unroll 4
-                    for (int k = 1; k < shares; ++k) most = fmaxf(most, mine[(k << log_once) * ROW + HDP]);
+                    for (int k = 1; k < taken; ++k) most = fmaxf(most, mine[(k << log_once) * ROW + HDP]);
                     const float f0 = rescale(m, most, scale_log2);
                     l *= f0;
                     y *= f0;
 #pragma unroll 4
-                    for (int k = 1; k < shares; ++k) {
+                    for (int k = 1; k < taken; ++k) {
                         const float* theirs = mine + (k << log_once) * ROW;
                         const float f = rescale(theirs[HDP], most, scale_log2);
                         l += theirs[HDP + 1] * f;
@@ -744,25 +739,34 @@ __global__ __launch_bounds__(64 * attend_waves(HDP, FULL, QT, sizeof(T)), attend
     }
 }
 
+template <typename T, int HDP, bool FULL, int QT>
+void launch_attend_waves(const AttendArgs& a, int groups, int waves, hipStream_t s) {
+    constexpr bool lean = attend_lean(HDP, FULL, QT, sizeof(T));
+    if constexpr (lean)
+        if (waves == 8) hipLaunchKernelGGL((k_kv_attend<T, HDP, FULL, QT, 8>), dim3(groups), dim3(512), 0, s, a);
+    if constexpr (!lean || QT == 1)
+        if (waves == 4) hipLaunchKernelGGL((k_kv_attend<T, HDP, FULL, QT, 4>), dim3(groups), dim3(256), 0, s, a);
+}
+
 template <typename T, int HDP, int QT>
-void launch_attend(const AttendArgs& a, int groups, hipStream_t s) {
+void launch_attend(const AttendArgs& a, int groups, int waves, hipStream_t s) {
     if (a.dim == HDP) {
-        hipLaunchKernelGGL((k_kv_attend<T, HDP, true, QT>), dim3(groups), dim3(64 * attend_waves(HDP, true, QT, sizeof(T))), 0, s, a);
+        launch_attend_waves<T, HDP, true, QT>(a, groups, waves, s);
     } else if constexpr (HDP != 80 && QT <= (HDP == 256 ? 1 : 2)) {
-        hipLaunchKernelGGL((k_kv_attend<T, HDP, false, QT>), dim3(groups), dim3(64 * attend_waves(HDP, false, QT, sizeof(T))), 0, s, a);
+        launch_attend_waves<T, HDP, false, QT>(a, groups, waves, s);
     }
 }
 
 template <typename T, int QT>
-void launch_attend_tiles(const AttendArgs& a, int groups, hipStream_t s) {
+void launch_attend_tiles(const AttendArgs& a, int groups, int waves, hipStream_t s) {
     switch (attend_dim_pad(a.dim)) {
-        case 32: return launch_attend<T, 32, QT>(a, groups, s);
-        case 64: return launch_attend<T, 64, QT>(a, groups, s);
-        case 80: return launch_attend<T, 80, QT>(a, groups, s);
-        case 96: return launch_attend<T, 96, QT>(a, groups, s);
-        case 128: return launch_attend<T, 128, QT>(a, groups, s);
+        case 32: return launch_attend<T, 32, QT>(a, groups, waves, s);
+        case 64: return launch_attend<T, 64, QT>(a, groups, waves, s);
+        case 80: return launch_attend<T, 80, QT>(a, groups, waves, s);
+        case 96: return launch_attend<T, 96, QT>(a, groups, waves, s);
+        case 128: return launch_attend<T, 128, QT>(a, groups, waves, s);
         default:
-            if constexpr (QT <= 2) launch_attend<T, 256, QT>(a, groups, s);
+            if constexpr (QT <= 2) launch_attend<T, 256, QT>(a, groups, waves, s);
     }
 }
 
