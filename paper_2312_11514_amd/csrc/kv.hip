@@ -106,11 +106,13 @@ Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) 
     g.blocks = (need + g.tiles - 1) / g.tiles;
     g.block_rows = std::min(rows, 16 * g.tiles);
     // Eight waves share a part, or four: the larger parts are fewer to add, the smaller ones fill the chip sooner, and two workgroups of them hide
-    // each other's beginnings and ends.  Larger ones pay where a part has some rows, and where no workgroup goes through more than one item (4 tokens of
-    // 4 sequences of up to 4000, 32 heads on 8: 20.8 us with four, 14.2 with eight; 64 sequences of one: 144.5 and 149.3).
+    // each other's beginnings and ends.  Larger ones pay where a part has some rows, and where workgroups go through parts of one item and few are left
+    // over (4 tokens of 4 sequences of up to 4000, 32 heads on 8: 20.8 us with four, 14.2 with eight; one of 32 sequences of 2000, 71 heads on one,
+    // 160 items: 15.1 and 18.4; one of 64 sequences, 512 items: 144.5 and 149.3).
     const long long items = (long long)batch * c.kv_heads * g.blocks;
-    const bool fits = lean(c, g.tiles), some = g.block_rows >= 4 && (positions > (g.block_rows >= 16 ? 1024 : 2048) || items >= kAttendUnits / 2);
-    g.waves = fits && (g.tiles > 1 || (some && items <= kAttendUnits)) ? 8 : 4;
+    const bool few = items <= kAttendUnits / 2 || (items <= kAttendUnits && 8 * items > 7 * kAttendUnits);
+    const bool fits = lean(c, g.tiles), some = g.block_rows >= 4 && (positions > (g.block_rows >= 16 ? 768 : 2048) || items >= kAttendUnits / 2);
+    g.waves = fits && (g.tiles > 1 || (some && few)) ? 8 : 4;
     g.steps = steps_of(4);
     const int at_once = kAttendUnits * attend_resident(fits, g.waves);
     g.units = units_of(g.blocks, at_once);
