@@ -9,8 +9,10 @@
 // a head, a power of two of lanes a head, so the sums of a norm are a few lane exchanges; the other half of a pair (half layout) is a second
 // 16-byte load of the same line and not an exchange, since it is normalised with other weights anyway.
 // Values: the cache keeps N consecutive tokens of a dimension in 16 bytes.  Written token by token, from workgroups on different XCDs,
-// those are N writes of a part of a line each; a workgroup takes the N tokens of a piece together and writes it whole where it has all of them
-// (32 prompts of up to 64 tokens, 64 heads of 64: 66.0 us before, with angles per lane).
+// those are N writes of a part of a line each; a workgroup takes the N tokens of a piece together and writes it whole where it has all of them.
+// What it measured: one token of 32 heads of 128 3.1 us (6.5 as called from Python, which is what a launch costs there); 32 prompts of up to 64
+// tokens, 64 heads of 64, bf16, layer norms, half of a head turned: 58 MB in 19.4 us, 3.0 TB/s of the 4.7 a large copy reaches (66 us with values
+// token by token and angles per lane).
 #pragma once
 
 #include "lif_kv.h"

@@ -11,13 +11,22 @@
 // Which position a row of a K tile stands for is free: tile a takes position N g + 4 a + i as its row 4 g + i, so that what a lane gets
 // out of the first products is what it has to hand into the second.  The weights never leave its registers; keys and values come
 // straight from their pages, 16 bytes a lane, in the order the products take them (values are stored with N consecutive positions
-// together for that), and no LDS is used before the end.  With one row in use of 16 the products cost a fifteenth of the
-// time that the bytes take, so one token of an unshared head takes the same path.
+// together for that).  With one row in use of 16 the products cost a fifteenth of the time that the bytes take, so one token of an
+// unshared head takes the same path.
+//
+// Rounding: scores, maxima, sums and outputs are fp32; a weight is rounded to E for the second products, which take nothing wider at their
+// rate (relative error of an output 2.3e-4 in fp16, 2e-3 in bf16, half of it the rounding of the output itself; fp32 4e-7).
 //
 // What bounds it: reading keys and values once, and for short sequences the chain slot -> length -> table entry -> keys -> sums.  Sequences
 // differ in length, and the host does not know them: the steps of all items, one after the other, are dealt to a fixed number of
 // workgroups in equal contiguous runs, each of which works out its own from the lengths.  A run that is a whole item writes its
 // output; of an item's parts every workgroup leaves the maximum, the sum and the unscaled output behind, and the last one to do so adds them.
+// What that leaves: one sequence of 200003, 32 heads of 128 on 8, bf16: 819 MB in 144 us, 5.7 TB/s (a plain streaming read reaches 6.3); 64 of up to
+// 8192, fp16: 794 MB in 146 us; 16 of up to 6001 with 5 tokens each: 120 MB in 36.5 us; one of 2048, 32 heads: 33.6 MB in 11.6 us, where a plain
+// read in a launch of its own takes 7.7; one of 77: 5.7 us.  Of those 11.6 the launch has 1.8, lengths and first table entries 2.5, the merge of the
+// waves 0.8, the count of parts 0.7, adding the parts 2.
+// Many rows are bound by the matrix cores and the arithmetic on scores between them, with one or two waves a SIMD: 20 tokens of 64 sequences of 8000, 71
+// heads of 64 on one, 186 GFLOP in 390 us, 0.47 PFLOP/s (a library's large product reaches 1.1).
 #pragma once
 
 #include "lif_kv.h"
@@ -27,8 +36,8 @@ namespace lif {
 
 constexpr int kAttendUnits = 256;        // compute units
 constexpr int kAttendMost = 2048;        // workgroups of a call that may leave parts
-constexpr int kAttendFan = 16;           // parts that one workgroup adds at most; of more, such sums are added again
-constexpr int kAttendAsk = 8;            // ... and asks for at once
+constexpr int kAttendFan = 16;           // parts that one workgroup adds at most; of more, such sums are added again (4: one stream of 2048 12.4 -> 14.8 us)
+constexpr int kAttendAsk = 8;            // ... and asks for at once (16: no difference beyond 3 %, in both directions)
 constexpr float kLog2e = 1.44269504088896340736f;
 // added to the exponent of every weight, and taken out of the sums: fp16 has no exponents below 2^-24, and of a long sequence many small
 // weights count; none can pass 2^15
@@ -138,8 +147,8 @@ __device__ __forceinline__ float rescale(float m, float most, float scale_log2) 
 // row with nothing to do has one step (it writes zeros).  Its items, one per key head, have the same.  The steps of all items, by
 // batch row, key head and position, are dealt to the `units` workgroups of a block of rows in runs:
 //   by items    every item in as many equal parts as it takes for none to be longer than the even share (or an eighth more), if that needs
-//               no more workgroups than there are: a workgroup then begins and ends one part.  16 sequences of 15 steps, 8 key heads, 512
-//               workgroups: 29.5 us against 31.1 with runs that go on into the next item
+//               no more workgroups than there are: a workgroup then begins and ends one part.  16 sequences of 15 steps of 128, 8 key
+//               heads, 512 workgroups: 29.5 us against 31.1 with runs that go on into the next item
 //   evenly      else: runs of equal length across the items (many items, or few steps for each workgroup)
 // Every wave works this out by itself, 64 batch rows at a time, one to a lane: for up to 64 that is no LDS and no barrier.
 struct RowRange {
