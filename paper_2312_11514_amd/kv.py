@@ -162,7 +162,9 @@ class KVCache:
         out_stride = self._rows(q_out, of_q, "q_out")
         qw = qb = kw = kb = 0
         if norm is not None:
-            qw, qb, kw, kb = (self._norm(t, what) for t, what in zip(norm, ("q weight", "q bias", "k weight", "k bias")))
+            qw, qb, kw, kb = norm
+            qw, qb = self._norm(qw, "q weight"), self._norm(qb, "q bias")
+            kw, kb = self._norm(kw, "k weight"), self._norm(kb, "k bias")
         _ROWS.pack_into(self._rows_arg, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), q_stride, k_stride, v_stride, out_stride,
                         qw, qb, kw, kb, self._ints(positions, batch * tokens, "positions") if positions is not None else 0,
                         self._slots(slots, batch), batch, tokens)
