@@ -26,7 +26,7 @@
 // read in a launch of its own takes 7.7; one of 77: 5.7 us.  Of those 11.6 the launch has 1.8, lengths and first table entries 2.5, the merge of the
 // waves 0.8, the count of parts 0.7, adding the parts 2.
 // Many rows are bound by the matrix cores and the arithmetic on scores between them, with one or two waves a SIMD: 20 tokens of 64 sequences of 8000, 71
-// heads of 64 on one, 186 GFLOP in 390 us, 0.47 PFLOP/s (a library's large product reaches 1.1).
+// heads of 64 on one, 186 GFLOP in 355 us, 0.52 PFLOP/s (a library's large product reaches 1.1).
 #pragma once
 
 #include "lif_kv.h"
@@ -39,9 +39,13 @@ constexpr int kAttendMost = 2048;        // workgroups of a call that may leave 
 constexpr int kAttendFan = 16;           // parts that one workgroup adds at most; of more, such sums are added again (4: one stream of 2048 12.4 -> 14.8 us)
 constexpr int kAttendAsk = 8;            // ... and asks for at once (16: no difference beyond 3 %, in both directions)
 constexpr float kLog2e = 1.44269504088896340736f;
+// Weights are relative to a reference that follows the maximum of their row.  Every change of it multiplies all sums, and a maximum creeps up for most of a
+// sequence: with tiles of 64 rows, whose time is arithmetic, it follows only once the maximum is more than this far ahead (as an exponent of two; 60 tokens
+// of 64 sequences of 8000, 71 heads on one: 1050 us instead of 1195).  Otherwise at once: the largest weight is then a power of two, and not rounded.
+constexpr float attend_slack(int tiles) { return tiles == 4 ? 4.f : 0.f; }
 // added to the exponent of every weight, and taken out of the sums: fp16 has no exponents below 2^-24, and of a long sequence many small
-// weights count; none can pass 2^15
-constexpr float kWeightBias = 15.f;
+// weights count; none passes 2^15 with the slack
+constexpr float attend_bias(int tiles) { return 15.f - attend_slack(tiles); }
 
 struct AttendArgs {
     const char* q;
@@ -237,6 +241,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
     // What a wave needs of its rows only now and then is not kept in registers: their place in `out` (a row, negative for padding, and the
     // head), of the first segment and of later ones; first position, last new token, and which of those they see.  Queries of several
     // tiles neither: 128 dimensions by 32 rows fit 256 registers then, and two workgroups a compute unit.
+    // (64 rows by 128 dimensions have a wave a SIMD either way, and are slower so: 77 -> 80 us for 60 tokens of 4 sequences of 8000.)
     constexpr bool QLDS = QT > 1 && (attend_lean(HDP, FULL, QT, sizeof(T)) || (HDP == 256 && CH <= 8));
     __shared__ int2 out_at[2][16 * QT], sees_at[WAVES][16 * QT];
     __shared__ unsigned long long seen_at[WAVES][16 * QT];
@@ -291,7 +296,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
     bool first_segment = true;
     bool arrived = false;                      // the first segment's part was the last of its run to be left
     int joins = 0;                             // bits of the segments that are parts
-    const float scale_log2 = a.scale_log2;
+    const float scale_log2 = a.scale_log2, slack = fminf(attend_slack(QT) / scale_log2, 1e30f);
     const int rows_here = min(16 * QT, rows - row0);
     // four dimensions of a row of the output
     auto finish = [&](int seg, int r0, int d, f32x4 v, float m, float total) {
@@ -306,7 +311,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
             for (int j = 0; j < 4; ++j) y[j] = none ? (T)0.f : (T)(v[j] * inv);
             *reinterpret_cast<T4*>((T*)a.out + out_row * a.out_stride + (unsigned)(to.y * dim + d)) = y;
         }
-        if (a.lse && d == 0) a.lse[out_row * a.heads + to.y] = none ? -INFINITY : (m * scale_log2 - kWeightBias + log2f(total)) / kLog2e;
+        if (a.lse && d == 0) a.lse[out_row * a.heads + to.y] = none ? -INFINITY : (m * scale_log2 - attend_bias(QT) + log2f(total)) / kLog2e;
     };
     char* parts = reinterpret_cast<char*>(a.parts);
     const int level2 = 2 * (int)gridDim.x;     // places of parts; those of runs are behind them
@@ -384,7 +389,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
             }
         }
         f32x4 o[QT][DT];
-        float top[QT], ref[QT], sum[QT];       // running maximum, the same or 0 where there is none, sum of the lane's weights
+        float top[QT], ref[QT], sum[QT];       // reference (-inf: nothing seen), the same or 0 there, sum of the lane's weights
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             top[t] = -INFINITY;
@@ -515,7 +520,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
                     float most = x[t][0];
 #pragma unroll
                     for (int e = 1; e < N; ++e) most = fmaxf(most, x[t][e]);
-                    if (__any(most > top[t])) {
+                    if (__any(most > (attend_slack(QT) > 0.f ? top[t] + slack : top[t]))) {
                         most = fmaxf(row_max(most), top[t]);
                         const float scale = rescale(top[t], most, scale_log2);
                         ref[t] = most == -INFINITY ? 0.f : most;
@@ -526,7 +531,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
                     }
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e] - ref[t], scale_log2, kWeightBias));
+                        const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e] - ref[t], scale_log2, attend_bias(QT)));
                         sum[t] += weight;
                         w[t][e] = (T)weight;
                     }

@@ -141,21 +141,22 @@ def test_one_long_sequence_beside_short_ones(dtype, heads, kv_heads, head_dim):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
-def test_many_small_weights_beside_a_large_one(dtype):
+@pytest.mark.parametrize("heads,max_pages,size", [(1, 0, 1.6), (1, 0, 0.8), (70, 1 << 18, 1.6), (70, 1 << 18, 0.8)])
+def test_many_small_weights_beside_a_large_one(dtype, heads, max_pages, size):
     """One key towers above 6000 others, which together still count: their weights are below what fp16 holds without a bias."""
     n, d = 6000, 64
 
     def change(kv, rows, q):
         keys, values = rows[0]
         keys *= 0.05
-        keys[0, 17] = q[0, 0, 0].double().cpu().numpy() * 1.6
+        keys[0, 17] = q[0, 0, 0].double().cpu().numpy() * size
         keys[:] = torch.from_numpy(keys).to(DTYPES[dtype]).double().numpy()
         values[0, :] = np.abs(values[0])
         from tests.kv_harness import put
         pages = kv.table[0, :-(-n // 16)].tolist()
         put(kv, 1, pages, torch.from_numpy(keys).to(DTYPES[dtype]), torch.from_numpy(values).to(DTYPES[dtype]))
 
-    _run([n], [1], heads=1, kv_heads=1, head_dim=d, page=16, dtype=dtype, tokens=1, change=change, peaked=1.3)
+    _run([n], [1], heads=heads, kv_heads=1, head_dim=d, page=16, dtype=dtype, tokens=1, change=change, peaked=1.3, max_pages=max_pages)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
