@@ -240,7 +240,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
     __shared__ float sums[WAVES][16][PITCH];
     // What a wave needs of its rows only now and then is not kept in registers: their place in `out` (a row, negative for padding, and the
     // head), of the first segment and of later ones; first position, last new token, and which of those they see.  Queries of several
-    // tiles neither: 128 dimensions by 32 rows fit 256 registers then, and two workgroups a compute unit.
+    // tiles neither: 128 dimensions by 32 rows fit 256 registers then, and eight waves a compute unit.
     // (64 rows by 128 dimensions have a wave a SIMD either way, and are slower so: 77 -> 80 us for 60 tokens of 4 sequences of 8000.)
     constexpr bool QLDS = QT > 1 && (attend_lean(HDP, FULL, QT, sizeof(T)) || (HDP == 256 && CH <= 8));
     __shared__ int2 out_at[2][16 * QT], sees_at[WAVES][16 * QT];
