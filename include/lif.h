@@ -543,8 +543,8 @@ int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* st
 
 /*
  * Performance hint for lif_kv_attend: cached tokens of a sequence as a rule; 0 (the default): as many as a table row holds.  Decides in
- * which blocks the rows of a call are taken where there are more than 16 of a key head, and with that the order of their sums: results
- * may differ in the last bits.
+ * which blocks rows and positions are taken where a key head has 4 rows or more (tokens times the query heads that share it), and with that
+ * the order of their sums: results may differ in the last bits.
  */
 int lif_kv_set_expected_tokens(lif_kv* kv, int32_t tokens);
 

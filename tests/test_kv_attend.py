@@ -28,9 +28,10 @@ def _check(out, lse, ref, dtype, n, d, tag):
 
 
 def _run(lengths, fresh, *, heads, kv_heads, head_dim, page, dtype, tokens, window=0, starts=None, tree=None, seed=1, slots=None, peaked=1.0,
-         max_seqs=None, max_pages=0, change=None, stride=0):
+         max_seqs=None, max_pages=0, change=None, stride=0, expected=0):
     kv, rows = build(lengths, fresh, kv_heads=kv_heads, head_dim=head_dim, page=page, dtype=dtype, seed=seed, heads=heads, max_tokens=tokens,
                      slots=slots, max_seqs=max_seqs, max_pages=max_pages)
+    kv.set_expected_tokens(expected)
     rng = np.random.default_rng(seed + 1)
     b = len(lengths)
     wide = torch.from_numpy(peaked * rng.standard_normal((b, tokens, heads * head_dim + stride), dtype=np.float32)).to(DTYPES[dtype]).cuda()
@@ -122,6 +123,13 @@ def test_rows_together(dtype, heads, kv_heads, head_dim, tokens):
 def test_many_blocks_of_rows(dtype, heads, kv_heads, head_dim, tokens, max_pages):
     _run([tokens + 130, 0, tokens, 1200], [tokens, 0, tokens // 2, tokens], heads=heads, kv_heads=kv_heads, head_dim=head_dim, page=16, dtype=dtype,
          tokens=tokens, max_pages=max_pages)
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,head_dim,tokens", [("f16", 8, 2, 128, 1), ("bf16", 8, 2, 128, 5), ("f16", 71, 1, 64, 1), ("f32", 6, 1, 80, 12)])
+@pytest.mark.parametrize("expected", [1, 100, 3000, 1 << 30])
+def test_hints_that_do_not_fit(dtype, heads, kv_heads, head_dim, tokens, expected):
+    _run([5000, 40, 0, 700], [tokens, tokens, 0, tokens], heads=heads, kv_heads=kv_heads, head_dim=head_dim, page=32, dtype=dtype, tokens=tokens,
+         expected=expected, max_pages=1 << 16)
 
 
 @pytest.mark.parametrize("batch", [1, 70, 300, 1024])
