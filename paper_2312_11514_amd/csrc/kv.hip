@@ -73,6 +73,9 @@ struct KvLayout {
 // A workgroup reads the keys once for its block, so blocks are as large as registers allow; where there are so few that all their steps
 // run at once, or nearly, the time is that of one workgroup with its parts, and smaller ones are faster (16 tokens of 2 sequences of 4000, 32
 // heads of 128 on 8: 22.2 us in blocks of 16 rows, 45.2 in ones of 64).
+// Tables are wider than their sequences as a rule, so blocks can come out too large: ones of 64 rows that leave a compute unit four waves only are taken for
+// 128 rows and more (16 tokens of one sequence of 1000 in a table for 32768: 15.4 us in blocks of 32 rows, 28.3 in ones of 64; 16 sequences of 4000: 64.1
+// and 61.7).
 struct Tiling {
     int tiles, waves, blocks, block_rows, units, round_units, round_steps;
     long long steps;                     // of a block's items, at most
@@ -99,7 +102,7 @@ Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) 
         return (long long)batch * c.kv_heads * ((positions + step - 1) / step + 1);
     };
     Tiling g;
-    g.tiles = std::min(attend_most_tiles(c.head_dim), need <= (pad > 128 ? 2 : 1) ? 1 : need <= 2 ? 2 : 4);
+    g.tiles = std::min(attend_most_tiles(c.head_dim), need <= (pad > 128 ? 2 : 1) ? 1 : need <= 2 || (need >= 4 && need < 8 && !lean(c, 4)) ? 2 : 4);
     while (g.tiles > 1 && steps_of(4) * ((need + g.tiles / 2 - 1) / (g.tiles / 2)) <= kAttendFew) g.tiles /= 2;
     // of several blocks the last one may be mostly empty: 71 rows, 8 x 16000 positions, heads of 64: 33.5 us in two blocks of 64
     while (g.tiles > 1 && need > g.tiles && 4 * ((need + g.tiles - 1) / g.tiles * g.tiles) > 5 * need) g.tiles /= 2;

@@ -100,17 +100,20 @@ def test_many_tokens(dtype, heads, kv_heads, head_dim, tokens):
          tokens=tokens)
 
 
-# How many rows a workgroup takes together goes by the rows and by what a full table would make of steps: the same calls with wide tables.
+# How many rows a workgroup takes together goes by the rows and the steps: by the hint where there is one, else by what a full table would make of
+# them.  Wide tables with a hint of many tokens, and without.
 LARGE = [("f16", 8, 1, 128), ("bf16", 8, 2, 128), ("f32", 8, 1, 128), ("f16", 9, 1, 64), ("f32", 8, 2, 64), ("bf16", 6, 1, 80), ("f32", 9, 1, 80),
          ("f16", 8, 1, 96), ("f32", 8, 1, 96), ("bf16", 8, 1, 32), ("f32", 8, 1, 32), ("f16", 8, 1, 256), ("f32", 8, 1, 256), ("bf16", 8, 1, 112),
          ("f32", 9, 1, 40), ("f16", 8, 1, 200), ("f16", 9, 1, 24)]
 
 
 @pytest.mark.parametrize("dtype,heads,kv_heads,head_dim", LARGE)
-@pytest.mark.parametrize("tokens", [4, 11])
-def test_rows_together(dtype, heads, kv_heads, head_dim, tokens):
+@pytest.mark.parametrize("tokens", [4, 6, 11, 16])
+@pytest.mark.parametrize("expected", [1 << 21, 0])
+def test_rows_together(dtype, heads, kv_heads, head_dim, tokens, expected):
     lengths, fresh = [tokens, 700, 0, 150, 33, 2100], [tokens, tokens, 0, tokens - 1, 2, tokens]
-    kw = dict(heads=heads, kv_heads=kv_heads, head_dim=head_dim, page=16, dtype=dtype, tokens=tokens, max_pages=1 << 17)
+    kw = dict(heads=heads, kv_heads=kv_heads, head_dim=head_dim, page=16, dtype=dtype, tokens=tokens, max_pages=1 << 17,
+              expected=expected)
     _run(lengths, fresh, **kw)
     rng = np.random.default_rng(tokens)
     tree = [[int(w) | 1 << j if j else 1 for j, w in enumerate(rng.integers(0, 1 << tokens, tokens))] for _ in lengths]
@@ -119,10 +122,19 @@ def test_rows_together(dtype, heads, kv_heads, head_dim, tokens):
 
 @pytest.mark.parametrize("dtype,heads,kv_heads,head_dim,tokens", [("f16", 71, 1, 64, 20), ("f32", 40, 1, 32, 30), ("bf16", 40, 2, 128, 40),
                                                                   ("bf16", 71, 1, 64, 256)])
-@pytest.mark.parametrize("max_pages", [0, 1 << 17])
-def test_many_blocks_of_rows(dtype, heads, kv_heads, head_dim, tokens, max_pages):
+@pytest.mark.parametrize("max_pages,expected", [(0, 0), (1 << 17, 0), (1 << 17, 1 << 21)])
+def test_many_blocks_of_rows(dtype, heads, kv_heads, head_dim, tokens, max_pages, expected):
     _run([tokens + 130, 0, tokens, 1200], [tokens, 0, tokens // 2, tokens], heads=heads, kv_heads=kv_heads, head_dim=head_dim, page=16, dtype=dtype,
-         tokens=tokens, max_pages=max_pages)
+         tokens=tokens, max_pages=max_pages, expected=expected)
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,head_dim,tokens", [("f16", 8, 4, 128, 9), ("bf16", 24, 4, 64, 3), ("f32", 8, 4, 64, 9)])
+def test_rows_together_by_the_lengths(dtype, heads, kv_heads, head_dim, tokens):
+    """A batch with many steps and no hint; two long sequences among short ones"""
+    rng = np.random.default_rng(5)
+    lengths = [int(n) for n in rng.integers(0, 40, 700)]
+    lengths[100], lengths[601] = 9000, 4001
+    _run(lengths, [min(tokens, n) for n in lengths], heads=heads, kv_heads=kv_heads, head_dim=head_dim, page=16, dtype=dtype, tokens=tokens, max_pages=4096)
 
 
 @pytest.mark.parametrize("dtype,heads,kv_heads,head_dim,tokens", [("f16", 8, 2, 128, 1), ("bf16", 8, 2, 128, 5), ("f16", 71, 1, 64, 1), ("f32", 6, 1, 80, 12)])
@@ -164,7 +176,8 @@ def test_many_small_weights_beside_a_large_one(dtype, heads, max_pages, size):
         pages = kv.table[0, :-(-n // 16)].tolist()
         put(kv, 1, pages, torch.from_numpy(keys).to(DTYPES[dtype]), torch.from_numpy(values).to(DTYPES[dtype]))
 
-    _run([n], [1], heads=heads, kv_heads=1, head_dim=d, page=16, dtype=dtype, tokens=1, change=change, peaked=1.3, max_pages=max_pages)
+    _run([n], [1], heads=heads, kv_heads=1, head_dim=d, page=16, dtype=dtype, tokens=1, change=change, peaked=1.3, max_pages=max_pages,
+         expected=max_pages * 16)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
@@ -191,6 +204,7 @@ def test_what_a_token_does_not_see_never_reaches_it(dtype, bad, max_pages):
         for starts, window in (([13], 0), (None, 24)):
             for t in (None, tree):
                 kv, rows = build([40], [5], kv_heads=kv_heads, head_dim=d, page=16, dtype=dtype, seed=4, heads=heads, max_pages=max_pages)
+                kv.set_expected_tokens(max_pages * 16)
                 change(kv, rows, None)
                 q = torch.randn(1, 5, heads, d, device="cuda").to(DTYPES[dtype])
                 out, lse = torch.empty_like(q), torch.empty(1, 5, heads, device="cuda")
@@ -213,6 +227,7 @@ def test_a_value_that_is_not_finite_reaches_the_rows_that_see_it():
     """... with its sign, and only its own dimension"""
     for dtype, heads, max_pages in (("f16", 2, 0), ("f32", 2, 0), ("f16", 9, 1 << 18), ("f32", 17, 1 << 18)):
         kv, rows = build([40], [3], kv_heads=1, head_dim=64, page=16, dtype=dtype, seed=4, heads=heads, max_pages=max_pages)
+        kv.set_expected_tokens(max_pages * 16)
         page, e = int(kv.table[0, 2]), kv.v.shape[5]
         j = 38                                                     # the second of three new tokens
         kv.v[1, page, 0, j % 16 // e, 11, j % 16 % e] = -float("inf")
