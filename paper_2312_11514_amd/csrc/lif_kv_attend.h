@@ -536,9 +536,9 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
                         w[t][e] = (T)weight;
                     }
                 }
-                // A weight of zero does not keep a value out that is not finite.  Where rows see different positions of a stage, such values are
-                // taken out of the products and added to the rows that see them.
-                if (edge && r.fresh > 1) {
+                // A weight of zero does not keep a value out that is not finite.  Where rows see different positions of a stage, or none of them
+                // sees one (by a tree, a single new token its own), such values are taken out of the products and added to the rows that see them.
+                if (edge && (r.fresh > 1 || a.tree)) {
                     bool finite = true;
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
