@@ -43,9 +43,6 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // sequence: with tiles of 64 rows, whose time is arithmetic, it follows only once the maximum is more than this far ahead (as an exponent of two; 60 tokens
 // of 64 sequences of 8000, 71 heads on one: 1050 us instead of 1195).  Otherwise at once: the largest weight is then a power of two, and not rounded.
 constexpr float attend_slack(int tiles) { return tiles == 4 ? 4.f : 0.f; }
-// added to the exponent of every weight, and taken out of the sums: fp16 has no exponents below 2^-24, and of a long sequence many small
-// weights count; none passes 2^15 with the slack
-constexpr float attend_bias(int tiles) { return 15.f - attend_slack(tiles); }
 
 struct AttendArgs {
     const char* q;
@@ -98,16 +95,30 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 template <typename T> struct Mat;
 template <> struct Mat<_Float16> {
     static constexpr int kParts = 1;
+    static constexpr bool kFewExponents = true;
     static __device__ __forceinline__ f32x4 mul(f16x8 a, f16x8 b, f32x4 c, int) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mat<__bf16> {
     static constexpr int kParts = 1;
+    static constexpr bool kFewExponents = false;
     static __device__ __forceinline__ f32x4 mul(bf16x8 a, bf16x8 b, f32x4 c, int) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mat<float> {
     static constexpr int kParts = 4;
+    static constexpr bool kFewExponents = false;
     static __device__ __forceinline__ f32x4 mul(f32x4 a, f32x4 b, f32x4 c, int e) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0); }
 };
+
+// Added to the exponent of every weight, and taken out of the sums.  fp16 has no exponents below 2^-24, and of a long sequence many small weights count:
+// as large as it goes, none passes 2^15 with the slack.  bf16 and fp32 have the exponents, but values as large as what the sums are held in: -k for more
+// than 2^(k-1) positions, up to 2^k, so that weights add up to one at most and sums stay below the largest value (with 15 as in fp16 a single
+// value above 1.04e34 came out infinite, and 200000 alike above 5e28).
+template <typename T>
+__device__ __forceinline__ int attend_bias(int tiles, int positions) {
+    const int slack = (int)attend_slack(tiles);
+    if constexpr (Mat<T>::kFewExponents) return 15 - slack;
+    else return (positions > 1 ? __builtin_clz(positions - 1) - 32 : 0) - slack;
+}
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
@@ -246,7 +257,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
     __shared__ int2 out_at[2][16 * QT], sees_at[WAVES][16 * QT];
     __shared__ unsigned long long seen_at[WAVES][16 * QT];
     __shared__ V q_at[QLDS ? WAVES : 1][QLDS ? QT : 1][QLDS ? CH : 1][64];
-    __shared__ int4 join_of[WAVES][2];         // parts to add behind the loop: w0, count, begins_before
+    __shared__ int4 join_of[WAVES][2];         // parts to add behind the loop: w0, count, begins_before, bias
     const int tid = threadIdx.x, lane = tid & 63, wv = whole_wave(tid >> 6), n = lane & 15, g = lane >> 4, dim = FULL ? HDP : a.dim;
     constexpr int STEP = STAGE * WAVES;
     const int error = *a.error;
@@ -299,7 +310,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
     const float scale_log2 = a.scale_log2, slack = fminf(attend_slack(QT) / scale_log2, 1e30f);
     const int rows_here = min(16 * QT, rows - row0);
     // four dimensions of a row of the output
-    auto finish = [&](int seg, int r0, int d, f32x4 v, float m, float total) {
+    auto finish = [&](int seg, int r0, int d, f32x4 v, float m, float total, float bias) {
         const int2 to = out_at[seg][r0];
         const size_t out_row = (unsigned)to.x & 0x7fffffffu;
         const bool none = to.x < 0 || total == 0.f;
@@ -311,7 +322,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
             for (int j = 0; j < 4; ++j) y[j] = none ? (T)0.f : (T)(v[j] * inv);
             *reinterpret_cast<T4*>((T*)a.out + out_row * a.out_stride + (unsigned)(to.y * dim + d)) = y;
         }
-        if (a.lse && d == 0) a.lse[out_row * a.heads + to.y] = none ? -INFINITY : (m * scale_log2 - attend_bias(QT) + log2f(total)) / kLog2e;
+        if (a.lse && d == 0) a.lse[out_row * a.heads + to.y] = none ? -INFINITY : (m * scale_log2 - bias + log2f(total)) / kLog2e;
     };
     char* parts = reinterpret_cast<char*>(a.parts);
     const int level2 = 2 * (int)gridDim.x;     // places of parts; those of runs are behind them
@@ -356,6 +367,8 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
         const int i = rc.first + il;
         const RowRange r = of_lane(rc.range, il);
         const int base = r.n - r.fresh, low_all = low_of(r, 0, a.window);
+        const int bias_exp = attend_bias<T>(QT, r.n - low_all);
+        const float bias = (float)bias_exp;
 
         const int seg = first_segment ? 0 : 1;
         if (!first_segment) lds_barrier();     // (the last segment's readers are done)
@@ -531,7 +544,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
                     }
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e] - ref[t], scale_log2, attend_bias(QT)));
+                        const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][e] - ref[t], scale_log2, bias));
                         sum[t] += weight;
                         w[t][e] = (T)weight;
                     }
@@ -621,7 +634,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
                         y += wy[e] * f;
                     }
                     if (whole) {
-                        finish(seg, r0, half * COLS + d, y, m, l);
+                        finish(seg, r0, half * COLS + d, y, m, l, bias);
                     } else {
                         store_through(parts, part_at(part, r0) + (half * COLS + d) * 4, a.part_bytes, y);
                         if (half == 0 && d == 0) store_through(parts, part_at(part, r0) + HDP * 4, a.part_bytes, f32x4{m, l, 0.f, 0.f});
@@ -632,7 +645,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
 
         if (!whole) {
             joins |= 1 << seg;
-            if (lane == 0) join_of[wv][seg] = make_int4(w0, count, begins_before, 0);
+            if (lane == 0) join_of[wv][seg] = make_int4(w0, count, begins_before, bias_exp);
         }
         if (by_items) break;
         at += s1 - s0;
@@ -653,6 +666,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
         const int4 of = join_of[wv][seg];
         const int w0 = whole_wave(of.x), count = whole_wave(of.y), runs = (count + kAttendFan - 1) / kAttendFan;
         const bool begins_before = whole_wave(of.z);
+        const float bias = (float)(M::kFewExponents ? attend_bias<T>(QT, 0) : whole_wave(of.w));
         int level = 0, from = (unit - w0) / kAttendFan * kAttendFan, stride = 1, n_parts = min(kAttendFan, count - from);
         while (true) {
             if (!arrived && !arrive(level, part_of(w0, begins_before, from), n_parts)) break;
@@ -668,7 +682,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
             const int units = ((rows_here + (1 << log_once) - 1) >> log_once) * per;
             auto leave = [&](int r0, f32x4 y, float m, float l) {
                 if (done) {
-                    finish(seg, r0, d, y, m, l);
+                    finish(seg, r0, d, y, m, l, bias);
                 } else {
                     const unsigned b = part_at(level2 + part_of(w0, begins_before, from), r0);
                     store_through(parts, b + d * 4, a.part_bytes, y);
