@@ -534,7 +534,8 @@ int lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* rows, void* stre
  *   out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m),   s_j = scale * q . k_j,  over the visible positions j
  * position j of a sequence of n tokens, f of them new, is visible to new token t iff  starts <= j,  j > n - f + t - window (if a
  * window is given), and j < n - f or new token j - (n - f) is visible to t (tree, or causal).  Nothing visible: zeros.
- * Keys and values at positions that a token does not see never reach its output, whatever they hold.  out must not overlap q.
+ * Keys and values at positions that a token does not see never reach its output, whatever they hold.  out may be q itself with the same stride, and
+ * must not overlap it otherwise (LIF_INVALID_ARG).
  * batch * kv_heads * steps of a full table row (128 positions of 16-bit elements, 64 of fp32) must stay below 2^31.
  * Scores, sums and outputs are accumulated in fp32 and rounded once to E; the weights e^(s_j - m) are rounded to E for the product with the
  * values.  Every sum has a fixed order for given lengths (and hint): results are reproducible bit for bit.

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <new>
 
 #include "lif_host.h"
@@ -180,6 +181,25 @@ int stride_ok(const lif_kv* kv, int64_t stride, int heads) {
     return LIF_OK;
 }
 
+// Whether rows of `width` elements, read from `from` and written to `to`, share memory in another way than that they are the same ones.  A stride
+// holds a row, so a row of one array can touch two of the other, those that begin around it; with equal strides the same two for all rows.
+bool overlap(const lif_kv* kv, const void* from, int64_t from_stride, const void* to, int64_t to_stride, int rows, int64_t width) {
+    const int64_t e = elem_bytes(kv->cfg.dtype), size = width * e, step = from_stride * e, to_step = to_stride * e;
+    const int64_t ahead = (int64_t)(reinterpret_cast<uintptr_t>(to) - reinterpret_cast<uintptr_t>(from));
+    if (ahead >= (rows - 1) * step + size || -ahead >= (rows - 1) * to_step + size) return false;
+    if (ahead == 0 && (step == to_step || rows == 1)) return false;
+    auto touches = [&](int64_t at, int64_t first, int64_t last) {
+        int64_t k = at / step - (at % step < 0);
+        for (int i = 0; i < 2; ++i, ++k)
+            if (k >= first && k <= last && std::abs(at - k * step) < size) return true;
+        return false;
+    };
+    if (step == to_step) return touches(ahead, 1 - rows, rows - 1);
+    for (int r = 0; r < rows; ++r)
+        if (touches(ahead + r * to_step, 0, rows - 1)) return true;
+    return false;
+}
+
 }  // namespace
 
 #define LIF_TRY(call)              \
@@ -338,6 +358,8 @@ int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* st
     const Tiling g = tiling(c, query->batch, rows, kv->expected ? std::min<long long>(kv->expected, width) : width);
     if (tiling(c, query->batch, rows, width).steps >= (1ll << 31) - 4096)
         return fail(LIF_INVALID_ARG, "batch, heads and the width of the table are too large together");
+    if (overlap(kv, query->q, query->q_stride, query->out, query->out_stride, query->batch * query->n_tokens, (int64_t)c.heads * c.head_dim))
+        return fail(LIF_INVALID_ARG, "out must not overlap q (or be q itself, with the same stride)");
     const KvView& v = kv->view;
     const size_t layer_at = (size_t)layer * c.pages * v.page_bytes;
     AttendArgs a{static_cast<const char*>(query->q), static_cast<char*>(query->out), query->lse, query->q_stride, query->out_stride,

@@ -285,6 +285,10 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
     }
     const int slots0 = 2 * block * a.units;    // the block's first place for a part
     const int rows = a.n_tokens * a.share, row0 = block * QT * 16;
+    // Rows that are not there compute with one that is, and are not looked at; but where the reference lags, they have a say in when it moves.  There it is the
+    // first row of the block, which no other item writes where `out` is q itself.
+    constexpr bool LAGS = attend_slack(QT) > 0.f;
+    const int tok0 = LAGS && row0 ? quotient(row0, a.share) : 0, share0 = row0 - tok0 * a.share;
     int run_steps = quotient(all + units - 1, units);
     // by items: parts of the lane's row, steps of each, parts of the rows before
     int parts_of_row = 0, part_steps = 1, parts_before = 0;
@@ -390,9 +394,9 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
                 my_seen = ~0ull;
                 if (ok && a.tree) my_seen = a.tree[(size_t)i * a.n_tokens + tok];
             }
-            const T* from = (const T*)a.q + ((size_t)i * a.n_tokens + (ok ? tok : 0)) * a.q_stride + (unsigned)((ok ? head : 0) * dim);
+            const T* from = (const T*)a.q + ((size_t)i * a.n_tokens + (ok ? tok : tok0)) * a.q_stride + (unsigned)((ok ? head : LAGS ? kvh * a.share + share0 : 0) * dim);
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {             // (a row that is not there computes with one that is, and is not looked at)
+            for (int c = 0; c < CH; ++c) {
                 const bool sure_in = FULL && (4 * c + 4) * N <= HDP;
                 const int d = (4 * c + g) * N;
                 V held = *reinterpret_cast<const V*>(from + (sure_in || d < dim ? d : 0));

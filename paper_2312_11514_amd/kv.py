@@ -173,7 +173,7 @@ class KVCache:
             _b._check(rc)
 
     def attend(self, layer, q, out, lse=None, window=0, starts=None, tree=None, slots=None):
-        """q, out [batch, tokens, heads, head_dim]; lse float32 [batch, tokens, heads]; starts int32 [batch]; tree int64 [batch, tokens], a
+        """q, out [batch, tokens, heads, head_dim], out may be q; lse float32 [batch, tokens, heads]; starts int32 [batch]; tree int64 [batch, tokens], a
         bit per new token that is seen; slots int32 [batch]."""
         if q.dim() != 4:
             _refuse("q must be [batch, tokens, heads, head_dim]")
