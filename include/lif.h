@@ -525,7 +525,7 @@ int lif_kv_compact(lif_kv* kv, void* stream);
  * go to their pages of `layer`, queries to q_out.
  *   RMS    x / sqrt(mean x^2 + eps) * weight            LAYER  (x - mean) / sqrt(var + eps) * weight + bias
  *   rotation by a of a pair (x, y): (x cos a - y sin a, x sin a + y cos a) * rotary_scale
- * q_out may be q itself with the same stride.
+ * q_out may be q itself with the same stride, and must not overlap it otherwise (LIF_INVALID_ARG), nor k or v.
  */
 int lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* rows, void* stream);
 

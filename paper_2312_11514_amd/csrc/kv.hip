@@ -322,6 +322,8 @@ int lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* rows, void* stre
     LIF_TRY(stride_ok(kv, rows->q_out_stride, c.heads));
     LIF_TRY(stride_ok(kv, rows->k_stride, c.kv_heads));
     LIF_TRY(stride_ok(kv, rows->v_stride, c.kv_heads));
+    if (overlap(kv, rows->q, rows->q_stride, rows->q_out, rows->q_out_stride, rows->batch * rows->n_tokens, (int64_t)c.heads * c.head_dim))
+        return fail(LIF_INVALID_ARG, "q_out must not overlap q (or be q itself, with the same stride)");
     AppendArgs a{static_cast<const char*>(rows->q), static_cast<const char*>(rows->k), static_cast<const char*>(rows->v),
                  static_cast<char*>(rows->q_out), rows->q_stride, rows->k_stride, rows->v_stride, rows->q_out_stride,
                  rows->q_weight, rows->q_bias, rows->k_weight, rows->k_bias, kv->frequencies, rows->positions, rows->slots, rows->batch,

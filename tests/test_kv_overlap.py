@@ -1,4 +1,4 @@
-"""Queries and outputs of attention that share memory: rows that are the same ones are fine, any other overlap is refused (behind the stand-in for
+"""Queries and outputs of attention and of rows of a cache that share memory: rows that are the same ones are fine, any other overlap is refused (behind the stand-in for
 the HIP runtime of test_launches.py)."""
 import ctypes as C
 import json
@@ -30,7 +30,7 @@ def _shares(a, a_step, b, b_step, rows, size):
     return any(x in taken for r in range(rows) for x in range(b + r * b_step, b + r * b_step + size, 16))
 
 
-def child_attend(lib, seed):
+def _calls(lib, seed, launch):
     """[refused or not, what every byte says] of calls with random places and strides, most of them close to one another"""
     rng, seen, p = random.Random(seed), [], lib.p + (1 << 24)
     for _ in range(4000):
@@ -43,8 +43,7 @@ def child_attend(lib, seed):
         out_stride = q_stride if rng.random() < 0.6 else stride()
         at = 16 * rng.choice((0, 0, 1, -1, width * e // 16, -width * e // 16, rng.randint(-300, 300), q_stride * e // 16, 4000))
         h = _cache(lib, dtype, heads, dim)
-        q = lib.b.LifKvQuery(q=p, out=p + at, q_stride=q_stride, out_stride=out_stride, batch=batch, n_tokens=tokens)
-        rc, got = lib.launches(lambda: lib.lib.lif_kv_attend(h, 0, C.byref(q), None))
+        rc, got = lib.launches(launch(h, p, p + at, q_stride, out_stride, batch, tokens, heads * dim))
         lib.lib.lif_kv_destroy(h)
         rows = batch * tokens
         same = at == 0 and (q_stride == out_stride or rows == 1)
@@ -52,6 +51,22 @@ def child_attend(lib, seed):
         assert (rc, len(got)) == ((1, 0) if bad else (0, 1)), (dtype, heads, dim, batch, tokens, q_stride, out_stride, at, rc, got)
         seen.append((bool(bad), same, q_stride == out_stride))
     return [sum(s[0] and not s[2] for s in seen), sum(s[0] and s[2] for s in seen), sum(s[1] for s in seen), sum(not s[0] and not s[1] for s in seen)]
+
+
+def child_attend(lib, seed):
+    def launch(h, q, out, q_stride, out_stride, batch, tokens, _):
+        query = lib.b.LifKvQuery(q=q, out=out, q_stride=q_stride, out_stride=out_stride, batch=batch, n_tokens=tokens)
+        return lambda: lib.lib.lif_kv_attend(h, 0, C.byref(query), None)
+    return _calls(lib, seed, launch)
+
+
+def child_append(lib, seed):
+    def launch(h, q, out, q_stride, out_stride, batch, tokens, width):
+        k = lib.p + (1 << 30)
+        rows = lib.b.LifKvRows(q=q, k=k, v=k, q_out=out, q_stride=q_stride, k_stride=width, v_stride=width, q_out_stride=out_stride, batch=batch,
+                               n_tokens=tokens)
+        return lambda: lib.lib.lif_kv_append(h, 0, C.byref(rows), None)
+    return _calls(lib, seed, launch)
 
 
 @pytest.fixture(scope="module")
@@ -70,6 +85,10 @@ def child(tmp_path_factory):
 
 def test_outputs_that_overlap_queries(child):
     assert all(n >= 200 for n in child("attend", 1))
+
+
+def test_turned_queries_that_overlap_queries(child):
+    assert all(n >= 200 for n in child("append", 2))
 
 
 if __name__ == "__main__":
