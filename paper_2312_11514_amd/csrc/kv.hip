@@ -370,11 +370,11 @@ int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* st
                  (unsigned)(v.page_bytes / c.kv_heads), c.pages, c.max_seqs, c.max_pages, v.log_page, query->batch, query->n_tokens, c.heads,
                  c.kv_heads, share, c.head_dim, query->window, g.units, g.round_units, g.round_steps, g.blocks, g.block_rows, c.scale * kLog2e};
     hipStream_t s = (hipStream_t)stream;
-    using Launch = void (*)(const AttendArgs&, int, int, hipStream_t);
+    using Launch = bool (*)(const AttendArgs&, int, int, hipStream_t);
     static constexpr Launch kLaunch[3][3] = {{launch_attend_f32_1, launch_attend_f32_2, launch_attend_f32_4},
                                              {launch_attend_f16_1, launch_attend_f16_2, launch_attend_f16_4},
                                              {launch_attend_bf16_1, launch_attend_bf16_2, launch_attend_bf16_4}};
-    kLaunch[c.dtype][g.tiles >> 1](a, g.blocks * g.units, g.waves, s);
+    if (!kLaunch[c.dtype][g.tiles >> 1](a, g.blocks * g.units, g.waves, s)) return fail(LIF_HIP_ERROR, "no kernel for this form of attention");
     return launched();
 }
 

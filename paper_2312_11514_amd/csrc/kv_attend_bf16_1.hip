@@ -1,5 +1,5 @@
 #include "lif_kv_attend.h"
 
 namespace lif {
-void launch_attend_bf16_1(const AttendArgs& a, int groups, int waves, hipStream_t s) { launch_attend_tiles<__bf16, 1>(a, groups, waves, s); }
+bool launch_attend_bf16_1(const AttendArgs& a, int groups, int waves, hipStream_t s) { return launch_attend_tiles<__bf16, 1>(a, groups, waves, s); }
 }  // namespace lif

@@ -1,5 +1,5 @@
 #include "lif_kv_attend.h"
 
 namespace lif {
-void launch_attend_f32_4(const AttendArgs& a, int groups, int waves, hipStream_t s) { launch_attend_tiles<float, 4>(a, groups, waves, s); }
+bool launch_attend_f32_4(const AttendArgs& a, int groups, int waves, hipStream_t s) { return launch_attend_tiles<float, 4>(a, groups, waves, s); }
 }  // namespace lif

@@ -71,16 +71,16 @@ struct AttendArgs {
     float scale_log2;                      // scale * log2 e
 };
 
-// per element type and tiles of 16 rows that a wave takes over the same keys
-void launch_attend_f16_1(const AttendArgs& a, int groups, int waves, hipStream_t s);
-void launch_attend_f16_2(const AttendArgs& a, int groups, int waves, hipStream_t s);
-void launch_attend_f16_4(const AttendArgs& a, int groups, int waves, hipStream_t s);
-void launch_attend_bf16_1(const AttendArgs& a, int groups, int waves, hipStream_t s);
-void launch_attend_bf16_2(const AttendArgs& a, int groups, int waves, hipStream_t s);
-void launch_attend_bf16_4(const AttendArgs& a, int groups, int waves, hipStream_t s);
-void launch_attend_f32_1(const AttendArgs& a, int groups, int waves, hipStream_t s);
-void launch_attend_f32_2(const AttendArgs& a, int groups, int waves, hipStream_t s);
-void launch_attend_f32_4(const AttendArgs& a, int groups, int waves, hipStream_t s);
+// per element type and tiles of 16 rows that a wave takes over the same keys; false: there is no such form, nothing was launched
+bool launch_attend_f16_1(const AttendArgs& a, int groups, int waves, hipStream_t s);
+bool launch_attend_f16_2(const AttendArgs& a, int groups, int waves, hipStream_t s);
+bool launch_attend_f16_4(const AttendArgs& a, int groups, int waves, hipStream_t s);
+bool launch_attend_bf16_1(const AttendArgs& a, int groups, int waves, hipStream_t s);
+bool launch_attend_bf16_2(const AttendArgs& a, int groups, int waves, hipStream_t s);
+bool launch_attend_bf16_4(const AttendArgs& a, int groups, int waves, hipStream_t s);
+bool launch_attend_f32_1(const AttendArgs& a, int groups, int waves, hipStream_t s);
+bool launch_attend_f32_2(const AttendArgs& a, int groups, int waves, hipStream_t s);
+bool launch_attend_f32_4(const AttendArgs& a, int groups, int waves, hipStream_t s);
 
 // head_dim rounded up to what the kernels are compiled for
 __host__ __device__ __forceinline__ int attend_dim_pad(int dim) {
@@ -772,25 +772,30 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
 }
 
 template <typename T, int HDP, bool FULL, int QT>
-void launch_attend_waves(const AttendArgs& a, int groups, int waves, hipStream_t s) {
+bool launch_attend_waves(const AttendArgs& a, int groups, int waves, hipStream_t s) {
     constexpr bool lean = attend_lean(HDP, FULL, QT, sizeof(T));
     if constexpr (lean)
-        if (waves == 8) hipLaunchKernelGGL((k_kv_attend<T, HDP, FULL, QT, 8>), dim3(groups), dim3(512), 0, s, a);
+        if (waves == 8) {
+            hipLaunchKernelGGL((k_kv_attend<T, HDP, FULL, QT, 8>), dim3(groups), dim3(512), 0, s, a);
+            return true;
+        }
     if constexpr (!lean || QT == 1)
-        if (waves == 4) hipLaunchKernelGGL((k_kv_attend<T, HDP, FULL, QT, 4>), dim3(groups), dim3(256), 0, s, a);
+        if (waves == 4) {
+            hipLaunchKernelGGL((k_kv_attend<T, HDP, FULL, QT, 4>), dim3(groups), dim3(256), 0, s, a);
+            return true;
+        }
+    return false;
 }
 
 template <typename T, int HDP, int QT>
-void launch_attend(const AttendArgs& a, int groups, int waves, hipStream_t s) {
-    if (a.dim == HDP) {
-        launch_attend_waves<T, HDP, true, QT>(a, groups, waves, s);
-    } else if constexpr (HDP != 80 && QT <= (HDP == 256 ? 1 : 2)) {
-        launch_attend_waves<T, HDP, false, QT>(a, groups, waves, s);
-    }
+bool launch_attend(const AttendArgs& a, int groups, int waves, hipStream_t s) {
+    if (a.dim == HDP) return launch_attend_waves<T, HDP, true, QT>(a, groups, waves, s);
+    if constexpr (HDP != 80 && QT <= (HDP == 256 ? 1 : 2)) return launch_attend_waves<T, HDP, false, QT>(a, groups, waves, s);
+    return false;
 }
 
 template <typename T, int QT>
-void launch_attend_tiles(const AttendArgs& a, int groups, int waves, hipStream_t s) {
+bool launch_attend_tiles(const AttendArgs& a, int groups, int waves, hipStream_t s) {
     switch (attend_dim_pad(a.dim)) {
         case 32: return launch_attend<T, 32, QT>(a, groups, waves, s);
         case 64: return launch_attend<T, 64, QT>(a, groups, waves, s);
@@ -798,7 +803,8 @@ void launch_attend_tiles(const AttendArgs& a, int groups, int waves, hipStream_t
         case 96: return launch_attend<T, 96, QT>(a, groups, waves, s);
         case 128: return launch_attend<T, 128, QT>(a, groups, waves, s);
         default:
-            if constexpr (QT <= 2) launch_attend<T, 256, QT>(a, groups, waves, s);
+            if constexpr (QT <= 2) return launch_attend<T, 256, QT>(a, groups, waves, s);
+            return false;
     }
 }
 
