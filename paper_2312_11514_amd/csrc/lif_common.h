@@ -187,6 +187,14 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// What lanes of a wave have stored to LDS is what its others load behind this.  The hardware keeps a wave's LDS accesses in order, so it costs nothing;
+// the compiler has to be kept to it.
+__device__ __forceinline__ void lds_wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Inclusive prefix sum over the lanes of a wave.
 __device__ __forceinline__ int wave_inclusive_scan(int v, int /*lane*/) {
     // data-parallel-primitive moves instead of six shuffles through the LDS crossbar: shifts by 1, 2, 4, 8 inside

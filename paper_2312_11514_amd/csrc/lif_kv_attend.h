@@ -512,6 +512,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
                 const int vp = p + N * g;
                 const bool edge = p < sure || p + STAGE > sure_end;
                 if (edge) {
+                    if (QT > 1) lds_wave_fence();          // (sees_at, seen_at: stored by the lanes of the first group)
 #pragma unroll
                     for (int t = 0; t < QT; ++t) {
                         const int2 at = QT == 1 ? my_sees : sees_at[wv][16 * t + n];
@@ -667,6 +668,7 @@ __global__ __launch_bounds__(64 * WAVES, attend_lean(HDP, FULL, QT, sizeof(T)) ?
 #pragma unroll 1
     for (int seg = 0; seg < 2; ++seg) {
         if (!(joins >> seg & 1)) continue;
+        lds_wave_fence();
         const int4 of = join_of[wv][seg];
         const int w0 = whole_wave(of.x), count = whole_wave(of.y), runs = (count + kAttendFan - 1) / kAttendFan;
         const bool begins_before = whole_wave(of.z);
