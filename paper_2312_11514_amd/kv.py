@@ -51,7 +51,7 @@ class KVCache:
         if dtype not in _DTYPES:
             _refuse("dtype must be f32, f16 or bf16")
         self.cfg = _b.LifKvConfig(layers, heads, kv_heads, head_dim, page_tokens, pages, max_seqs, max_pages, max_tokens, _DTYPES[dtype],
-                                  norm, rotary, rotary_dim, norm_eps, rotary_scale, head_dim ** -0.5 if scale is None else scale)
+                                  norm, rotary, rotary_dim, norm_eps, rotary_scale, max(head_dim, 1) ** -0.5 if scale is None else scale)
         ws_bytes = self.lib.lif_kv_workspace_bytes(C.byref(self.cfg))
         if ws_bytes == 0:
             _refuse("configuration rejected by lif_kv_workspace_bytes")
