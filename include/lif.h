@@ -473,7 +473,10 @@ typedef struct lif_kv_query {
     int32_t window;         /* positions more than window - 1 before a token's own are not visible to it; 0: all are */
 } lif_kv_query;
 
-/* Bytes of scratch lif_kv_create needs for this configuration (0 if cfg is invalid). */
+/*
+ * Bytes of scratch lif_kv_create needs for this configuration (0 if cfg is invalid).  Most of it is for the parts of lif_kv_attend's sums, and grows with
+ * max_tokens * heads / kv_heads up to some 64 rows a workgroup: 32 heads of 128 on 8 take 4 MB for 1 token, 17 for 5, 38 for 64, 151 for 256.
+ */
 size_t lif_kv_workspace_bytes(const lif_kv_config* cfg);
 
 /* As lif_create: validates, enqueues nothing; call lif_kv_reset (or write the tables and call lif_kv_adopt) first. */
@@ -545,7 +548,8 @@ int lif_kv_attend(lif_kv* kv, int32_t layer, const lif_kv_query* query, void* st
 /*
  * Performance hint for lif_kv_attend: cached tokens of a sequence as a rule; 0 (the default): as many as a table row holds.  Decides in
  * which blocks rows and positions are taken where a key head has 4 rows or more (tokens times the query heads that share it), and with that
- * the order of their sums: results may differ in the last bits.
+ * the order of their sums: results may differ in the last bits.  Worth setting where tables are much wider than sequences (5 tokens of 4 sequences of
+ * 1000, 32 heads on 8, in tables for 32768: 11.5 us with it, 15.0 without).
  */
 int lif_kv_set_expected_tokens(lif_kv* kv, int32_t tokens);
 

@@ -76,7 +76,7 @@ struct KvLayout {
 // heads of 128 on 8: 22.2 us in blocks of 16 rows, 45.2 in ones of 64).
 // Tables are wider than their sequences as a rule, so blocks can come out too large: ones of 64 rows that leave a compute unit four waves only are taken for
 // 128 rows and more (16 tokens of one sequence of 1000 in a table for 32768: 15.4 us in blocks of 32 rows, 28.3 in ones of 64; 16 sequences of 4000: 64.1
-// and 61.7).
+// and 61.7).  With lif_kv_set_expected_tokens(1000) that call takes 11.5 us.
 struct Tiling {
     int tiles, waves, blocks, block_rows, units, round_units, round_steps;
     long long steps;                     // of a block's items, at most
@@ -112,7 +112,8 @@ Tiling tiling(const lif_kv_config& c, int batch, int rows, long long positions) 
     // Eight waves share a part, or four: the larger parts are fewer to add, the smaller ones fill the chip sooner, and two workgroups of them hide
     // each other's beginnings and ends.  Larger ones pay where a part has some rows, and where workgroups go through parts of one item and few are left
     // over (4 tokens of 4 sequences of up to 4000, 32 heads on 8: 20.8 us with four, 14.2 with eight; one of 32 sequences of 2000, 71 heads on one,
-    // 160 items: 15.1 and 18.4; one of 64 sequences, 512 items: 144.5 and 149.3).
+    // 160 items: 15.1 and 18.4; one of 64 sequences, 512 items: 144.5 and 149.3).  Between these points, and around the 768 and 2048 positions, nothing was
+    // measured.
     const long long items = (long long)batch * c.kv_heads * g.blocks;
     const bool few = items <= kAttendUnits / 2 || (items <= kAttendUnits && 8 * items > 7 * kAttendUnits);
     const bool fits = lean(c, g.tiles), some = g.block_rows >= 4 && (positions > (g.block_rows >= 16 ? 768 : 2048) || items >= kAttendUnits / 2);

@@ -10,9 +10,10 @@
 // 16-byte load of the same line and not an exchange, since it is normalised with other weights anyway.
 // Values: the cache keeps N consecutive tokens of a dimension in 16 bytes.  Written token by token, from workgroups on different XCDs,
 // those are N writes of a part of a line each; a workgroup takes the N tokens of a piece together and writes it whole where it has all of them.
-// What it measured: one token of 32 heads of 128 3.1 us (6.5 as called from Python, which is what a launch costs there); 32 prompts of up to 64
-// tokens, 64 heads of 64, bf16, layer norms, half of a head turned: 58 MB in 19.4 us, 3.0 TB/s of the 4.7 a large copy reaches (66 us with values
-// token by token and angles per lane).
+// What it measured: one token of 32 heads of 128 3.1 us in a graph (6.5 as called from Python, which is what a launch costs there); 32 prompts of up to
+// 64 tokens, 64 heads of 64, bf16, layer norms, half of a head turned: 58 MB in 19.5 us where the last-level cache has them, 23.5 from memory, 2.5 TB/s of
+// the 4.8 a large copy reaches (66 us with values token by token and angles per lane).  117 registers in that form leave a compute unit four
+// workgroups of 4352, so they come in more than four rounds, each a chain of five round trips.
 #pragma once
 
 #include "lif_kv.h"
@@ -156,8 +157,8 @@ __global__ __launch_bounds__(256) void k_kv_append(const KvView kv, const Append
     const int d1 = !turns || INTERLEAVED ? d0 : upper ? d0 - half : d0 + half;
     const int first = (unit - t * a.head_blocks) * a.heads_per_block, last = min(first + a.heads_per_block, a.heads + a.kv_heads);
     // The lane's dimensions of its next heads, and those they are paired with.  Of single tokens the first ones are asked for before it is
-    // known whether the token is there; of several many may not be, and reading all of them costs more than the wait (25.9 us against 22 in
-    // the case above, where half are padding).
+    // known whether the token is there; of several many may not be, and reading all of them costs more than the wait (from memory 25.7 us against
+    // 23.5 in the case above, where half are padding; 32.5 against 30.8 where none is).
     const T *q_row = (const T*)a.q + (size_t)row * a.q_stride, *k_row = (const T*)a.k + (size_t)row * a.k_stride;
     T* q_to = (T*)a.q_out + (size_t)row * a.q_out_stride + d0;
     V own[kAppendAhead], other[kAppendAhead];

@@ -21,12 +21,15 @@
 // differ in length, and the host does not know them: the steps of all items, one after the other, are dealt to a fixed number of
 // workgroups in equal contiguous runs, each of which works out its own from the lengths.  A run that is a whole item writes its
 // output; of an item's parts every workgroup leaves the maximum, the sum and the unscaled output behind, and the last one to do so adds them.
-// What that leaves: one sequence of 200003, 32 heads of 128 on 8, bf16: 819 MB in 144 us, 5.7 TB/s (a plain streaming read reaches 6.3); 64 of up to
-// 8192, fp16: 794 MB in 146 us; 16 of up to 6001 with 5 tokens each: 120 MB in 36.5 us; one of 2048, 32 heads: 33.6 MB in 11.6 us, where a plain
-// read in a launch of its own takes 7.7; one of 77: 5.7 us.  Of those 11.6 the launch has 1.8, lengths and first table entries 2.5, the merge of the
-// waves 0.8, the count of parts 0.7, adding the parts 2.
+// What that leaves, with tables about as wide as the sequences: one sequence of 200003, 32 heads of 128 on 8, bf16: 819 MB in 146 us, 5.6 TB/s (a plain
+// streaming read reaches 6.3); 64 of up to 8192, fp16: 794 MB in 147 us; 16 of up to 6001 with 5 tokens each: 120 MB in 37.5 us; one of 2048, 32 heads:
+// 33.6 MB in 12 us, where a plain read in a launch of its own takes 7.3; one of 77: 5.8 us.  Of those 12 the launch has 1.8, lengths and first table
+// entries 2.5, the merge of the waves 0.8, the count of parts 0.7, adding the parts 2.
 // Many rows are bound by the matrix cores and the arithmetic on scores between them, with one or two waves a SIMD: 20 tokens of 64 sequences of 8000, 71
-// heads of 64 on one, 186 GFLOP in 355 us, 0.52 PFLOP/s (a library's large product reaches 1.1).
+// heads of 64 on one, 186 GFLOP in 367 us, 0.51 PFLOP/s (a library's large product reaches 1.16); 64 tokens of 4 sequences of 4000, 32 heads of 128 on 8:
+// bf16 49 us, 0.34 PFLOP/s, fp32 180 us, 0.093 of 0.154.
+// Registers go to memory in fp32 for dimensions that are not compiled: 188 to 196 bytes a lane for 104, 112 and 120, 312 for 136 to 248 (one token of 8
+// sequences of 1000, 16 heads of 112: 52 us, of 128: 31.5), and 12 bytes in bf16 with eight waves for 104 to 120.
 #pragma once
 
 #include "lif_kv.h"

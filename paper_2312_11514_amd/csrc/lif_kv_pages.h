@@ -1,7 +1,7 @@
 // The calls on the pages of a key-value cache: reset, adopt, reserve, truncate, fork, compact.
 //
 // A page is free iff refs[page] == 0.  The same as one bit per page, set where it is free, is what the calls look for pages in: 64
-// pages a word, so that one workgroup sees 65536 pages per pass.  The plans (which page goes where) are made by one workgroup, whose
+// pages a word and a word a thread, so that one workgroup sees 16384 pages a pass with 256 threads, 65536 with 1024.  The plans (which page goes where) are made by one workgroup, whose
 // time is a few dependent memory round trips; the copies that follow from them by a launch over the whole chip (k_kv_move).  A reservation,
 // which every step of a program makes, is a single launch.
 #pragma once
@@ -10,7 +10,8 @@
 
 namespace lif {
 
-// threads of the planning workgroup, one per slot: 256 or 1024 (max_seqs).  A barrier among 16 waves costs more than one among 4.
+// threads of the planning workgroup, one per slot: 256 or 1024 (max_seqs).  A barrier among 16 waves costs more than one among 4; a pool of more
+// than 16384 pages takes more passes with 256 (one of 200000 whose first pages are in use 9.7 us for reserve + truncate, one of 8192 9.5).
 constexpr int kKvPlanFew = 256;
 
 // Walks the set bits of the words [w0, w1) in ascending order by the whole workgroup: emit(rank, page) for those of rank < total, and
@@ -136,7 +137,8 @@ __device__ __forceinline__ void copy_pages(const KvView& kv, const int2* moves, 
 // Without sharing the first workgroup does everything.  With it every workgroup works out the same plan for itself, and copies its
 // part of the pages; nothing that the plan follows from may change before all of them have read it, so it is the last one to have
 // planned that writes it down.  One launch, and no workgroup waits for another (reserve + truncate of 64 slots, called one after the other:
-// 8.8 us a pair; 12.2 with the copies in a launch of their own).
+// 8.8 us a pair; 12.2 with the copies in a launch of their own).  After a fork a page may have several holders, and stays counted as such until
+// lif_kv_reset or lif_kv_adopt: 32 sequences of 2000, 9.5 us a pair before a fork, 12.0 after it, also when the beam is gone.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void k_kv_reserve(const KvView kv, const int32_t* __restrict__ counts) {
     __shared__ WalkScratch<THREADS> ws;

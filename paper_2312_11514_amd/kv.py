@@ -195,6 +195,7 @@ class KVCache:
             _b._check(rc)
 
     def set_expected_tokens(self, tokens: int):
+        """Cached tokens of a sequence as a rule (0: as many as a table row holds): for attend(), where tables are much wider than sequences."""
         _b._check(self.lib.lif_kv_set_expected_tokens(self.handle, int(tokens)))
 
     # ---- introspection ---------------------------------------------------------------------------------------------------
