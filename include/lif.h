@@ -563,6 +563,109 @@ int lif_kv_get_state(lif_kv* kv, lif_kv_state* out, void* stream);
 int lif_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double trained, double slow, double fast,
                          double* out);
 
+/*
+ * ---- What stays resident beside them: norms with the residual's addition, and projections with weights in 4 bits -----------------
+ *
+ * The attention weights, the output head and the norms are not streamed (Section 3, selective persistence); weights in 4 bits leave the memory to the
+ * neuron cache.  Per half of a layer the caller issues, on one HIP stream,
+ *
+ *     lif_add_norm  ->  lif_packed_multiply (queries, keys and values)  ->  lif_kv_append -> lif_kv_attend  ->  lif_packed_multiply  -> ...
+ *
+ *   - E is fp32, fp16 or bfloat16.  Rows lie at a stride in elements; rows of E begin at multiples of 16 bytes, rows of 8 bits at multiples of 8.
+ *   - Neither call needs a workspace, blocks or synchronises, and all can be captured into a HIP graph.  lif_add_norm has no handle; calls of
+ *     lif_packed_multiply and lif_packed_dequantize on one handle may overlap on several streams, lif_packed_quantize and lif_packed_pack with none.
+ *   - Rows in 8 bits are whole numbers -127..127 with an fp32 scale for the row, or for each `group` of its elements (the last group may be
+ *     shorter): element = code * scale.
+ */
+
+/* Rows of a lif_add_norm. */
+typedef struct lif_norm_rows {
+    const void* x;          /* [n_rows x width] E                                                */
+    const void* residual;   /* [n_rows x width] E, added to x; NULL: none                        */
+    void* total;            /* [n_rows x width] E, written: residual + x; NULL: not wanted.  May be the rows of x or of the residual */
+    void* out;              /* [n_rows x width], written: E, or 8 bits if scales are given.  May be the rows of x or of the residual (E) */
+    float* scales;          /* [n_rows] or [n_rows x ceil(width / group)] fp32, written; NULL: out is E */
+    const float* weight;    /* [width] fp32; NULL: ones.  Unused without a norm                  */
+    const float* bias;      /* [width] fp32; NULL: zeros.  LIF_NORM_LAYER only                   */
+    int64_t x_stride, residual_stride, total_stride, out_stride;  /* elements between rows       */
+    int32_t n_rows;         /* 1..2^19                                                           */
+    int32_t width;          /* a multiple of 8, 8..65536                                         */
+    int32_t dtype;          /* enum lif_dtype: E                                                 */
+    int32_t norm;           /* enum lif_norm (LIF_NORM_NONE: the addition, the rounding to 8 bits) */
+    int32_t group;          /* elements of a scale: 32, 64 or 128; 0: the row has one            */
+    float eps;
+} lif_norm_rows;
+
+/*
+ * h = residual + x, total = h rounded to E, and of h (not of the rounded total)
+ *   NONE  h      RMS  h / sqrt(mean h^2 + eps) * weight      LAYER  (h - mean) / sqrt(var + eps) * weight + bias
+ * rounded to E, or to 8 bits: scale = max |y| * (1 / 127), in fp32, rounded to 16 significant bits, code = y / scale rounded to the nearest whole number, of
+ * two the even one (a step of 16 bits makes that exact).  Sums are fp64, rounded once; the rest is fp32 in the order written here, every operation
+ * rounded: results do not depend on the number of rows, and are reproducible bit for bit.  Where the scale is below 2^-110 scale and codes are 0; where it
+ * would be infinite or not a number the scale is not a number.  total, out and scales must not overlap each other, nor weight and bias, nor x and the residual in
+ * another way than as the same rows (LIF_INVALID_ARG; of rows at different strides whose ranges meet, any).
+ */
+int lif_add_norm(const lif_norm_rows* rows, void* stream);
+
+typedef struct lif_packed lif_packed;
+
+typedef struct lif_packed_config {
+    int32_t n_out;          /* rows of the matrix: 1..2^20                                       */
+    int32_t n_in;           /* a multiple of 8, 8..65536                                         */
+    int32_t group;          /* inputs that share a scale (and a zero point): 32, 64 or 128       */
+    int32_t zeros;          /* 0: every zero point is 8; 1: each group has one                   */
+    int32_t dtype;          /* enum lif_dtype: of full weights, rows and outputs                 */
+} lif_packed_config;
+
+typedef struct lif_packed_buffers {
+    void* codes;            /* device, lif_packed_code_bytes(cfg) bytes, 16-byte aligned         */
+    void* groups;           /* device, lif_packed_group_bytes(cfg) bytes, 16-byte aligned        */
+    size_t code_bytes, group_bytes;
+} lif_packed_buffers;
+
+/* Rows of a lif_packed_multiply. */
+typedef struct lif_packed_rows {
+    const void* x;          /* [n_rows x n_in]: E, or 8 bits if x_scales are given               */
+    const float* x_scales;  /* [n_rows] or [n_rows x ceil(n_in / x_group)] fp32; NULL: x is E    */
+    const float* bias;      /* [n_out] fp32, or NULL                                             */
+    void* out;              /* [n_rows x n_out] E, written; must not overlap x, x_scales or bias */
+    int64_t x_stride, out_stride;  /* elements between rows; that of out need not be a multiple of anything */
+    int32_t n_rows;         /* 1..2^19                                                           */
+    int32_t x_group;        /* 0: a scale for each row; else the group of the weights            */
+} lif_packed_rows;
+
+/* Bytes of the two arrays (0 if cfg is invalid): n_out rounded up to 16 times n_in rounded up to 128, half a byte each; 4 bytes for each group. */
+size_t lif_packed_code_bytes(const lif_packed_config* cfg);
+size_t lif_packed_group_bytes(const lif_packed_config* cfg);
+
+/* As lif_create: validates, enqueues nothing; call lif_packed_quantize or lif_packed_pack first (or fill the arrays with those of an equal handle). */
+int lif_packed_create(const lif_packed_config* cfg, const lif_packed_buffers* buf, lif_packed** out);
+int lif_packed_destroy(lif_packed* packed);
+
+/*
+ * From full weights (device, [n_out x n_in] E, rows at `stride` elements, 16-byte aligned).  Of the weights w of a group
+ *   zeros 0   scale = max |w| * (1 / 7), zero = 8      zeros 1   scale = (max(w, 0) - min(w, 0)) * (1 / 15), zero = -min(w, 0) / scale, nearest
+ * scale in fp32, rounded to 16 significant bits;  code = w / scale + zero to the nearest whole number, of two the even w / scale, in 0..15.  A scale below 2^-110
+ * counts as 0; groups with a weight that is not finite, or whose scale would not be, give weights that are not numbers.
+ */
+int lif_packed_quantize(lif_packed* packed, const void* weights, int64_t stride, void* stream);
+
+/*
+ * From codes (device, [n_out x n_in / 2], two in a byte, the lower input in the lower half), scales [n_out x ceil(n_in / group)] fp32, which are
+ * rounded to 16 significant bits (fp16 and bf16 values are kept), and zeros [n_out x ceil(n_in / group)], 0..255, NULL if the configuration has none.
+ */
+int lif_packed_pack(lif_packed* packed, const uint8_t* codes, const float* scales, const uint8_t* zeros, void* stream);
+
+/* What the weights stand for, scale * (code - zero) rounded to E, [n_out x n_in] at `stride` elements, 16-byte aligned. */
+int lif_packed_dequantize(lif_packed* packed, void* weights, int64_t stride, void* stream);
+
+/*
+ * out[t, n] = sum_k x[t, k] * scale[n, k / group] * (code[n, k] - zero[n, k / group]) + bias[n]
+ * Weights are not rounded further: a group's sum is fp32 (whole numbers for rows in 8 bits), scaled, added up in fp32 and rounded once to E.  Sums have a
+ * fixed order for a given number of rows.  A row that holds infinity or NaN, or meets a scale that does, gives infinity or NaN there; other rows do not see it.
+ */
+int lif_packed_multiply(lif_packed* packed, const lif_packed_rows* rows, void* stream);
+
 /* Message of the last LIF_HIP_ERROR / LIF_INVALID_ARG on the calling thread. */
 const char* lif_last_error_string(void);
 

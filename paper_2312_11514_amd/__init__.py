@@ -1,7 +1,8 @@
 """MI355X-native sparse-FFN hot path of "LLM in a flash" (arXiv 2312.11514).
 
 The product is the C-ABI library declared in include/lif.h (HIP kernels for gfx950);
-this package is the thin ctypes binding over it: Layer (an FFN layer) and KVCache (a paged key-value cache with its attention).  There is no CPU fallback: importing
+this package is the thin ctypes binding over it: Layer (an FFN layer), KVCache (a paged key-value cache with its attention), and what
+stays resident beside them: add_norm and PackedLinear (weights in 4 bits).  There is no CPU fallback: importing
 `binding` without a built liblif.so raises.
 """
 from .binding import (  # noqa: F401
@@ -11,3 +12,4 @@ from .binding import (  # noqa: F401
     ROPE_RAMP,
 )
 from .kv import KVCache, rope_frequencies  # noqa: F401
+from .packed import PackedLinear, add_norm  # noqa: F401

@@ -73,6 +73,25 @@ class LifKvQuery(C.Structure):
         [(n, C.c_void_p) for n in ("slots", "starts", "tree")] + [(n, C.c_int32) for n in ("batch", "n_tokens", "window")]
 
 
+class LifNormRows(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "residual", "total", "out", "scales", "weight", "bias")] + \
+        [(n, C.c_int64) for n in ("x_stride", "residual_stride", "total_stride", "out_stride")] + \
+        [(n, C.c_int32) for n in ("n_rows", "width", "dtype", "norm", "group")] + [("eps", C.c_float)]
+
+
+class LifPackedConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_out", "n_in", "group", "zeros", "dtype")]
+
+
+class LifPackedBuffers(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("groups", C.c_void_p), ("code_bytes", C.c_size_t), ("group_bytes", C.c_size_t)]
+
+
+class LifPackedRows(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "x_scales", "bias", "out")] + [("x_stride", C.c_int64), ("out_stride", C.c_int64)] + \
+        [("n_rows", C.c_int32), ("x_group", C.c_int32)]
+
+
 EXPORTS = {
     "lif_version": (C.c_int, []),
     "lif_last_error_string": (C.c_char_p, []),
@@ -113,6 +132,15 @@ EXPORTS = {
     "lif_kv_attend": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(LifKvQuery), C.c_void_p]),
     "lif_kv_set_expected_tokens": (C.c_int, [C.c_void_p, C.c_int32]),
     "lif_kv_get_state": (C.c_int, [C.c_void_p, C.POINTER(LifKvState), C.c_void_p]),
+    "lif_add_norm": (C.c_int, [C.POINTER(LifNormRows), C.c_void_p]),
+    "lif_packed_code_bytes": (C.c_size_t, [C.POINTER(LifPackedConfig)]),
+    "lif_packed_group_bytes": (C.c_size_t, [C.POINTER(LifPackedConfig)]),
+    "lif_packed_create": (C.c_int, [C.POINTER(LifPackedConfig), C.POINTER(LifPackedBuffers), C.POINTER(C.c_void_p)]),
+    "lif_packed_destroy": (C.c_int, [C.c_void_p]),
+    "lif_packed_quantize": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "lif_packed_pack": (C.c_int, [C.c_void_p] * 5),
+    "lif_packed_dequantize": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    "lif_packed_multiply": (C.c_int, [C.c_void_p, C.POINTER(LifPackedRows), C.c_void_p]),
     "lif_rope_frequencies": (C.c_int, [C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4 + [C.POINTER(C.c_double)]),
 }
 

@@ -1,0 +1,5 @@
+#include "lif_packed_few.h"
+
+namespace lif {
+void launch_product_bf16(const ProductArgs& a, bool zeros, hipStream_t s) { launch_product_as<__bf16>(a, zeros, s); }
+}  // namespace lif
