@@ -21,7 +21,7 @@ def flags_of(source):
     """The flags of a source.  Attention: sums of the matrix instructions stay in vector registers also where a wave has more than 256 of
     them; as accumulation registers they are moved back and forth around every rescaling."""
     name = os.path.basename(source)
-    return HIPCC_FLAGS + (["-mllvm", "-amdgpu-mfma-vgpr-form"] if name.startswith("kv_attend") else [])
+    return HIPCC_FLAGS + (["-mllvm", "-amdgpu-mfma-vgpr-form"] if name.startswith(("kv_attend", "packed_")) else [])
 
 
 def _run(cmd, verbose):

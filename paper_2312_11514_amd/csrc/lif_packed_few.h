@@ -3,13 +3,14 @@
 //   y[t, n] = sum over groups g of step[n, g] * sum_{k in g} x[t, k] * (code[n, k] - zero[n, g])   (+ bias[n])
 //
 // A tile of 16 outputs is one operand, 16 rows of x the other, and the lane (r, q) gets row r of the outputs 4 q .. 4 q + 3: with one row in use of 16 the
-// products still cost less than the bytes.  Codes become elements by a mask and, where it takes one, an addition, exactly:
-//   fp16  1024 + c and 1024 + 16 c are patterns of bits; minus 1032, or times 1/16 minus 72, is c - 8
-//   bf16  (16 + c) / 2^12 is a pattern of bits; what is too much comes off with the zero point, by the sum of x
+// products still cost less than the bytes.  Codes become elements by masks, exactly:
+//   fp16  64 + c is a pattern of bits; so is 1024 + c or 1024 + 16 c, and minus 1032, or times 1/16 minus 72, that is c - 8
+//   bf16  (128 + c) / 2^16 is a pattern of bits
 //   fp32  c - 8 in bf16; x / 2^11 is three bf16 pieces of 8 bits each, which are exact together
 //   8 bits  16 (c - 8), whole numbers throughout
-// Every group's sum is fp32 (or whole), and its step and zero point are applied to that: weights are not rounded.  bf16 and fp32 rows may be as large as what
-// sums are held in: with 2^-12 or 2^-11 on one side no group's sum is infinite before its step is applied, and an output gets the factor back at its end.
+// What is too much comes off with the sum of x.  Every group's sum is fp32 (or whole), and its step and zero point are applied to that: weights are not rounded.
+// bf16 and fp32 rows may be as large as what sums are held in: with 2^-16 or 2^-11 on one side no group's sum is infinite before its step is applied, and an
+// output gets the factor back at its end.
 #pragma once
 
 #include <type_traits>
@@ -27,42 +28,35 @@ struct ProductArgs {
     const float* x_scales;           // rows in 8 bits: [rows][x_groups]
     const float* bias;
     long long x_stride, out_stride;  // elements
-    int32_t rows, x_groups, out_type;      // x_groups: 1, or as many as the matrix has; out_type: enum lif_dtype
+    int32_t rows, x_groups, out_type;      // x_groups: 1, or as many as a row of the matrix has; out_type: enum lif_dtype
 };
 
-// Eight inputs of a row as the matrix cores take them, and the codes beside them.
+// Eight codes as the matrix cores take them: codes() counts kMiddle as 0; all(v) in the place of codes adds v times the sum of x.
 template <typename X> struct Operand;
 template <> struct Operand<_Float16> {
-    typedef f32x4 Acc;
     static constexpr int kPieces = 1;
     static constexpr float kUp = 1.f;        // what an output is multiplied by at its end
-    static constexpr float kMiddle = 8.f;    // the code that counts 0
+    static constexpr float kMiddle = -64.f;  // the code that counts 0
     typedef f16x8 Word;
     static __device__ __forceinline__ Word codes(unsigned w) {
-        const unsigned u = w >> 8;
-        const f16x2 minus{(_Float16)-1032.f, (_Float16)-1032.f}, part{(_Float16)0.0625f, (_Float16)0.0625f}, less{(_Float16)-72.f, (_Float16)-72.f};
-        auto low = [&](unsigned v) { return __builtin_bit_cast(f16x2, (v & 0x000f000fu) ^ 0x64086408u) + minus; };
-        auto high = [&](unsigned v) { return __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (v & 0x00f000f0u) ^ 0x64806480u), part, less); };
-        const f16x2 a = low(w), b = high(w), c = low(u), d = high(u);
-        return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+        auto pair = [](unsigned v) { return (v & 0x00f000f0u) ^ 0x54805480u; };
+        return __builtin_bit_cast(Word, u32x4{pair(w << 4), pair(w), pair(w >> 4), pair(w >> 8)});
     }
-    static __device__ __forceinline__ Word ones() { const _Float16 o = (_Float16)1.f; return Word{o, o, o, o, o, o, o, o}; }
-    static __device__ __forceinline__ Acc mul(Word a, f16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ Word all(float v) { const _Float16 o = (_Float16)v; return Word{o, o, o, o, o, o, o, o}; }
+    static __device__ __forceinline__ f32x4 mul(Word a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 template <> struct Operand<__bf16> {
-    typedef f32x4 Acc;
     static constexpr int kPieces = 1;
-    static constexpr float kUp = 4096.f, kMiddle = -16.f;
+    static constexpr float kUp = 65536.f, kMiddle = -128.f;
     typedef bf16x8 Word;
     static __device__ __forceinline__ Word codes(unsigned w) {
-        auto pair = [](unsigned v) { return (v & 0x00780078u) ^ 0x3bc03bc0u; };
-        return __builtin_bit_cast(Word, u32x4{pair(w << 3), pair(w >> 1), pair(w >> 5), pair(w >> 9)});
+        auto pair = [](unsigned v) { return (v & 0x000f000fu) ^ 0x3b083b08u; };      // (128 + c) / 2^16
+        return __builtin_bit_cast(Word, u32x4{pair(w), pair(w >> 4), pair(w >> 8), pair(w >> 12)});
     }
-    static __device__ __forceinline__ Word ones() { return __builtin_bit_cast(Word, u32x4{0x39803980u, 0x39803980u, 0x39803980u, 0x39803980u}); }     // 2^-12
-    static __device__ __forceinline__ Acc mul(Word a, bf16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ Word all(float v) { const __bf16 o = (__bf16)(v / kUp); return Word{o, o, o, o, o, o, o, o}; }
+    static __device__ __forceinline__ f32x4 mul(Word a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Operand<float> {
-    typedef f32x4 Acc;
     static constexpr int kPieces = 3;
     static constexpr float kUp = 2048.f, kMiddle = 8.f;
     typedef bf16x8 Word;
@@ -73,9 +67,45 @@ template <> struct Operand<float> {
         };
         return __builtin_bit_cast(Word, u32x4{pair(0), pair(1), pair(2), pair(3)});
     }
-    static __device__ __forceinline__ Word ones() { return __builtin_bit_cast(Word, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}); }
-    static __device__ __forceinline__ Acc mul(Word a, bf16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ Word all(float v) { const __bf16 o = (__bf16)v; return Word{o, o, o, o, o, o, o, o}; }
+    static __device__ __forceinline__ f32x4 mul(Word a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
+template <> struct Operand<signed char> {    // 16 (c - 8)
+    static constexpr float kUp = 0.0625f, kMiddle = 8.f;
+};
+// an element of a row in 8 bits that has a scale for each group of the weights
+struct ByGroup {
+    signed char code;
+};
+template <> struct Operand<ByGroup> : Operand<signed char> {};
+
+// Rows first .. first + n - 1 of x as a buffer: what lies behind the last of them is 0, and so is every row that is not there.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const ProductArgs& a, int bytes, int first, int n) {
+    const int rows = min(n, a.rows - first);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.x) + (long long)first * a.x_stride * bytes, 0,
+                                             (int)((rows - 1) * (int)a.x_stride * bytes + a.w.n_in * bytes), 0x00027000);
+}
+
+// sum of eight elements
+__device__ __forceinline__ float sum_of(const f16x8& v) {
+    const f16x2 one{(_Float16)1.f, (_Float16)1.f};
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_fdot2(f16x2{v[2 * i], v[2 * i + 1]}, one, s, false);
+    return s;
+}
+__device__ __forceinline__ float sum_of(const bf16x8& v) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += (float)v[i];
+    return s;
+}
+__device__ __forceinline__ float sum_of(const Eight<float>::Raw& v) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += v[i];
+    return s;
+}
 
 // Rows of x: eight inputs of an fp32 row as three pieces, cut off and not rounded, so that what is left is exact and nothing becomes infinite.
 struct Pieces {
@@ -97,30 +127,6 @@ __device__ __forceinline__ Pieces pieces_of(const Eight<float>::Raw& v) {
     return Pieces{{__builtin_bit_cast(bf16x8, w[0]), __builtin_bit_cast(bf16x8, w[1]), __builtin_bit_cast(bf16x8, w[2])}};
 }
 
-// A tile's products: c[s] += of the sub-group s = word * S / 4, S = 128 / G sub-groups, and the sums of x beside them.
-template <typename X>
-struct Rows {
-    typename Eight<X>::Raw v[4];
-    __device__ __forceinline__ void load(const X* row, int at, int n_in, bool in) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (in && at + 32 * j < n_in) v[j] = Eight<X>::load(row + at + 32 * j);
-            else v[j] = typename Eight<X>::Raw{};
-        }
-    }
-};
-template <>
-struct Rows<signed char> {
-    u32x2 v[4];
-    __device__ __forceinline__ void load(const signed char* row, int at, int n_in, bool in) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (in && at + 32 * j < n_in) v[j] = *reinterpret_cast<const u32x2*>(row + at + 32 * j);
-            else v[j] = u32x2{0, 0};
-        }
-    }
-};
-
 template <typename X>
 __device__ __forceinline__ void store_as(char* out, int type, long long at, float v) {
     if constexpr (sizeof(X) != 1) reinterpret_cast<X*>(out)[at] = (X)v;
@@ -129,126 +135,200 @@ __device__ __forceinline__ void store_as(char* out, int type, long long at, floa
     else reinterpret_cast<__bf16*>(out)[at] = (__bf16)v;
 }
 
-// One workgroup: 16 outputs, 16 * NT rows; its waves take the tiles of the inputs in turn and add up in LDS.
-template <typename X, int G, bool ZEROS, int NT, int WAVES>
+// A tile of the inputs of 4 * MQ rows, of one wave: asked for row by row, 16 lanes each, and handed to the lanes that the matrix cores want them from
+// through LDS, where rows are a chunk longer than they need, so that the 16 lanes that read one chunk of 16 rows meet different banks.
+template <typename X, int MQ>
+struct FewRows {
+    static constexpr bool kBytes = sizeof(X) == 1;
+    static constexpr int kRows = 4 * MQ, kSlots = 4 / MQ, kChunks = kBytes ? 8 : 16, kPlanes = sizeof(X) == 4 ? 3 : 1;
+    struct Buffer {
+        u32x4 x[kPlanes][kRows + (kSlots > 1)][kChunks + 1];      // (the last row is zeros)
+    };
+    std::conditional_t<kBytes, u32x2, typename Eight<std::conditional_t<kBytes, float, X>>::Raw> v[MQ];
+
+    // k: of this lane, inside the row
+    __device__ __forceinline__ void ask(const X* const (&from)[MQ], int k) {
+#pragma unroll
+        for (int i = 0; i < MQ; ++i) {
+            if constexpr (kBytes) v[i] = *reinterpret_cast<const u32x2*>(from[i] + k);
+            else v[i] = Eight<X>::load(from[i] + k);
+        }
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < MQ; ++i) {
+            if constexpr (kBytes) v[i] = u32x2{0, 0};
+            else v[i] = typename Eight<X>::Raw{};
+        }
+    }
+    __device__ __forceinline__ void put(Buffer& b, int lane) const {
+        const int c = lane & 15;
+#pragma unroll
+        for (int i = 0; i < MQ; ++i) {
+            const int row = 4 * i + (lane >> 4);
+            if constexpr (kBytes) {
+                // word j = c / 4 of the lane group q = c mod 4: half j mod 2 of the chunk 4 (j / 2) + q
+                u32x2* at = reinterpret_cast<u32x2*>(&b.x[0][row][4 * (c >> 3) + (c & 3)]) + (c >> 2 & 1);
+                *at = u32x2{__builtin_amdgcn_perm(v[i][1], v[i][0], 0x05010400u), __builtin_amdgcn_perm(v[i][1], v[i][0], 0x07030602u)};
+            } else if constexpr (sizeof(X) == 4) {
+                const Pieces p = pieces_of(v[i]);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) b.x[k][row][c] = __builtin_bit_cast(u32x4, p.p[k]);
+            } else {
+                b.x[0][row][c] = __builtin_bit_cast(u32x4, v[i]);
+            }
+        }
+    }
+};
+
+// One workgroup: 16 outputs, up to 4 * MQ rows; its waves take the tiles of the inputs in turn, each with DEPTH of them on their way, and add up in LDS.
+// The matrix cores have 16 columns: with 4 or 8 rows the others go to the next groups.  Column r is row r mod 4 MQ of every (4 / MQ)-th group and zero in the
+// others', so that the sums of up to four groups stand side by side and get their steps and zero points in one go.
+template <typename X, int G, bool ZEROS, int MQ, int DEPTH, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void k_packed_few(ProductArgs a) {
     constexpr int S = kTileIn / G, PER = 4 / S;              // groups of a tile, words of a group
-    constexpr bool kBytes = sizeof(X) == 1, kSums = ZEROS || (!kBytes && Operand<std::conditional_t<kBytes, float, X>>::kMiddle != 8.f);
-    __shared__ float part[WAVES][NT * 4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-    const int tile_out = blockIdx.x, first = blockIdx.y * (16 * NT);
+    using Rows = FewRows<X, MQ>;
+    constexpr int SLOTS = Rows::kSlots, ROWS = Rows::kRows;
+    constexpr int UNIT = S >= SLOTS ? 1 : SLOTS / S, SETS = S >= SLOTS ? S / SLOTS : 1;     // tiles that share sums; sets of sums of a tile
+    static_assert(DEPTH % UNIT == 0, "whole units on their way");
+    constexpr bool kBytes = sizeof(X) == 1, kByGroup = std::is_same_v<X, ByGroup>;
+    __shared__ typename Rows::Buffer buffers[WAVES];
+    __shared__ float part[WAVES][4][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    const int tile_out = blockIdx.x, first = blockIdx.y * 16, mine = r & (ROWS - 1), slot = r / ROWS;
     const PackedView& w = a.w;
-    const u32x4* codes = reinterpret_cast<const u32x4*>(w.codes) + (size_t)tile_out * w.in_tiles * 64 + lane;
-    const u32x4* groups = reinterpret_cast<const u32x4*>(w.groups) + (size_t)tile_out * w.n_groups * 4 + q;
-    float y[NT][4];
+    const int last = w.in_tiles - 1, tail = w.n_in - 8 - last * kTileIn;
+    const char* codes = reinterpret_cast<const char*>(w.codes) + (size_t)tile_out * w.in_tiles * 1024;
+    const char* groups = reinterpret_cast<const char*>(w.groups) + (size_t)tile_out * w.n_groups * 64;
+    typename Rows::Buffer& buffer = buffers[wave];
+    if constexpr (SLOTS > 1) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[t][i] = 0.f;
-    const X* rows[NT];
-    bool in[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int row = first + 16 * t + r;
-        in[t] = row < a.rows;
-        rows[t] = reinterpret_cast<const X*>(a.x) + (long long)min(row, a.rows - 1) * a.x_stride;
+        for (int p = 0; p < Rows::kPlanes; ++p)
+            if (lane <= Rows::kChunks) buffer.x[p][ROWS][lane] = u32x4{0, 0, 0, 0};
     }
-    for (int it = wave; it < w.in_tiles; it += WAVES) {
-        const u32x4 tile = codes[(size_t)it * 64];
-        u32x4 gw[S];
+    const u32x4* column[SLOTS];                              // chunk q of the row, or of the zeros, by the group's slot
 #pragma unroll
-        for (int s = 0; s < S; ++s) gw[s] = groups[(it * S + s) * 4];
-        Rows<X> x[NT];
+    for (int i = 0; i < SLOTS; ++i) column[i] = &buffer.x[0][SLOTS == 1 || slot == i ? mine : ROWS][q];
+    constexpr int kPlane = (ROWS + (SLOTS > 1)) * (Rows::kChunks + 1);
+    // (of rows behind the last one the last one: their columns count for nothing)
+    const X* from[MQ];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) x[t].load(rows[t], it * kTileIn + 8 * q, w.n_in, in[t]);
+    for (int i = 0; i < MQ; ++i) from[i] = reinterpret_cast<const X*>(a.x) + (long long)min(first + 4 * i + (lane >> 4), a.rows - 1) * a.x_stride;
+    const float* scales = kByGroup ? a.x_scales + (long long)min(first + mine, a.rows - 1) * a.x_groups : nullptr;
+
+    float y[4] = {0.f, 0.f, 0.f, 0.f};
+    u32x4 tile[DEPTH], gw[DEPTH / UNIT][SETS];
+    float xs[kByGroup ? DEPTH / UNIT : 1][SETS];
+    Rows rows[DEPTH];
+    auto ask = [&](int d, int it) {
+        const int safe = min(it, last);
+        tile[d] = reinterpret_cast<const u32x4*>(codes + (size_t)safe * 1024)[lane];
+        rows[d].ask(from, safe * kTileIn + min(8 * r, safe == last ? tail : kTileIn));
+        if (d % UNIT == 0) {
+#pragma unroll
+            for (int v = 0; v < SETS; ++v) {
+                // the group that this lane's column belongs to
+                const int g = UNIT == 1 ? safe * S + v * SLOTS + slot : min(it + (slot / S) * WAVES, last) * S + slot % S;
+                gw[d / UNIT][v] = *reinterpret_cast<const u32x4*>(groups + (unsigned)(g * 64 + q * 16));
+                if constexpr (kByGroup) xs[d / UNIT][v] = scales[min(g, a.x_groups - 1)];      // (behind the last group: of a step of 0)
+            }
+        }
+    };
+    using Acc = std::conditional_t<kBytes, i32x4, f32x4>;
+    Acc acc[SETS], sum[SETS];
+    auto take = [&](int d, int it) {
+        if (it == last && 8 * r > tail) rows[d].clear();
+        rows[d].put(buffer, lane);
+        lds_wave_fence();
+        if (d % UNIT == 0) {
+#pragma unroll
+            for (int v = 0; v < SETS; ++v) acc[v] = sum[v] = Acc{0, 0, 0, 0};
+        }
 #pragma unroll
         for (int s = 0; s < S; ++s) {
+            const int v = UNIT == 1 ? s / SLOTS : 0;
+            const u32x4* from_column = column[(d * S + s) % SLOTS];
             if constexpr (kBytes) {
-                i32x4 acc[NT], sum[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[t] = sum[t] = i32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int j = s * PER; j < (s + 1) * PER; j += 2) {
-                    // of a group of 32, the second half of the instruction's inputs is 0
+                for (int h = 0; h < (PER + 1) / 2; ++h) {
+                    const int pair = PER == 1 ? s / 2 : s * PER / 2 + h;       // words 2 pair, 2 pair + 1
                     constexpr unsigned m = 0xf0f0f0f0u;
-                    const unsigned w0 = tile[j], w1 = PER == 1 ? 0u : tile[(j + 1) & 3];
+                    // of a group of 32 the other half of the instruction's inputs counts nothing
+                    const bool no0 = PER == 1 && s % 2, no1 = PER == 1 && s % 2 == 0;
+                    const unsigned w0 = no0 ? 0u : tile[d][2 * pair], w1 = no1 ? 0u : tile[d][2 * pair + 1];
                     const i32x4 c{(int)(w0 << 4 & m), (int)(w0 & m), (int)(w1 << 4 & m), (int)(w1 & m)};
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const u32x2 x0 = x[t].v[j], x1 = PER == 1 ? u32x2{0, 0} : x[t].v[(j + 1) & 3];
-                        const i32x4 b{(int)__builtin_amdgcn_perm(x0[1], x0[0], 0x05010400u), (int)__builtin_amdgcn_perm(x0[1], x0[0], 0x07030602u),
-                                      (int)__builtin_amdgcn_perm(x1[1], x1[0], 0x05010400u), (int)__builtin_amdgcn_perm(x1[1], x1[0], 0x07030602u)};
-                        acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(c, b, acc[t], 0, 0, 0);
-                        if constexpr (ZEROS) {
-                            constexpr int o = 0x10101010;
-                            sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(i32x4{o, o, o, o}, b, sum[t], 0, 0, 0);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    float xs = 0.0625f;
-                    if (a.x_groups > 1) {
-                        const int row = first + 16 * t + r, g = it * S + s;
-                        xs *= in[t] && g < a.x_groups ? a.x_scales[(long long)row * a.x_groups + g] : 0.f;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        int v = acc[t][i];
-                        if constexpr (ZEROS) v -= ((int)(gw[s][i] & 0xffu) - 8) * sum[t][i];
-                        y[t][i] = __builtin_fmaf(step_of(gw[s][i]), (float)v * xs, y[t][i]);
+                    const i32x4 x = __builtin_bit_cast(i32x4, from_column[4 * pair]);
+                    acc[v] = __builtin_amdgcn_mfma_i32_16x16x64_i8(c, x, acc[v], 0, 0, 0);
+                    if constexpr (ZEROS) {
+                        const int o0 = no0 ? 0 : 0x10101010, o1 = no1 ? 0 : 0x10101010;
+                        sum[v] = __builtin_amdgcn_mfma_i32_16x16x64_i8(i32x4{o0, o0, o1, o1}, x, sum[v], 0, 0, 0);
                     }
                 }
             } else {
                 using O = Operand<X>;
-                f32x4 acc[NT], sum[NT];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) acc[t] = sum[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int j = s * PER; j < (s + 1) * PER; ++j) {
-                    const auto c = O::codes(tile[j]);
+                    const auto c = O::codes(tile[d][j]);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        if constexpr (O::kPieces == 3) {
-                            const Pieces b = pieces_of(x[t].v[j]);
-#pragma unroll
-                            for (int k = 2; k >= 0; --k) {
-                                acc[t] = O::mul(c, b.p[k], acc[t]);
-                                if constexpr (kSums) sum[t] = O::mul(O::ones(), b.p[k], sum[t]);
-                            }
-                        } else {
-                            acc[t] = O::mul(c, x[t].v[j], acc[t]);
-                            if constexpr (kSums) sum[t] = O::mul(O::ones(), x[t].v[j], sum[t]);
-                        }
+                    for (int p = O::kPieces - 1; p >= 0; --p) {
+                        const auto x = __builtin_bit_cast(typename O::Word, from_column[p * kPlane + 4 * j]);
+                        acc[v] = O::mul(c, x, acc[v]);
+                        if constexpr (ZEROS) sum[v] = O::mul(O::all(1.f), x, sum[v]);
+                        else if constexpr (O::kMiddle != 8.f) acc[v] = O::mul(O::all(O::kMiddle - 8.f), x, acc[v]);
                     }
                 }
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float v = acc[t][i];
-                        if constexpr (kSums) v = __builtin_fmaf(O::kMiddle - (ZEROS ? zero_of(gw[s][i]) : 8.f), sum[t][i], v);
-                        y[t][i] = __builtin_fmaf(step_of(gw[s][i]), v, y[t][i]);
-                    }
             }
+        }
+        lds_wave_fence();
+    };
+    auto finish = [&](int d) {                               // behind the last tile of a unit, d its first one
+#pragma unroll
+        for (int v = 0; v < SETS; ++v) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned word = gw[d / UNIT][v][i];
+                float s = (float)acc[v][i];
+                if constexpr (ZEROS) s = __builtin_fmaf(Operand<X>::kMiddle - zero_of(word), (float)sum[v][i], s);
+                if constexpr (kByGroup) s *= xs[d / UNIT][v];
+                y[i] = __builtin_fmaf(step_of(word), s, y[i]);
+            }
+        }
+    };
+    // (loads without branches around them: the compiler waits for all of them where it cannot tell how many are on their way)
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) ask(d, wave + d * WAVES);
+    int it = wave;
+    for (; it + DEPTH * WAVES <= last; it += DEPTH * WAVES) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; d += UNIT) {
+#pragma unroll
+            for (int u = 0; u < UNIT; ++u) take(d + u, it + (d + u) * WAVES);
+            finish(d);
+#pragma unroll
+            for (int u = 0; u < UNIT; ++u) ask(d + u, it + (d + u + DEPTH) * WAVES);
         }
     }
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int d = 0; d < DEPTH; d += UNIT) {
+        if (it + d * WAVES > last) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[wave][4 * t + i][lane] = y[t][i];
+        for (int u = 0; u < UNIT; ++u)
+            if (u == 0 || it + (d + u) * WAVES <= last) take(d + u, it + (d + u) * WAVES);
+        finish(d);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[wave][i][lane] = y[i];
     lds_barrier();
-    for (int o = threadIdx.x; o < NT * 256; o += WAVES * 64) {
-        const int t = o >> 8, row = first + 16 * t + ((o >> 4) & 15), n = o & 15, out = tile_out * kTileOut + n;
+    if (threadIdx.x < 16 * ROWS) {
+        const int t = threadIdx.x >> 4, row = first + t, n = threadIdx.x & 15, out = tile_out * kTileOut + n;
         float v = 0.f;
 #pragma unroll
-        for (int k = 0; k < WAVES; ++k) v += part[k][4 * t + (n & 3)][(n >> 2) * 16 + ((o >> 4) & 15)];
+        for (int k = 0; k < WAVES; ++k)
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) v += part[k][n & 3][(n >> 2) * 16 + i * ROWS + t];
         if (row < a.rows && out < w.n_out) {
-            if constexpr (kBytes) {
-                if (a.x_groups == 1) v *= a.x_scales[row];
-            } else {
-                v *= Operand<X>::kUp;
-            }
+            v *= Operand<X>::kUp;
+            if constexpr (kBytes && !kByGroup) v *= a.x_scales[row];
             if (a.bias) v += a.bias[out];
             store_as<X>(a.out, a.out_type, row * a.out_stride + out, v);
         }
@@ -259,18 +339,6 @@ void launch_product_f32(const ProductArgs& a, bool zeros, hipStream_t s);
 void launch_product_f16(const ProductArgs& a, bool zeros, hipStream_t s);
 void launch_product_bf16(const ProductArgs& a, bool zeros, hipStream_t s);
 void launch_product_i8(const ProductArgs& a, bool zeros, hipStream_t s);
-
-template <typename X, int G, bool ZEROS>
-void launch_product_form(const ProductArgs& a, hipStream_t s) {
-    constexpr int NT = 1, WAVES = 8;
-    hipLaunchKernelGGL((k_packed_few<X, G, ZEROS, NT, WAVES>), dim3((a.w.n_out + kTileOut - 1) / kTileOut, (a.rows + 16 * NT - 1) / (16 * NT)),
-                       dim3(WAVES * 64), 0, s, a);
-}
-template <typename X>
-void launch_product_as(const ProductArgs& a, bool zeros, hipStream_t s) {
-    if (a.w.group == 32) zeros ? launch_product_form<X, 32, true>(a, s) : launch_product_form<X, 32, false>(a, s);
-    else if (a.w.group == 64) zeros ? launch_product_form<X, 64, true>(a, s) : launch_product_form<X, 64, false>(a, s);
-    else zeros ? launch_product_form<X, 128, true>(a, s) : launch_product_form<X, 128, false>(a, s);
-}
+void launch_product_i8_groups(const ProductArgs& a, bool zeros, hipStream_t s);
 
 }  // namespace lif

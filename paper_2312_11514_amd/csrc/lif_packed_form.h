@@ -1,0 +1,46 @@
+// Which kernel takes a product, by the number of outputs and rows (host code).
+#pragma once
+
+namespace lif {
+
+// Tiles of 16 outputs for up to 4, 8 or 16 rows, the inputs dealt to the waves (k_packed_few); or workgroups of so many outputs and rows (k_packed_many).
+enum class PackedForm { few4, few8, few16, outs32_rows16, outs64_rows16, outs64_rows32_16, outs64_rows32, outs64_rows48, outs64_rows64, outs128_rows64 };
+
+// A larger workgroup reads and unpacks less for an output, but where there are fewer of them than the 256 compute units its own time is that of the call.
+// So a call is taken to last `alone` where the workgroups fit the chip at once, one to a compute unit, and `more` for every 256 beyond: us for 4096 inputs in fp16 with
+// groups of 128, in fp32 with groups of 64 and zero points, from 17 to 1024 rows by 1024 to 50000 outputs.  Other inputs, types and groups scale them alike: with
+// the rule the time is that of the fastest form, or within a tenth of it (bf16 with groups of 32, bytes with scales by groups of 64).
+// E.g. 4096 outputs, fp16: 24 rows 5.8 (few16 6.3, outs64_rows32_16 9.5), 128 rows 10.6 (outs32_rows16 13.7, outs64_rows64 16.9), 512 rows 28.9 (outs64_rows32
+// 31.0, outs64_rows64 29.2); 50000 outputs: 24 rows 29.5 (few16 50.8, outs64_rows64 43.6), 512 rows 292 (outs64_rows32 379, outs64_rows64 326).
+struct PackedCost {
+    PackedForm form;
+    int tiles, rows;             // of a workgroup
+    float alone, more;
+};
+constexpr PackedCost kPackedCosts[] = {
+    {PackedForm::few16, 1, 16, 4.4f, 2.1f},           {PackedForm::outs32_rows16, 2, 16, 5.7f, 3.1f},  {PackedForm::outs64_rows32_16, 4, 32, 9.4f, 9.0f},
+    {PackedForm::outs64_rows32, 4, 32, 10.3f, 7.8f},  {PackedForm::outs64_rows48, 4, 48, 13.2f, 10.8f}, {PackedForm::outs64_rows64, 4, 64, 16.5f, 13.2f},
+    {PackedForm::outs128_rows64, 8, 64, 26.f, 23.1f}};
+constexpr PackedCost kPackedCostsF32[] = {
+    {PackedForm::few16, 1, 16, 11.5f, 6.2f}, {PackedForm::outs32_rows16, 2, 16, 13.4f, 12.f}, {PackedForm::outs64_rows16, 4, 16, 19.5f, 13.3f},
+    {PackedForm::outs128_rows64, 8, 64, 70.f, 75.f}};
+
+// tiles: of 16 outputs
+inline PackedForm packed_form(int tiles, int rows, bool f32, int group) {
+    if (rows <= 16) return rows <= 4 ? PackedForm::few4 : rows <= 8 ? PackedForm::few8 : PackedForm::few16;
+    PackedForm best = PackedForm::few16;
+    float least = 0.f;
+    auto look = [&](const PackedCost& c) {
+        if (c.form == PackedForm::outs64_rows64 && group == 32) return;      // (registers to memory: 28 us instead of 16 alone)
+        const float groups = (float)((tiles + c.tiles - 1) / c.tiles) * (float)((rows + c.rows - 1) / c.rows) / 256.f;
+        const float time = c.alone + c.more * (groups > 1.f ? groups - 1.f : 0.f);
+        if (least == 0.f || time < least) best = c.form, least = time;
+    };
+    if (f32)
+        for (const PackedCost& c : kPackedCostsF32) look(c);
+    else
+        for (const PackedCost& c : kPackedCosts) look(c);
+    return best;
+}
+
+}  // namespace lif

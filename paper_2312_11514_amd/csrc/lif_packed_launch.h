@@ -1,0 +1,49 @@
+// Which kernel takes a product.
+#pragma once
+
+#include "lif_packed_few.h"
+#include "lif_packed_form.h"
+#include "lif_packed_many.h"
+
+namespace lif {
+
+template <typename X, int G, bool ZEROS>
+void launch_product_form(const ProductArgs& a, hipStream_t s) {
+    const int tiles = (a.w.n_out + kTileOut - 1) / kTileOut;
+    constexpr bool kF32 = sizeof(X) == 4;
+    constexpr int kWide = kF32 ? 2 : 1;
+    auto go = [&](auto kernel, int outs, int rows, int waves) {
+        hipLaunchKernelGGL(kernel, dim3((tiles + outs - 1) / outs, (a.rows + rows - 1) / rows), dim3(waves * 64), 0, s, a);
+    };
+    const PackedForm f = packed_form(tiles, a.rows, kF32, G);
+    switch (f) {
+        case PackedForm::few4: return go(k_packed_few<X, G, ZEROS, 1, 4, 8>, 1, 16, 8);
+        case PackedForm::few8: return go(k_packed_few<X, G, ZEROS, 2, 4 / kWide, 8>, 1, 16, 8);
+        case PackedForm::few16: return go(k_packed_few<X, G, ZEROS, 4, 2 / kWide, 8 / kWide>, 1, 16, 8 / kWide);
+        case PackedForm::outs32_rows16: return go(k_packed_many<X, G, ZEROS, 1, 2, 4>, 2, 16, 8);
+        case PackedForm::outs128_rows64: return go(k_packed_many<X, G, ZEROS, 4, 8, 1>, 8, 64, 8);
+        case PackedForm::outs64_rows16:
+            if constexpr (kF32) return go(k_packed_many<X, G, ZEROS, 1, 4, 2>, 4, 16, 8);
+            break;
+        case PackedForm::outs64_rows32_16:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 2, 4, 4>, 4, 32, 16);
+            break;
+        case PackedForm::outs64_rows32:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 2, 4, 2>, 4, 32, 8);
+            break;
+        case PackedForm::outs64_rows48:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 3, 4, 2>, 4, 48, 8);
+            break;
+        case PackedForm::outs64_rows64:
+            if constexpr (!kF32 && G > 32) return go(k_packed_many<X, G, ZEROS, 4, 4, 2>, 4, 64, 8);
+            break;
+    }
+}
+template <typename X>
+void launch_product_as(const ProductArgs& a, bool zeros, hipStream_t s) {
+    if (a.w.group == 32) zeros ? launch_product_form<X, 32, true>(a, s) : launch_product_form<X, 32, false>(a, s);
+    else if (a.w.group == 64) zeros ? launch_product_form<X, 64, true>(a, s) : launch_product_form<X, 64, false>(a, s);
+    else zeros ? launch_product_form<X, 128, true>(a, s) : launch_product_form<X, 128, false>(a, s);
+}
+
+}  // namespace lif

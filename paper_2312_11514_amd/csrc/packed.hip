@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kMaxWidth = 65536, kMaxOut = 1 << 20, kMaxRows = 1 << 19;
 constexpr int kMakeBlocks = 2048;                // 8 workgroups per compute unit
-constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxStride = (int64_t)1 << 40, kMaxXStride = 1 << 22;
 
 int bytes_of(int dtype) { return dtype == LIF_F32 ? 4 : 2; }
 bool dtype_ok(int dtype) { return dtype == LIF_F32 || dtype == LIF_F16 || dtype == LIF_BF16; }
@@ -201,8 +201,10 @@ int lif_packed_multiply(lif_packed* p, const lif_packed_rows* rows, void* stream
         return fail(LIF_INVALID_ARG, "x_group must be 0 or the group of the weights, with scales");
     const bool eight = rows->x_scales != nullptr;
     const int e = bytes_of(c.dtype), x_e = eight ? 1 : e;
-    if (!aligned(rows->x, eight ? 8 : 16) || !stride_ok(rows->x_stride, c.n_in, x_e, eight ? 8 : 16))
-        return fail(LIF_INVALID_ARG, "rows of x must be 16-byte aligned at a stride that holds them and is a multiple of 16 bytes (8 bits: 8 and 8)");
+    // (with one row there is no stride; more than 2^22 elements would take offsets of 64 bits)
+    const int64_t x_stride = rows->n_rows == 1 ? c.n_in : rows->x_stride;
+    if (!aligned(rows->x, eight ? 8 : 16) || !stride_ok(rows->x_stride, c.n_in, x_e, eight ? 8 : 16) || x_stride > kMaxXStride)
+        return fail(LIF_INVALID_ARG, "rows of x must be 16-byte aligned at a stride that holds them, is a multiple of 16 bytes (8 bits: 8 and 8), at most 2^22");
     if (!aligned(rows->out, e) || rows->out_stride < c.n_out || rows->out_stride > kMaxStride)
         return fail(LIF_INVALID_ARG, "rows of out must be aligned to their elements, at a stride that holds them");
     if (!aligned(rows->x_scales, 4) || !aligned(rows->bias, 4)) return fail(LIF_INVALID_ARG, "fp32 arrays must be 4-byte aligned");
@@ -211,11 +213,12 @@ int lif_packed_multiply(lif_packed* p, const lif_packed_rows* rows, void* stream
         scales{rows->x_scales, groups * 4, groups * 4, rows->n_rows}, bias{rows->bias, c.n_out * 4ll, c.n_out * 4ll, 1};
     if (overlap(out, x) || (scales.at && overlap(out, scales)) || (bias.at && overlap(out, bias)))
         return fail(LIF_INVALID_ARG, "out must not overlap x, its scales or the bias");
-    const ProductArgs a{p->view, static_cast<const char*>(rows->x), static_cast<char*>(rows->out), rows->x_scales, rows->bias, rows->x_stride,
+    const ProductArgs a{p->view, static_cast<const char*>(rows->x), static_cast<char*>(rows->out), rows->x_scales, rows->bias, x_stride,
                         rows->out_stride, rows->n_rows, (int32_t)groups, c.dtype};
     hipStream_t s = (hipStream_t)stream;
     const bool z = c.zeros != 0;
-    if (eight) launch_product_i8(a, z, s);
+    if (eight && groups > 1) launch_product_i8_groups(a, z, s);
+    else if (eight) launch_product_i8(a, z, s);
     else if (c.dtype == LIF_F32) launch_product_f32(a, z, s);
     else if (c.dtype == LIF_F16) launch_product_f16(a, z, s);
     else launch_product_bf16(a, z, s);

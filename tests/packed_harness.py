@@ -10,7 +10,7 @@ DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 UNIT = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}       # largest relative error of one rounding
 TINY = {"f32": 2.0 ** -149, "f16": 2.0 ** -24, "bf16": 2.0 ** -133}    # smallest step of the type
 NORMS = {"none": lif.NORM_NONE, "rms": lif.NORM_RMS, "layer": lif.NORM_LAYER}
-MIDDLE = {"f32": 8.0, "f16": 8.0, "bf16": -16.0, "i8": 8.0}            # the code that counts nothing
+MIDDLE = {"f32": 8.0, "f16": -64.0, "bf16": -128.0, "i8": 8.0}          # the code that counts nothing, at most
 
 
 def values(rng, shape, dtype, size=1.0):
