@@ -132,7 +132,7 @@ EXPORTS = {
     "lif_kv_attend": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(LifKvQuery), C.c_void_p]),
     "lif_kv_set_expected_tokens": (C.c_int, [C.c_void_p, C.c_int32]),
     "lif_kv_get_state": (C.c_int, [C.c_void_p, C.POINTER(LifKvState), C.c_void_p]),
-    "lif_add_norm": (C.c_int, [C.POINTER(LifNormRows), C.c_void_p]),
+    "lif_add_norm": (C.c_int, [C.c_void_p, C.c_void_p]),            # (a pointer to the structure, or the bytes of one)
     "lif_packed_code_bytes": (C.c_size_t, [C.POINTER(LifPackedConfig)]),
     "lif_packed_group_bytes": (C.c_size_t, [C.POINTER(LifPackedConfig)]),
     "lif_packed_create": (C.c_int, [C.POINTER(LifPackedConfig), C.POINTER(LifPackedBuffers), C.POINTER(C.c_void_p)]),
@@ -140,7 +140,7 @@ EXPORTS = {
     "lif_packed_quantize": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     "lif_packed_pack": (C.c_int, [C.c_void_p] * 5),
     "lif_packed_dequantize": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
-    "lif_packed_multiply": (C.c_int, [C.c_void_p, C.POINTER(LifPackedRows), C.c_void_p]),
+    "lif_packed_multiply": (C.c_int, [C.c_void_p] * 3),
     "lif_rope_frequencies": (C.c_int, [C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4 + [C.POINTER(C.c_double)]),
 }
 

@@ -18,7 +18,7 @@ import struct
 from . import binding as _b
 from .binding import LIF_INVALID_ARG, LifError
 
-# lif_norm_rows and lif_packed_rows, filled in one go, as those of the key-value cache are
+# lif_norm_rows and lif_packed_rows, filled in one go; the bytes themselves are the argument, so that threads share none
 _NORM, _PRODUCT = struct.Struct("@7P4q5if"), struct.Struct("@4P2q2i")
 assert _NORM.size == C.sizeof(_b.LifNormRows) and _PRODUCT.size == C.sizeof(_b.LifPackedRows)
 
@@ -64,16 +64,14 @@ def _stride(t, what):
     _refuse(f"{what} must have its elements one after the other and its rows at one stride")
 
 
-def _row_scales(scales, rows, width, group, device):
-    groups = -(-width // group) if group else 1
-    if scales.dtype is not _Torch.float32 or scales.numel() != rows * groups or scales.get_device() != device or not scales.is_contiguous():
-        _refuse(f"scales must be a contiguous float32 tensor of {rows} x {groups} elements beside the rows")
-    return scales.data_ptr()
+def _like(t, shape, dtype, device, what):
+    """The stride of rows that have to be as others are."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _refuse(f"{what} must be {list(shape)} of {dtype} beside the rows")
+    return shape[-1] if t.is_contiguous() else _stride(t, what)
 
 
-def _vector(t, n, device, what):
-    if t is None:
-        return 0
+def _floats(t, n, device, what):
     if t.dtype is not _Torch.float32 or t.numel() != n or t.get_device() != device or not t.is_contiguous():
         _refuse(f"{what} must be a contiguous float32 tensor of {n} elements beside the rows")
     return t.data_ptr()
@@ -94,25 +92,21 @@ def add_norm(x, out, *, norm=_b.NORM_RMS, eps=1e-5, weight=None, bias=None, resi
         _refuse("x must be on the current GPU")
     width = shape[-1]
     rows = x.numel() // width if width else 0
-    if out.shape != shape or out.dtype is not (dtype if scales is None else _Torch.int8) or out.get_device() != device:
-        _refuse("out must be as x is (int8 if there are scales)")
     r_ptr = r_stride = t_ptr = t_stride = s_ptr = 0
-    if residual is not None:
-        if residual.shape != shape or residual.dtype is not dtype or residual.get_device() != device:
-            _refuse("residual must be as x is")
-        r_ptr, r_stride = residual.data_ptr(), _stride(residual, "residual")
-    if total is not None:
-        if total.shape != shape or total.dtype is not dtype or total.get_device() != device:
-            _refuse("total must be as x is")
-        t_ptr, t_stride = total.data_ptr(), _stride(total, "total")
-    if scales is not None:
+    if scales is None:
+        out_stride = _like(out, shape, dtype, device, "out")
+    else:
         if group not in (0, 32, 64, 128):
             _refuse("group must be 0, 32, 64 or 128")
-        s_ptr = _row_scales(scales, rows, width, group, device)
-    args = _b.LifNormRows()
-    _NORM.pack_into(args, 0, x.data_ptr(), r_ptr, t_ptr, out.data_ptr(), s_ptr, _vector(weight, width, device, "weight"),
-                    _vector(bias, width, device, "bias"), _stride(x, "x"), r_stride, t_stride, _stride(out, "out"), rows, width, code, norm, group, eps)
-    rc = _Torch.add_norm(C.byref(args), _b._stream())
+        out_stride = _like(out, shape, _Torch.int8, device, "out")
+        s_ptr = _floats(scales, rows * (-(-width // group) if group else 1), device, "scales")
+    if residual is not None:
+        r_ptr, r_stride = residual.data_ptr(), _like(residual, shape, dtype, device, "residual")
+    if total is not None:
+        t_ptr, t_stride = total.data_ptr(), _like(total, shape, dtype, device, "total")
+    rc = _Torch.add_norm(_NORM.pack(x.data_ptr(), r_ptr, t_ptr, out.data_ptr(), s_ptr, _floats(weight, width, device, "weight") if weight is not None else 0,
+                                    _floats(bias, width, device, "bias") if bias is not None else 0, _stride(x, "x"), r_stride, t_stride, out_stride,
+                                    rows, width, code, norm, group, eps), _b._stream())
     if rc:
         _b._check(rc)
 
@@ -187,20 +181,21 @@ class PackedLinear:
     def multiply(self, x, out, bias=None, scales=None):
         """lif_packed_multiply: out [..., n_out] = x [..., n_in] times the matrix (+ bias, float32 [n_out]).  x is of the matrix's type, or int8 with scales,
         float32, [rows] or [rows, groups of a row]."""
-        self._here()
-        shape, device = x.shape, self._gpu
-        if not shape or shape[-1] != self.n_in or x.dtype is not (self.tdtype if scales is None else _Torch.int8) or x.get_device() != device:
-            _refuse(f"x must be [..., {self.n_in}] of the matrix's type (int8 if there are scales) beside it")
-        if out.shape[-1:] != (self.n_out,) or out.shape[:-1] != shape[:-1] or out.dtype is not self.tdtype or out.get_device() != device:
-            _refuse(f"out must be [..., {self.n_out}] of the matrix's type, its leading dimensions those of x")
-        rows = x.numel() // self.n_in
+        shape, device, dtype, n_in = x.shape, self._gpu, self.tdtype, self.n_in
+        if device < 0 or device != _Torch.device():
+            _refuse("the weights must be on the current GPU")
+        if not shape or shape[-1] != n_in or x.dtype is not (dtype if scales is None else _Torch.int8) or x.get_device() != device:
+            _refuse(f"x must be [..., {n_in}] of the matrix's type (int8 if there are scales) beside it")
+        rows = x.numel() // n_in
         s_ptr = x_group = 0
         if scales is not None:
-            x_group = self.group if self.row_groups > 1 and scales.numel() != rows else 0
-            s_ptr = _row_scales(scales, rows, self.n_in, x_group, device)
-        args = _b.LifPackedRows()
-        _PRODUCT.pack_into(args, 0, x.data_ptr(), s_ptr, _vector(bias, self.n_out, device, "bias"), out.data_ptr(), _stride(x, "x"), _stride(out, "out"),
-                           rows, x_group)
-        rc = _Torch.multiply(self.handle, C.byref(args), _b._stream())
+            groups = self.row_groups
+            if groups > 1 and scales.numel() != rows:
+                x_group, s_ptr = self.group, _floats(scales, rows * groups, device, "scales")
+            else:
+                s_ptr = _floats(scales, rows, device, "scales")
+        rc = _Torch.multiply(self.handle, _PRODUCT.pack(
+            x.data_ptr(), s_ptr, _floats(bias, self.n_out, device, "bias") if bias is not None else 0, out.data_ptr(), _stride(x, "x"),
+            _like(out, (*shape[:-1], self.n_out), dtype, device, "out"), rows, x_group), _b._stream())
         if rc:
             _b._check(rc)
