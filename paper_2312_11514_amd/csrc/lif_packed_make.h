@@ -5,13 +5,12 @@
 
 namespace lif {
 
-// a word of 8 codes - 8 from two's complements in v[0..8)
-__device__ __forceinline__ unsigned word_of(const int (&v)[8]) {
-    unsigned w = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w |= ((unsigned)v[i] & 15u) << (4 * (i >> 1) + 16 * (i & 1));
-    return w;
+// a word of eight codes - 8, two's complements in the lowest bits
+__device__ __forceinline__ unsigned word_of(const float (&t)[8]) {
+    const unsigned low = low_bytes(t[0], t[4], t[1], t[5]), high = low_bytes(t[2], t[6], t[3], t[7]);
+    return (low & 0x0f0f0f0fu) | (high << 4 & 0xf0f0f0f0u);
 }
+
 // 256 threads have a tile: thread (r, c) = (tid / 16, tid mod 16) the inputs 8 c .. 8 c + 7 of output r.
 struct TilePlace {
     int row, chunk, at;                                  // output, chunk, input
@@ -37,46 +36,46 @@ __device__ __forceinline__ unsigned* group_word(const PackedView& w, int tile, i
 template <typename T, bool ZEROS>
 __global__ __launch_bounds__(256) void k_packed_quantize(PackedView w, const T* __restrict__ from, long long stride, int tiles) {
 #pragma clang fp contract(off)
+    typename Eight<T>::Raw next{};
+    auto ask = [&](int tile) {
+        const TilePlace p = tile_place(w, min(tile, tiles - 1));
+        next = Eight<T>::load(from + min(p.row, w.n_out - 1) * stride + min(p.at, w.n_in - 8));
+    };
+    ask(blockIdx.x);
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const TilePlace p = tile_place(w, tile);
         float v[8];
-        if (p.in) {
-            const auto raw = Eight<T>::load(from + p.row * stride + p.at);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (float)raw[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.f;
-        }
+        for (int e = 0; e < 8; ++e) v[e] = p.in ? (float)next[e] : 0.f;
+        ask(tile + gridDim.x);
         const int lanes = w.group / 8;
-        int code[8];
-        float step, zero = 8.f;
+        float step, zero = 8.f, t[8];
         if constexpr (ZEROS) {
-            unsigned low = 0, high = 0;                      // magnitudes of the lowest below zero and of the highest above
+            // Bits of numbers above zero are ordered as whole numbers, those below zero, as unsigned ones, by their magnitudes; NaN is beyond infinity in both.
+            unsigned low = 0;
+            int high = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (v[e] < 0.f) low = max(low, magnitude_bits(v[e]));
-                else high = max(high, magnitude_bits(v[e]));      // (NaN among them)
+                low = max(low, __builtin_bit_cast(unsigned, v[e]));
+                high = max(high, __builtin_bit_cast(int, v[e]));
             }
             low = lanes_max(low, lanes);
-            high = lanes_max(high, lanes);
-            const float lowest = __builtin_bit_cast(float, low), highest = __builtin_bit_cast(float, high);
+            const float highest = __builtin_bit_cast(float, lanes_max((unsigned)high, lanes)), lowest = low >> 31 ? __builtin_bit_cast(float, low & 0x7fffffffu) : 0.f;
             step = grid_step((highest + lowest) * (1.f / 15.f));
-            const float inverse = 1.f / step;
-            if (step > 0.f) zero = fminf(nearest(lowest, step, inverse), 15.f);
+            if (step > 0.f) zero = fminf(nearest(lowest, step, 1.f / step), 15.f);
+            nearest_of(v, step, t);
+            // a code between 0 and 15, and 8 less than that: the whole number between -zero and 15 - zero, and zero - 8 more
 #pragma unroll
-            for (int e = 0; e < 8; ++e) code[e] = step > 0.f ? min(max((int)nearest(v[e], step, inverse) + (int)zero, 0), 15) - 8 : (int)zero - 8;
+            for (int e = 0; e < 8; ++e) t[e] = __builtin_amdgcn_fmed3f(t[e], kWhole - zero, kWhole + (15.f - zero)) + (zero - 8.f);
         } else {
             unsigned most = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) most = max(most, magnitude_bits(v[e]));
             most = lanes_max(most, lanes);
             step = grid_step(__builtin_bit_cast(float, most) * (1.f / 7.f));
-            const float inverse = 1.f / step;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) code[e] = step > 0.f ? (int)nearest(v[e], step, inverse) : 0;
+            nearest_of(v, step, t);
         }
-        *tile_word(w, tile) = word_of(code);
+        *tile_word(w, tile) = word_of(t);
         if (p.chunk % lanes == 0) *group_word(w, tile, p.at) = (__builtin_bit_cast(unsigned, step) & ~0xffu) | (unsigned)zero;
     }
 }
@@ -89,10 +88,11 @@ __global__ __launch_bounds__(256) void k_packed_pack(PackedView w, const unsigne
         const TilePlace p = tile_place(w, tile);
         unsigned four = 0x88888888u;
         if (p.in) four = *reinterpret_cast<const unsigned*>(codes + (size_t)p.row * (w.n_in / 2) + p.at / 2);
-        int code[8];
+        // pairs (2 p, 2 p + 1) lie side by side, and go to bits 4 p and 16 + 4 p; a code's two's complement less 8 has its upper bit turned over
+        unsigned word = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) code[e] = (int)(four >> 4 * e & 15u) - 8;
-        *tile_word(w, tile) = word_of(code);
+        for (int i = 0; i < 8; ++i) word |= (four >> 4 * i & 15u) << (4 * (i >> 1) + 16 * (i & 1));
+        *tile_word(w, tile) = word ^ 0x88888888u;
         if (p.chunk % (w.group / 8) == 0) {
             const size_t g = (size_t)p.row * row_groups + p.at / w.group;
             float step = 0.f;

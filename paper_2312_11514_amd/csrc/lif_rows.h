@@ -68,12 +68,41 @@ __device__ __forceinline__ float grid_step(float v) {
     return __builtin_fabsf(s) < 0x1p-110f ? 0.f : s;
 }
 
-// The whole number nearest to v / step, of two the even one, exactly; `inverse` is 1 / step, rounded, |v / step| < 128, step > 0.
+// The whole number nearest to v / step, of two the even one, exactly; `inverse` is 1 / step to 2^-22, |v / step| < 128, step > 0.
 __device__ __forceinline__ float nearest(float v, float step, float inverse) {
     const float below = __builtin_floorf(v * inverse);       // may be off by one where v is next to a multiple: nearest to the half, all the same
     const float half = (below + 0.5f) * step;
     const bool odd = ((int)below & 1) != 0;
     return v > half || (v == half && odd) ? below + 1.f : below;
+}
+// The lowest bytes of four.
+__device__ __forceinline__ unsigned low_bytes(float a, float b, float c, float d) {
+    auto two = [](float x, float y) { return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, y), __builtin_bit_cast(unsigned, x), 0x0c0c0400u); };
+    return __builtin_amdgcn_perm(two(c, d), two(a, b), 0x05040100u);
+}
+// The same of eight, as t with t - kWhole the whole number and its two's complement in the lowest bits of t.  Nearly always the product with the inverse is
+// further from a half than the 2^-15 it may be off by, and adding kWhole rounds it; a wave that has one nearer to a half looks at its own again.
+// No step (0, or not a number): 0.
+constexpr float kWhole = 12582912.f;         // 1.5 * 2^23: its neighbours are whole numbers
+__device__ __forceinline__ void nearest_of(const float (&v)[8], float step, float (&t)[8]) {
+#pragma clang fp contract(off)
+    const bool some = step > 0.f;
+    const float inverse = __builtin_amdgcn_rcpf(step);
+    float far = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float q = v[e] * inverse;
+        t[e] = q + kWhole;
+        far = fmaxf(far, __builtin_fabsf(q - (t[e] - kWhole)));
+    }
+    if (far > 0.4999f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = nearest(v[e], step, inverse) + kWhole;
+    }
+    if (!some) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = kWhole;
+    }
 }
 
 }  // namespace lif

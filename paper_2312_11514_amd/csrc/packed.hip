@@ -110,11 +110,11 @@ int lif_add_norm(const lif_norm_rows* n, void* stream) {
     const bool norm = n->norm != LIF_NORM_NONE;
     const NormArgs a{static_cast<const char*>(n->x), static_cast<const char*>(n->residual), static_cast<char*>(n->total), static_cast<char*>(n->out),
                      n->scales, norm ? n->weight : nullptr, n->norm == LIF_NORM_LAYER ? n->bias : nullptr, n->x_stride, n->residual_stride,
-                     n->total_stride, n->out_stride, groups, n->width, n->norm, n->group, n->eps};
+                     n->total_stride, n->out_stride, groups, n->n_rows, n->width, n->norm, n->group, n->eps};
     hipStream_t s = (hipStream_t)stream;
-    if (n->dtype == LIF_F32) launch_add_norm_f32(a, n->n_rows, s);
-    else if (n->dtype == LIF_F16) launch_add_norm_f16(a, n->n_rows, s);
-    else launch_add_norm_bf16(a, n->n_rows, s);
+    if (n->dtype == LIF_F32) launch_add_norm_f32(a, s);
+    else if (n->dtype == LIF_F16) launch_add_norm_f16(a, s);
+    else launch_add_norm_bf16(a, s);
     return launched();
 }
 
