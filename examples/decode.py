@@ -2,6 +2,7 @@
 its neuron cache (Layer).  Random weights; what it shows is the order of the calls.
 
     python examples/decode.py
+    python examples/decode.py --packed         # projections and logits with weights in 4 bits, norms with the residual's addition in one call
 
     prompts in pieces      reserve -> per layer: append (norms, rotation, keys and values into their pages), attend, FFN
     beams                  fork: sequences that share the pages of a prompt
@@ -30,16 +31,21 @@ FFN_ROWS = 8          # tokens that one FFN step takes
 
 
 class Decoder:
-    """Layers of: x += attention(norm(x)); x += ffn(norm(x)).  Sequences are slots of the key-value cache."""
+    """Layers of: x += attention(norm(x)); x += ffn(norm(x)).  Sequences are slots of the key-value cache.  packed: the resident matrices in 4 bits, and the
+    rows that they take in 8."""
 
     def __init__(self, *, layers=2, d_model=512, d_ffn=2048, heads=8, kv_heads=2, vocabulary=1000, page_tokens=16, pages=64, max_seqs=8, max_pages=16,
-                 max_tokens=16, dense=False, seed=0):
+                 max_tokens=16, dense=False, packed=False, seed=0):
         self.heads, self.kv_heads, self.dim, self.seqs = heads, kv_heads, d_model // heads, max_seqs
         gen = torch.Generator().manual_seed(seed)
         rand = lambda *shape: (torch.randn(*shape, generator=gen) / shape[0] ** 0.5).half().cuda()
         self.embedding = (torch.randn(vocabulary, d_model, generator=gen)).half().cuda()
         self.qkv = [rand(d_model, (heads + 2 * kv_heads) * self.dim) for _ in range(layers)]
         self.out = [rand(d_model, d_model) for _ in range(layers)]
+        self.packed = packed
+        if packed:
+            self.qkv, self.out = ([_packed(w.T.contiguous()) for w in ws] for ws in (self.qkv, self.out))
+            self.head = _packed(self.embedding)
         self.norm = [tuple(torch.ones(self.dim, device="cuda") if i % 2 == 0 else None for i in range(4)) for _ in range(layers)]
         self.kv = lif.KVCache(layers=layers, heads=heads, kv_heads=kv_heads, head_dim=self.dim, page_tokens=page_tokens, pages=pages, max_seqs=max_seqs,
                               max_pages=max_pages, max_tokens=max_tokens, norm=lif.NORM_RMS, rotary_dim=self.dim,
@@ -64,6 +70,9 @@ class Decoder:
         of_slot = torch.tensor(slots, dtype=torch.int32).cuda()
         self.kv.reserve(counts)
         x = self.embedding[rows]                                                  # [slots, longest, d_model]
+        if self.packed:
+            logits = self._step_packed(x, valid, of_slot)
+            return {s: logits[i, :len(tokens[s])] for i, s in enumerate(slots)}
         h, k = self.heads, self.kv_heads
         for l in range(len(self.ffn)):
             qkv = _normed(x) @ self.qkv[l]
@@ -82,6 +91,38 @@ class Decoder:
         logits = (_normed(x) @ self.embedding.T.contiguous()).float()
         return {s: logits[i, :len(tokens[s])] for i, s in enumerate(slots)}
 
+    def _step_packed(self, x, valid, of_slot):
+        """The same layers: every norm adds what the half before it has left, and the rows that a matrix in 4 bits takes are rounded to 8 bits."""
+        d, shape = x.shape[-1], x.shape[:-1]
+        make = lambda *more, dtype=torch.float16: torch.empty(*shape, *more, dtype=dtype, device="cuda")
+        codes, scales, normed, y = make(d, dtype=torch.int8), make(1, dtype=torch.float32), make(d), None
+        qkv = make((self.heads + 2 * self.kv_heads) * self.dim)
+        q, key, value = (t.unflatten(-1, (-1, self.dim)) for t in
+                         qkv.split((self.heads * self.dim, self.kv_heads * self.dim, self.kv_heads * self.dim), -1))
+        turned, mixed = make(self.heads, self.dim), make(self.heads, self.dim)
+        for l in range(len(self.ffn)):
+            if y is None:
+                lif.add_norm(x, codes, scales=scales)
+            else:
+                lif.add_norm(y, codes, residual=x, total=x, scales=scales)
+            self.qkv[l].multiply(codes, qkv, scales=scales)
+            self.kv.append(l, q, key, value, turned, norm=self.norm[l], slots=of_slot)
+            self.kv.attend(l, turned, mixed, slots=of_slot)
+            lif.add_norm(mixed.flatten(-2), codes, norm=lif.NORM_NONE, scales=scales)
+            y = make(d)
+            self.out[l].multiply(codes, y, scales=scales)
+            lif.add_norm(y, normed, residual=x, total=x)
+            flat = normed.flatten(0, 1)[valid]
+            ffn = torch.empty_like(flat)
+            for at in range(0, len(flat), FFN_ROWS):
+                self.ffn[l].layer.step(flat[at:at + FFN_ROWS], ffn[at:at + FFN_ROWS], min(FFN_ROWS, len(flat) - at))
+            y = torch.zeros_like(normed)
+            y.view(-1, d)[valid] = ffn
+        lif.add_norm(y, normed, residual=x, total=x)
+        logits = make(self.head.n_out)
+        self.head.multiply(normed, logits)
+        return logits.float()
+
     def truncate(self, lengths):
         """{slot: tokens to keep}"""
         self.kv.truncate(torch.tensor([lengths.get(s, -1) for s in range(self.seqs)], dtype=torch.int32).cuda())
@@ -89,6 +130,12 @@ class Decoder:
     def fork(self, source, slots):
         make = lambda v: torch.tensor(v, dtype=torch.int32).cuda()
         self.kv.fork(make([source] * len(slots)), make(slots))
+
+
+def _packed(weight):
+    matrix = lif.PackedLinear(*weight.shape, group=64, zeros=True)
+    matrix.quantize(weight)
+    return matrix
 
 
 def _normed(x):
@@ -140,7 +187,7 @@ def main(steps=16, drafted=4, **options):
 
 
 if __name__ == "__main__":
-    result = main()
+    result = main(packed="--packed" in sys.argv[1:])
     print("decode step of 5 sequences, 2 layers: %.0f us (eager)" % result["us_per_step"])
     print("%d of 4 drafted tokens accepted; pages in use %d -> %d after two sequences ended, %d moved" %
           (result["accepted"], result["pages_before"], result["pages"], result["moved"]))

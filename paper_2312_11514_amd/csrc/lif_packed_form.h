@@ -7,9 +7,10 @@ namespace lif {
 enum class PackedForm { few4, few8, few16, outs32_rows16, outs64_rows16, outs64_rows32_16, outs64_rows32, outs64_rows48, outs64_rows64, outs128_rows64 };
 
 // A larger workgroup reads and unpacks less for an output, but where there are fewer of them than the 256 compute units its own time is that of the call.
-// So a call is taken to last `alone` where the workgroups fit the chip at once, one to a compute unit, and `more` for every 256 beyond: us for 4096 inputs in fp16 with
-// groups of 128, in fp32 with groups of 64 and zero points, from 17 to 1024 rows by 1024 to 50000 outputs.  Other inputs, types and groups scale them alike: with
-// the rule the time is that of the fastest form, or within a tenth of it (bf16 with groups of 32, bytes with scales by groups of 64).
+// So a call is taken to last `alone` where the workgroups fit the chip at once, one to a compute unit, and `more` for every 256 beyond, three quarters of it for the
+// first of them (outs128_rows64: 256 workgroups 28.4 us, 258 42.8, 512 45.0): us for 4096 inputs in fp16 with groups of 128, in fp32 with groups of 64 and zero points, from 17 to 1024 rows by 1024 to 50000 outputs.  Other inputs, types and groups scale them
+// alike: against the fastest of 15 forms that were tried the rule's choice loses 2 % on average and 15 % at most in fp16, in bf16 with groups of 32 and in bytes with
+// scales by groups of 64; in fp32 11 % and 39 % (50000 outputs: two tiles of outputs to a wave, which is not compiled).
 // E.g. 4096 outputs, fp16: 24 rows 5.8 (few16 6.3, outs64_rows32_16 9.5), 128 rows 10.6 (outs32_rows16 13.7, outs64_rows64 16.9), 512 rows 28.9 (outs64_rows32
 // 31.0, outs64_rows64 29.2); 50000 outputs: 24 rows 29.5 (few16 50.8, outs64_rows64 43.6), 512 rows 292 (outs64_rows32 379, outs64_rows64 326).
 struct PackedCost {
@@ -33,7 +34,8 @@ inline PackedForm packed_form(int tiles, int rows, bool f32, int group) {
     auto look = [&](const PackedCost& c) {
         if (c.form == PackedForm::outs64_rows64 && group == 32) return;      // (registers to memory: 28 us instead of 16 alone)
         const float groups = (float)((tiles + c.tiles - 1) / c.tiles) * (float)((rows + c.rows - 1) / c.rows) / 256.f;
-        const float time = c.alone + c.more * (groups > 1.f ? groups - 1.f : 0.f);
+        const float beyond = groups > 1.f ? groups - 1.f : 0.f, begun = (float)(long long)beyond + ((float)(long long)beyond < beyond ? 1.f : 0.f);
+        const float time = c.alone + c.more * (0.75f * begun + 0.25f * beyond);
         if (least == 0.f || time < least) best = c.form, least = time;
     };
     if (f32)
