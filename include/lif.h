@@ -628,7 +628,7 @@ typedef struct lif_packed_rows {
     const void* x;          /* [n_rows x n_in]: E, or 8 bits if x_scales are given               */
     const float* x_scales;  /* [n_rows] or [n_rows x ceil(n_in / x_group)] fp32; NULL: x is E    */
     const float* bias;      /* [n_out] fp32, or NULL                                             */
-    void* out;              /* [n_rows x n_out] E, written; must not overlap x, x_scales or bias */
+    void* out;              /* [n_rows x n_out] E, written; must not overlap x, x_scales, bias or the matrix */
     int64_t x_stride, out_stride;  /* elements between rows; that of out need not be a multiple of anything */
     int32_t n_rows;         /* 1..2^19                                                           */
     int32_t x_group;        /* 0: a scale for each row; else the group of the weights            */
@@ -651,6 +651,7 @@ int lif_packed_destroy(lif_packed* packed);
 int lif_packed_quantize(lif_packed* packed, const void* weights, int64_t stride, void* stream);
 
 /*
+ * (Neither these arrays nor the full weights of the two other calls may overlap the arrays of the matrix.)
  * From codes (device, [n_out x n_in / 2], two in a byte, the lower input in the lower half), scales [n_out x ceil(n_in / group)] fp32, which are
  * rounded to 16 significant bits (fp16 and bf16 values are kept), and zeros [n_out x ceil(n_in / group)], 0..255, NULL if the configuration has none.
  */
@@ -662,7 +663,8 @@ int lif_packed_dequantize(lif_packed* packed, void* weights, int64_t stride, voi
 /*
  * out[t, n] = sum_k x[t, k] * scale[n, k / group] * (code[n, k] - zero[n, k / group]) + bias[n]
  * Weights are not rounded further: a group's sum is fp32 (whole numbers for rows in 8 bits), scaled, added up in fp32 and rounded once to E.  Sums have a
- * fixed order for a given number of rows.  A row that holds infinity or NaN, or meets a scale that does, gives infinity or NaN there; other rows do not see it.
+ * fixed order for a given number of rows.  x_stride is at most 2^22.  In bf16 and fp32 a product below 2^-133 may be lost.  A row that holds infinity or NaN,
+ * or meets a scale that does, gives infinity or NaN there; other rows do not see it.
  */
 int lif_packed_multiply(lif_packed* packed, const lif_packed_rows* rows, void* stream);
 

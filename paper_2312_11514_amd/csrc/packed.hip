@@ -72,6 +72,22 @@ bool aligned(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(
 // a stride of at least one row; `bytes` of an element, whole `unit` bytes
 bool stride_ok(int64_t stride, int64_t width, int bytes, int unit) { return stride >= width && stride <= kMaxStride && stride * bytes % unit == 0; }
 
+// Whether rows share memory with the codes or the words of the groups.
+bool overlaps_matrix(const lif_packed* p, const Span& rows) {
+    const int64_t codes = (int64_t)lif_packed_code_bytes(&p->cfg), groups = (int64_t)lif_packed_group_bytes(&p->cfg);
+    return overlap(rows, Span{p->view.codes, codes, codes, 1}) || overlap(rows, Span{p->view.groups, groups, groups, 1});
+}
+// full weights, of a call that reads or writes all of them
+int weights_ok(const lif_packed* p, const void* weights, int64_t stride) {
+    if (!p || !weights) return fail(LIF_INVALID_ARG, "null pointer");
+    const int e = bytes_of(p->cfg.dtype);
+    if (!aligned(weights, 16) || !stride_ok(stride, p->cfg.n_in, e, 16))
+        return fail(LIF_INVALID_ARG, "rows of weights must be 16-byte aligned, at a stride that holds them");
+    if (overlaps_matrix(p, Span{weights, stride * e, (int64_t)p->cfg.n_in * e, p->cfg.n_out}))
+        return fail(LIF_INVALID_ARG, "weights must not overlap the codes or the words of the groups");
+    return LIF_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -152,10 +168,7 @@ int lif_packed_destroy(lif_packed* p) {
 }
 
 int lif_packed_quantize(lif_packed* p, const void* weights, int64_t stride, void* stream) {
-    if (!p || !weights) return fail(LIF_INVALID_ARG, "null pointer");
-    const int e = bytes_of(p->cfg.dtype);
-    if (!aligned(weights, 16) || !stride_ok(stride, p->cfg.n_in, e, 16))
-        return fail(LIF_INVALID_ARG, "rows of weights must be 16-byte aligned, at a stride that holds them");
+    if (const int rc = weights_ok(p, weights, stride)) return rc;
     const dim3 grid(std::min(p->tiles, kMakeBlocks)), block(256);
     hipStream_t s = (hipStream_t)stream;
     const bool z = p->cfg.zeros;
@@ -175,15 +188,16 @@ int lif_packed_pack(lif_packed* p, const uint8_t* codes, const float* scales, co
     if (!p || !codes || !scales) return fail(LIF_INVALID_ARG, "null pointer");
     if ((zeros != nullptr) != (p->cfg.zeros != 0)) return fail(LIF_INVALID_ARG, "zeros go with a configuration that has them");
     if (!aligned(codes, 4) || !aligned(scales, 4)) return fail(LIF_INVALID_ARG, "codes and scales must be 4-byte aligned");
+    const int64_t row = p->cfg.n_in / 2, groups = row_groups(p->cfg), n = p->cfg.n_out;
+    if (overlaps_matrix(p, Span{codes, row, row, n}) || overlaps_matrix(p, Span{scales, groups * 4, groups * 4, n}) ||
+        (zeros && overlaps_matrix(p, Span{zeros, groups, groups, n})))
+        return fail(LIF_INVALID_ARG, "codes, scales and zeros must not overlap the arrays of the matrix");
     hipLaunchKernelGGL(k_packed_pack, dim3(std::min(p->tiles, kMakeBlocks)), dim3(256), 0, (hipStream_t)stream, p->view, codes, scales, zeros, p->tiles);
     return launched();
 }
 
 int lif_packed_dequantize(lif_packed* p, void* weights, int64_t stride, void* stream) {
-    if (!p || !weights) return fail(LIF_INVALID_ARG, "null pointer");
-    const int e = bytes_of(p->cfg.dtype);
-    if (!aligned(weights, 16) || !stride_ok(stride, p->cfg.n_in, e, 16))
-        return fail(LIF_INVALID_ARG, "rows of weights must be 16-byte aligned, at a stride that holds them");
+    if (const int rc = weights_ok(p, weights, stride)) return rc;
     const dim3 grid(std::min(p->tiles, kMakeBlocks)), block(256);
     hipStream_t s = (hipStream_t)stream;
     if (p->cfg.dtype == LIF_F32) hipLaunchKernelGGL(k_packed_dequantize<float>, grid, block, 0, s, p->view, static_cast<float*>(weights), (long long)stride, p->tiles);
@@ -211,8 +225,8 @@ int lif_packed_multiply(lif_packed* p, const lif_packed_rows* rows, void* stream
     const int64_t groups = rows->x_group ? row_groups(c) : 1;
     const Span x{rows->x, rows->x_stride * x_e, (int64_t)c.n_in * x_e, rows->n_rows}, out{rows->out, rows->out_stride * e, (int64_t)c.n_out * e, rows->n_rows},
         scales{rows->x_scales, groups * 4, groups * 4, rows->n_rows}, bias{rows->bias, c.n_out * 4ll, c.n_out * 4ll, 1};
-    if (overlap(out, x) || (scales.at && overlap(out, scales)) || (bias.at && overlap(out, bias)))
-        return fail(LIF_INVALID_ARG, "out must not overlap x, its scales or the bias");
+    if (overlap(out, x) || (scales.at && overlap(out, scales)) || (bias.at && overlap(out, bias)) || overlaps_matrix(p, out))
+        return fail(LIF_INVALID_ARG, "out must not overlap x, its scales, the bias or the matrix");
     const ProductArgs a{p->view, static_cast<const char*>(rows->x), static_cast<char*>(rows->out), rows->x_scales, rows->bias, x_stride,
                         rows->out_stride, rows->n_rows, (int32_t)groups, c.dtype};
     hipStream_t s = (hipStream_t)stream;

@@ -17,7 +17,7 @@ SIZES = {0: 4, 1: 2, 2: 2}
 def _handle(lib, **c):
     b = lib.b
     cfg, h = b.LifPackedConfig(**c), C.c_void_p()
-    buf = b.LifPackedBuffers(lib.p, lib.p, lib.lib.lif_packed_code_bytes(C.byref(cfg)), lib.lib.lif_packed_group_bytes(C.byref(cfg)))
+    buf = b.LifPackedBuffers(1 << 36, 1 << 38, lib.lib.lif_packed_code_bytes(C.byref(cfg)), lib.lib.lif_packed_group_bytes(C.byref(cfg)))
     assert lib.lib.lif_packed_create(C.byref(cfg), C.byref(buf), C.byref(h)) == 0, lib.lib.lif_last_error_string()
     return h
 
@@ -29,7 +29,7 @@ def child_multiply(lib, seed, n):
         h = _handle(lib, n_out=n_out, n_in=n_in, group=group, zeros=zeros, dtype=dtype)
         for rows in [1, 4, 5, 8, 9, 16, 17, 1 << 19] + [int(2 ** rng.uniform(0, 19)) for _ in range(4)]:
             eight = rng.choice((0, 0, 1, 2))
-            far = 1 << 40                                  # (arrays that do not overlap)
+            far = 1 << 42                                  # (arrays that do not overlap)
             r = lib.b.LifPackedRows(x=far, x_scales=2 * far if eight else None, out=3 * far, x_stride=n_in, out_stride=n_out, n_rows=rows,
                                     x_group=group if eight == 2 else 0)
             rc, got = lib.launches(lambda: lib.lib.lif_packed_multiply(h, C.byref(r), None))
@@ -82,9 +82,9 @@ def child_make(lib):
         for dtype in (0, 1, 2):
             for zeros in (0, 1):
                 h = _handle(lib, n_out=n_out, n_in=n_in, group=64, zeros=zeros, dtype=dtype)
-                tiles, call = -(-n_out // 16) * -(-n_in // 128), lib.lib
-                for f in (lambda: call.lif_packed_quantize(h, lib.p, n_in, None), lambda: call.lif_packed_dequantize(h, lib.p, n_in, None),
-                          lambda: call.lif_packed_pack(h, lib.p, lib.p, lib.p if zeros else None, None)):
+                tiles, call, far = -(-n_out // 16) * -(-n_in // 128), lib.lib, 1 << 42        # (arrays beyond those of the matrix)
+                for f in (lambda: call.lif_packed_quantize(h, far, n_in, None), lambda: call.lif_packed_dequantize(h, far, n_in, None),
+                          lambda: call.lif_packed_pack(h, far, far, far if zeros else None, None)):
                     rc, got = lib.launches(f)
                     assert rc == 0 and [(g, b) for _, g, b, _, _ in got] == [(min(tiles, 2048), 256)], (n_out, n_in, got)
                     seen.append(got[0][0])

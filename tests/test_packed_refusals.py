@@ -16,7 +16,7 @@ def b():
     return binding
 
 
-P = 1 << 32
+P, M = 1 << 32, 1 << 34                                   # of rows, of the matrix
 CONFIG = dict(n_out=100, n_in=264, group=64, zeros=1, dtype=1)
 NORM = dict(x=P, residual=P + (1 << 20), total=P + (2 << 20), out=P + (3 << 20), weight=P + (5 << 20), bias=P + (6 << 20), x_stride=264,
             residual_stride=264, total_stride=264, out_stride=264, n_rows=10, width=264, dtype=1, norm=2, group=0, eps=1e-5)
@@ -32,7 +32,7 @@ def _refused(b, rc, *words):
 def _handle(b, **changes):
     cfg = b.LifPackedConfig(**dict(CONFIG, **changes))
     lib, h = b.load_library(), C.c_void_p()
-    buf = b.LifPackedBuffers(P, P, lib.lif_packed_code_bytes(C.byref(cfg)), lib.lif_packed_group_bytes(C.byref(cfg)))
+    buf = b.LifPackedBuffers(M, M + (1 << 30), lib.lif_packed_code_bytes(C.byref(cfg)), lib.lif_packed_group_bytes(C.byref(cfg)))
     assert lib.lif_packed_create(C.byref(cfg), C.byref(buf), C.byref(h)) == 0
     return lib, h
 
@@ -92,7 +92,8 @@ def test_add_norm_in_8_bits(b, change, word):
     (dict(x_group=32, x_scales=P + (3 << 20)), "x_group"), (dict(x=P + 8), "aligned"), (dict(x_stride=256), "stride"), (dict(x_stride=268), "stride"),
     (dict(out=P + (2 << 20) + 1), "aligned"), (dict(out_stride=99), "out"), (dict(out_stride=1 << 41), "out"), (dict(bias=P + 2), "aligned"),
     (dict(x_scales=P + 2), "aligned"), (dict(out=P + 16), "overlap"), (dict(out=P), "overlap"), (dict(bias=P + (2 << 20) + 8), "overlap"),
-    (dict(x_scales=P + (2 << 20) + 8), "overlap")])
+    (dict(x_scales=P + (2 << 20) + 8), "overlap"), (dict(out=M + 100), "overlap"), (dict(out=M + (1 << 30) - 1998), "overlap"),
+    (dict(x_stride=(1 << 22) + 8), "2^22")])
 def test_multiply(b, change, word):
     lib, h = _handle(b)
     args = b.LifPackedRows(**dict(ROWS, **change))
@@ -122,6 +123,11 @@ def test_making_weights(b):
     _refused(b, lib.lif_packed_quantize(h, P, 268, None), "stride")
     _refused(b, lib.lif_packed_dequantize(h, P + 4, 264, None), "aligned")
     _refused(b, lib.lif_packed_dequantize(h, P, 100, None), "stride")
+    for at in (M, M + 16, M - 16, M + (1 << 30) + 32):
+        _refused(b, lib.lif_packed_quantize(h, at, 264, None), "overlap")
+        _refused(b, lib.lif_packed_dequantize(h, at, 264, None), "overlap")
+        for arrays in ((at, P, P), (P, at, P), (P, P, at)):
+            _refused(b, lib.lif_packed_pack(h, *arrays, None), "overlap")
     _refused(b, lib.lif_packed_pack(h, P, P, None, None), "zeros")
     _refused(b, lib.lif_packed_pack(h, None, P, P, None), "null")
     _refused(b, lib.lif_packed_pack(h, P + 2, P, P, None), "aligned")
