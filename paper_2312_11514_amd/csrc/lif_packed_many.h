@@ -181,7 +181,7 @@ __global__ __launch_bounds__(64 * WN * WK, 4) void k_packed_many(ProductArgs a) 
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[t][i] = 0.f;
-    Stage stage[2];
+    Stage stage;
     u32x4 tile[2], gw[2][S];
     auto tile_of = [&](int i) { return min(i * WK + set, last); };
     auto ask = [&](int d, int i) {
@@ -190,8 +190,8 @@ __global__ __launch_bounds__(64 * WN * WK, 4) void k_packed_many(ProductArgs a) 
 #pragma unroll
         for (int s = 0; s < S; ++s) gw[d][s] = reinterpret_cast<const u32x4*>(groups + (size_t)(it * S + s) * 64)[q];
     };
-    auto ask_rows = [&](int d, int i) { stage[d].ask(a, x, offset, first, tile_of(i), tid); };
-    auto put = [&](int d, int i) { stage[d].put(a, shared.x[set][d], tile_of(i), tid); };
+    auto ask_rows = [&](int i) { stage.ask(a, x, offset, first, tile_of(i), tid); };
+    auto put = [&](int d, int i) { stage.put(a, shared.x[set][d], tile_of(i), tid); };
     auto take = [&](int d) {
         const typename Stage::Buffer& now = shared.x[set][d];
 #pragma unroll
@@ -247,21 +247,20 @@ __global__ __launch_bounds__(64 * WN * WK, 4) void k_packed_many(ProductArgs a) 
             __builtin_amdgcn_sched_barrier(0);               // one group after the other: the sums of several do not fit
         }
     };
-    // Codes are asked for two rounds ahead of their use, rows two rounds ahead of being handed over, one round ahead of their use, so that no one waits for LDS
-    // at the barrier.  (Without branches around the loads: the compiler waits for all of them where it cannot tell how many are on their way.)
-#pragma unroll
-    for (int d = 0; d < 2; ++d) {
-        ask_rows(d, d);
-        ask(d, d);
-    }
+    // Codes are asked for two rounds ahead of their use; rows one round ahead of being handed over, and that one round ahead of their use, so that no one waits
+    // for LDS at the barrier.  (Without branches around the loads: the compiler waits for all of them where it cannot tell how many are on their way.)
+    ask_rows(0);
+    ask(0, 0);
+    ask(1, 1);
     put(0, 0);
+    ask_rows(1);
     for (int i = 0; i < rounds; i += 2) {
 #pragma unroll
         for (int d = 0; d < 2; ++d) {
             if (d == 1 && i + 1 >= rounds) break;            // (for all waves)
             lds_barrier();
             put(d ^ 1, i + d + 1);
-            ask_rows(d, i + d + 2);
+            ask_rows(i + d + 2);
             if ((i + d) * WK + set <= last) take(d);
             ask(d, i + d + 2);
         }
