@@ -11,6 +11,14 @@
 // What is too much comes off with the sum of x.  Every group's sum is fp32 (or whole), and its step and zero point are applied to that: weights are not rounded.
 // bf16 and fp32 rows may be as large as what sums are held in: with 2^-16 or 2^-11 on one side no group's sum is infinite before its step is applied, and an
 // output gets the factor back at its end.
+//
+// What bounds it, up to 16 rows: the launch and one round trip to memory where the matrix is small (one row of 4096 by 4096, fp16: 3.6 us, 1.8 of them the launch,
+// 4.7 where no cache has the codes), the bytes where it is large (one row by 50001 outputs, groups of 64 with zero points: 19.7 us, 22.5 from memory, 116 MB at
+// 5.1 TB/s of the 6.3 that a plain read reaches), and between them what a tile costs in instructions: a SIMD issues one in four cycles, and the bytes of a tile
+// take a compute unit 100 cycles.  So codes take seven instructions for eight of them, the offset of their patterns comes off on the matrix cores, which have
+// the time, and groups stand side by side in columns that rows have no use for (with an addition for every two codes and steps group by group 27 us instead of
+// 19.9).  16 rows by 11008 outputs: 9.1 us, 11.6 from memory.  fp32 pays for its conversions: 8 rows of 2560 by 10240, groups of 32: 11 us for 16 MB.
+// Four waves instead of eight: the same for 50001 outputs, 3.7 us instead of 3.55 for 4096; sixteen: 30 and 4.1.
 #pragma once
 
 #include <type_traits>
@@ -136,7 +144,8 @@ __device__ __forceinline__ void store_as(char* out, int type, long long at, floa
 }
 
 // A tile of the inputs of 4 * MQ rows, of one wave: asked for row by row, 16 lanes each, and handed to the lanes that the matrix cores want them from
-// through LDS, where rows are a chunk longer than they need, so that the 16 lanes that read one chunk of 16 rows meet different banks.
+// through LDS, where rows are a chunk longer than they need, so that the 16 lanes that read one chunk of 16 rows meet different banks.  (A load whose neighbouring
+// lanes are in 16 different rows takes a compute unit 65 cycles, row by row 17: 16 rows by 11008 outputs 14.4 us instead of 9.4.)
 template <typename X, int MQ>
 struct FewRows {
     static constexpr bool kBytes = sizeof(X) == 1;
