@@ -4,7 +4,7 @@
 namespace lif {
 
 // Tiles of 16 outputs for up to 4, 8 or 16 rows, the inputs dealt to the waves (k_packed_few); or workgroups of so many outputs and rows (k_packed_many).
-enum class PackedForm { few4, few8, few16, outs32_rows16, outs64_rows16, outs64_rows32_16, outs64_rows32, outs64_rows48, outs64_rows64, outs128_rows64 };
+enum class PackedForm { few4, few8, few16, outs32_rows16, outs32_rows32, outs64_rows16, outs64_rows32_16, outs64_rows32, outs64_rows48, outs64_rows64, outs128_rows64 };
 
 // A larger workgroup reads and unpacks less for an output, but where there are fewer of them than the 256 compute units its own time is that of the call.
 // So a call is taken to last `alone` where the workgroups fit the chip at once, one to a compute unit, and `more` for every 256 beyond, three quarters of it for the
@@ -19,8 +19,9 @@ struct PackedCost {
     float alone, more;
 };
 constexpr PackedCost kPackedCosts[] = {
-    {PackedForm::few16, 1, 16, 4.4f, 2.1f},           {PackedForm::outs32_rows16, 2, 16, 5.7f, 3.1f},  {PackedForm::outs64_rows32_16, 4, 32, 9.4f, 9.0f},
-    {PackedForm::outs64_rows32, 4, 32, 10.3f, 7.8f},  {PackedForm::outs64_rows48, 4, 48, 13.2f, 10.8f}, {PackedForm::outs64_rows64, 4, 64, 16.5f, 13.2f},
+    {PackedForm::few16, 1, 16, 4.4f, 2.1f},           {PackedForm::outs32_rows16, 2, 16, 5.7f, 3.1f},   {PackedForm::outs32_rows32, 2, 32, 7.8f, 5.1f},
+    {PackedForm::outs64_rows32_16, 4, 32, 9.4f, 9.0f}, {PackedForm::outs64_rows32, 4, 32, 10.3f, 7.8f},
+    {PackedForm::outs64_rows48, 4, 48, 13.2f, 10.8f}, {PackedForm::outs64_rows64, 4, 64, 16.5f, 13.2f},
     {PackedForm::outs128_rows64, 8, 64, 26.f, 23.1f}};
 constexpr PackedCost kPackedCostsF32[] = {
     {PackedForm::few16, 1, 16, 11.5f, 6.2f}, {PackedForm::outs32_rows16, 2, 16, 13.4f, 12.f}, {PackedForm::outs64_rows16, 4, 16, 19.5f, 13.3f},

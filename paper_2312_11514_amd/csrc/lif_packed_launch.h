@@ -22,6 +22,9 @@ void launch_product_form(const ProductArgs& a, hipStream_t s) {
         case PackedForm::few16: return go(k_packed_few<X, G, ZEROS, 4, 2 / kWide, 8 / kWide>, 1, 16, 8 / kWide);
         case PackedForm::outs32_rows16: return go(k_packed_many<X, G, ZEROS, 1, 2, 4>, 2, 16, 8);
         case PackedForm::outs128_rows64: return go(k_packed_many<X, G, ZEROS, 4, 8, 1>, 8, 64, 8);
+        case PackedForm::outs32_rows32:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 2, 2, 4>, 2, 32, 8);
+            break;
         case PackedForm::outs64_rows16:
             if constexpr (kF32) return go(k_packed_many<X, G, ZEROS, 1, 4, 2>, 4, 16, 8);
             break;

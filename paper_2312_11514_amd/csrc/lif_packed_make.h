@@ -1,7 +1,7 @@
 // Making packed weights, from full ones or from codes as checkpoints hold them, and what they stand for.
 // A tile of 16 outputs x 128 inputs at a time, a word of eight codes to a thread; its group's largest weight by register moves between the lanes.  What bounds it:
 // 16384 x 4096 in fp16, the bytes and some arithmetic (38 us, 4.4 TB/s of the 5.2 that a large copy reaches; 47 with each weight compared with the half and codes
-// put together one by one); what the weights stand for 29 us, 5.8 TB/s, in fp32 3.3 TB/s (two stores of 16 bytes a lane, each half a line).
+// put together one by one); what the weights stand for 29 us, 5.8 TB/s.
 #pragma once
 
 #include "lif_packed.h"
@@ -110,18 +110,26 @@ __global__ __launch_bounds__(256) void k_packed_pack(PackedView w, const unsigne
     }
 }
 
+// 16 bytes of a row to a thread, so that its neighbours' stores lie beside them (fp32 with 32 bytes a thread in two stores: 18176 x 4544 111 us).
 template <typename T>
 __global__ __launch_bounds__(256) void k_packed_dequantize(PackedView w, T* __restrict__ to, long long stride, int tiles) {
+    constexpr int PER = 16 / sizeof(T), ACROSS = kTileIn / PER;
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const TilePlace p = tile_place(w, tile);
-        if (!p.in) continue;
-        const unsigned word = *tile_word(w, tile), g = *group_word(w, tile, p.at);
-        const float step = step_of(g);
-        const int zero = (int)(g & 0xffu) - 8;
-        float v[8];
+        const int ot = tile / w.in_tiles, it = tile - ot * w.in_tiles;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = step * (float)(code_of(word, e) - zero);
-        store_eight<T>(to + p.row * stride + p.at, v);
+        for (int place = threadIdx.x; place < kTileOut * ACROSS; place += 256) {
+            const int r = place / ACROSS, k = place % ACROSS * PER, row = ot * kTileOut + r, at = it * kTileIn + k, c = k / 8;
+            if (row >= w.n_out || at >= w.n_in) continue;
+            const unsigned word = w.codes[(size_t)tile * 256 + ((c & 3) * 16 + r) * 4 + (c >> 2)];
+            const unsigned g = w.groups[((size_t)ot * w.n_groups + at / w.group) * kTileOut + r];
+            const float step = step_of(g);
+            const int zero = (int)(g & 0xffu) - 8;
+            typedef T Some __attribute__((ext_vector_type(PER)));
+            Some v;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) v[e] = (T)(step * (float)(code_of(word, (k & 7) + e) - zero));
+            *reinterpret_cast<Some*>(to + row * stride + at) = v;
+        }
     }
 }
 
