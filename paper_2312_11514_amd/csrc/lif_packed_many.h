@@ -7,23 +7,24 @@
 // What bounds it: the instructions of a SIMD.  By measurement a matrix instruction takes two issue slots of four cycles of the sixteen that it works, an
 // arithmetic one about one, a read of LDS two, and a wave alone has one slot in two; with 64 rows there are four arithmetic instructions and one read to a
 // matrix instruction, with 16 rows nine.  1024 rows of 4096 by 11008, fp16: 130 us, 0.71 PFLOP/s of the 1.37 that a library's large product reaches; rows in 8 bits
-// 92 us, 1.0 PFLOP/s; 777 rows by 4096 with zero points 50 us (0.52; a library's fp16 product of these sizes 42); 48 rows in 8 bits with scales by groups by 18176
-// outputs 33 us; 64 rows by 4096 8.4 us, 60 rows of 11008 in groups of 32, bf16, 25 us.
+// 92 us, 1.0 PFLOP/s; 777 rows by 4096 with zero points 48 us (0.54; a library's fp16 product of these sizes 42); 48 rows in 8 bits with scales by groups by 18176
+// outputs 33 us; 64 rows by 4096 7.8 us, 60 rows of 11008 in groups of 32, bf16, 23.5 us.
 #pragma once
 
 #include "lif_packed_few.h"
 
 namespace lif {
 
-// The codes where their unpacking is shared by many rows: in fp16 c - 8 itself, or c where the sum of x is taken off anyway.
+// The codes as they come, where the sum of x is taken off anyway; in fp16 without zero points c - 8 itself, from which nothing has to be.  (With zero points
+// c itself, two instructions more for a pair: 777 rows by 4096 50 us instead of 48.)
 template <typename X, bool ZEROS>
 struct Exact : Operand<X> {};
-template <bool ZEROS>
-struct Exact<_Float16, ZEROS> {
-    static constexpr float kMiddle = ZEROS ? 0.f : 8.f;
+template <>
+struct Exact<_Float16, false> {
+    static constexpr float kMiddle = 8.f;
     static __device__ __forceinline__ f16x8 codes(unsigned w) {
         const unsigned u = w >> 8;
-        const _Float16 m = (_Float16)(-1024.f - kMiddle), l = (_Float16)(-64.f - kMiddle);
+        const _Float16 m = (_Float16)-1032.f, l = (_Float16)-72.f;
         const f16x2 minus{m, m}, part{(_Float16)0.0625f, (_Float16)0.0625f}, less{l, l};
         auto low = [&](unsigned v) { return __builtin_bit_cast(f16x2, (v & 0x000f000fu) ^ 0x64086408u) + minus; };
         auto high = [&](unsigned v) { return __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (v & 0x00f000f0u) ^ 0x64806480u), part, less); };
