@@ -8,11 +8,12 @@ enum class PackedForm { few4, few8, few16, outs32_rows16, outs32_rows32, outs64_
 
 // A larger workgroup reads and unpacks less for an output, but where there are fewer of them than the 256 compute units its own time is that of the call.
 // So a call is taken to last `alone` where the workgroups fit the chip at once, one to a compute unit, and `more` for every 256 beyond, three quarters of it for the
-// first of them (outs128_rows64: 256 workgroups 28.4 us, 258 42.8, 512 45.0): us for 4096 inputs in fp16 with groups of 128, in fp32 with groups of 64 and zero points, from 17 to 1024 rows by 1024 to 50000 outputs.  Other inputs, types and groups scale them
-// alike: against the fastest of 15 forms that were tried the rule's choice loses 2 % on average and 15 % at most in fp16, in bf16 with groups of 32 and in bytes with
-// scales by groups of 64; in fp32 11 % and 39 % (50000 outputs: two tiles of outputs to a wave, which is not compiled).
-// E.g. 4096 outputs, fp16: 24 rows 5.8 (few16 6.3, outs64_rows32_16 9.5), 128 rows 10.6 (outs32_rows16 13.7, outs64_rows64 16.9), 512 rows 28.9 (outs64_rows32
-// 31.0, outs64_rows64 29.2); 50000 outputs: 24 rows 29.5 (few16 50.8, outs64_rows64 43.6), 512 rows 292 (outs64_rows32 379, outs64_rows64 326).
+// first of them (outs128_rows64: 256 workgroups 28.4 us, 258 42.8, 512 45.0): us for 4096 inputs in fp16 with groups of 128, in fp32 with groups of 64 and zero
+// points, from 17 to 1024 rows by 1024 to 50000 outputs.  Other inputs, types and groups scale them alike: against the fastest of these forms the rule's choice
+// loses 1 % on average and 4 % at most in fp16 and fp32, 6 % in bf16 with groups of 32; in bytes with scales by groups of 64 2 % and 20 % (48 rows by 50000 outputs,
+// 52 instead of 43).
+// E.g. 4096 outputs, fp16: 24 rows 5.7 (few16 6.0, outs64_rows32_16 9.3), 128 rows 10.4 (outs32_rows16 14.0, outs64_rows64 15.8), 512 rows 28.5 (outs64_rows32
+// 33.0, outs64_rows64 29.6); 50000 outputs: 24 rows 31.8 (few16 51.9, outs64_rows64 42.6), 512 rows 295 (outs64_rows32 373, outs64_rows64 331).
 struct PackedCost {
     PackedForm form;
     int tiles, rows;             // of a workgroup
