@@ -3,30 +3,34 @@
 
 namespace lif {
 
-// Tiles of 16 outputs for up to 4, 8 or 16 rows, the inputs dealt to the waves (k_packed_few); or workgroups of so many outputs and rows (k_packed_many).
-enum class PackedForm { few4, few8, few16, outs32_rows16, outs32_rows32, outs64_rows16, outs64_rows32_16, outs64_rows32, outs64_rows48, outs64_rows64, outs128_rows64 };
+// Tiles of 16 outputs for up to 4, 8 or 16 rows, the inputs dealt to the waves (k_packed_few); or workgroups of so many outputs and rows (k_packed_many; _16: in
+// 16 waves instead of 8, sooner done alone).
+enum class PackedForm { few4, few8, few16, outs32_rows16, outs32_rows32, outs64_rows16, outs64_rows32_16, outs64_rows32, outs48_rows48, outs64_rows48, outs64_rows64_16,
+                        outs64_rows64, outs80_rows64, outs96_rows32, outs96_rows64, outs112_rows48, outs128_rows64 };
 
 // A larger workgroup reads and unpacks less for an output, but where there are fewer of them than the 256 compute units its own time is that of the call.
 // So a call is taken to last `alone` where the workgroups fit the chip at once, one to a compute unit, and `more` for every 256 beyond, three quarters of it for the
 // first of them (outs128_rows64: 256 workgroups 28.4 us, 258 42.8, 512 45.0): us for 4096 inputs in fp16 with groups of 128, in fp32 with groups of 64 and zero
-// points, from 17 to 1024 rows by 1024 to 50000 outputs.  Other inputs, types and groups scale them alike: against the fastest of these forms the rule's choice
-// loses 1 % on average and 4 % at most in fp16 and fp32, 6 % in bf16 with groups of 32; in bytes with scales by groups of 64 2 % and 20 % (48 rows by 50000 outputs,
-// 52 instead of 43).
+// points, from 17 to 1024 rows by 1024 to 50000 outputs.  Widths of 48, 80, 96 and 112 outputs are there for what 64 and 128 leave idle (48 rows by 18176, bytes
+// with scales by groups: 284 workgroups of 64 outputs 30.9 us, 228 of 80 24.7).  Other inputs, types and groups scale the times alike: against the fastest of these
+// forms the rule's choice loses 1 % on average and 16 % at most (fp16, bf16 with groups of 32, bytes with scales by groups of 64), in fp32 0.3 % and 3 %.
 // E.g. 4096 outputs, fp16: 24 rows 5.7 (few16 6.0, outs64_rows32_16 9.3), 128 rows 10.4 (outs32_rows16 14.0, outs64_rows64 15.8), 512 rows 28.5 (outs64_rows32
-// 33.0, outs64_rows64 29.6); 50000 outputs: 24 rows 31.8 (few16 51.9, outs64_rows64 42.6), 512 rows 295 (outs64_rows32 373, outs64_rows64 331).
+// 33.0, outs64_rows64 29.6); 50000 outputs: 24 rows 31.8 (few16 51.9), 512 rows 295 (outs64_rows32 373, outs64_rows64 331).
 struct PackedCost {
     PackedForm form;
     int tiles, rows;             // of a workgroup
     float alone, more;
+    int group;                   // the smallest it is compiled for: with less, registers go to memory
 };
 constexpr PackedCost kPackedCosts[] = {
-    {PackedForm::few16, 1, 16, 4.4f, 2.1f},           {PackedForm::outs32_rows16, 2, 16, 5.7f, 3.1f},   {PackedForm::outs32_rows32, 2, 32, 7.8f, 5.1f},
-    {PackedForm::outs64_rows32_16, 4, 32, 9.4f, 9.0f}, {PackedForm::outs64_rows32, 4, 32, 10.3f, 7.8f},
-    {PackedForm::outs64_rows48, 4, 48, 13.2f, 10.8f}, {PackedForm::outs64_rows64, 4, 64, 16.5f, 13.2f},
-    {PackedForm::outs128_rows64, 8, 64, 26.f, 23.1f}};
+    {PackedForm::few16, 1, 16, 4.3f, 1.9f, 32},            {PackedForm::outs32_rows16, 2, 16, 5.5f, 2.9f, 32},    {PackedForm::outs32_rows32, 2, 32, 7.5f, 4.9f, 32},
+    {PackedForm::outs64_rows32_16, 4, 32, 10.f, 8.9f, 32}, {PackedForm::outs64_rows32, 4, 32, 11.4f, 6.8f, 32},   {PackedForm::outs64_rows48, 4, 48, 13.f, 9.4f, 32},
+    {PackedForm::outs48_rows48, 3, 48, 10.8f, 9.9f, 32},   {PackedForm::outs64_rows64_16, 4, 64, 14.4f, 14.7f, 64}, {PackedForm::outs64_rows64, 4, 64, 15.5f, 11.8f, 64},
+    {PackedForm::outs80_rows64, 5, 64, 17.3f, 17.6f, 64},  {PackedForm::outs96_rows32, 6, 32, 13.6f, 10.5f, 32},  {PackedForm::outs96_rows64, 6, 64, 20.2f, 20.4f, 32},
+    {PackedForm::outs112_rows48, 7, 48, 19.6f, 18.7f, 32}, {PackedForm::outs128_rows64, 8, 64, 25.8f, 19.9f, 32}};
 constexpr PackedCost kPackedCostsF32[] = {
-    {PackedForm::few16, 1, 16, 11.5f, 6.2f}, {PackedForm::outs32_rows16, 2, 16, 13.4f, 12.f}, {PackedForm::outs64_rows16, 4, 16, 19.5f, 13.3f},
-    {PackedForm::outs128_rows64, 8, 64, 70.f, 75.f}};
+    {PackedForm::few16, 1, 16, 11.5f, 6.2f, 32}, {PackedForm::outs32_rows16, 2, 16, 13.4f, 12.f, 32}, {PackedForm::outs64_rows16, 4, 16, 19.5f, 13.3f, 32},
+    {PackedForm::outs128_rows64, 8, 64, 70.f, 75.f, 32}};
 
 // tiles: of 16 outputs
 inline PackedForm packed_form(int tiles, int rows, bool f32, int group) {
@@ -34,7 +38,7 @@ inline PackedForm packed_form(int tiles, int rows, bool f32, int group) {
     PackedForm best = PackedForm::few16;
     float least = 0.f;
     auto look = [&](const PackedCost& c) {
-        if (c.form == PackedForm::outs64_rows64 && group == 32) return;      // (registers to memory: 28 us instead of 16 alone)
+        if (group < c.group) return;
         const float groups = (float)((tiles + c.tiles - 1) / c.tiles) * (float)((rows + c.rows - 1) / c.rows) / 256.f;
         const float beyond = groups > 1.f ? groups - 1.f : 0.f, begun = (float)(long long)beyond + ((float)(long long)beyond < beyond ? 1.f : 0.f);
         const float time = c.alone + c.more * (0.75f * begun + 0.25f * beyond);

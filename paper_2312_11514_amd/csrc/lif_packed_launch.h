@@ -25,6 +25,9 @@ void launch_product_form(const ProductArgs& a, hipStream_t s) {
         case PackedForm::outs32_rows32:
             if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 2, 2, 4>, 2, 32, 8);
             break;
+        case PackedForm::outs48_rows48:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 3, 3, 4>, 3, 48, 12);
+            break;
         case PackedForm::outs64_rows16:
             if constexpr (kF32) return go(k_packed_many<X, G, ZEROS, 1, 4, 2>, 4, 16, 8);
             break;
@@ -37,8 +40,23 @@ void launch_product_form(const ProductArgs& a, hipStream_t s) {
         case PackedForm::outs64_rows48:
             if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 3, 4, 2>, 4, 48, 8);
             break;
+        case PackedForm::outs64_rows64_16:
+            if constexpr (!kF32 && G > 32) return go(k_packed_many<X, G, ZEROS, 4, 4, 4>, 4, 64, 16);
+            break;
         case PackedForm::outs64_rows64:
             if constexpr (!kF32 && G > 32) return go(k_packed_many<X, G, ZEROS, 4, 4, 2>, 4, 64, 8);
+            break;
+        case PackedForm::outs80_rows64:
+            if constexpr (!kF32 && G > 32) return go(k_packed_many<X, G, ZEROS, 4, 5, 3>, 5, 64, 15);
+            break;
+        case PackedForm::outs96_rows32:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 2, 6, 2>, 6, 32, 12);
+            break;
+        case PackedForm::outs96_rows64:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 4, 6, 2>, 6, 64, 12);
+            break;
+        case PackedForm::outs112_rows48:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 3, 7, 2>, 7, 48, 14);
             break;
     }
 }

@@ -109,7 +109,8 @@ def child(tmp_path_factory):
 def test_products(child):
     forms = child("multiply", 1, 150)
     few = {"('few', %s, %d)" % (f32, q) for f32 in (False, True) for q in (1, 2, 4)}
-    many = {"('many', False, %d, %d, %d)" % f for f in ((1, 2, 4), (2, 2, 4), (2, 4, 4), (2, 4, 2), (3, 4, 2), (4, 4, 2), (4, 8, 1))}
+    many = {"('many', False, %d, %d, %d)" % f for f in ((1, 2, 4), (2, 2, 4), (2, 4, 4), (2, 4, 2), (3, 3, 4), (3, 4, 2), (4, 4, 4), (4, 4, 2), (4, 5, 3), (2, 6, 2), (4, 6, 2),
+                                                          (3, 7, 2), (4, 8, 1))}
     many |= {"('many', True, %d, %d, %d)" % f for f in ((1, 2, 4), (1, 4, 2), (4, 8, 1))}
     assert set(forms) == few | many, sorted(set(forms) ^ (few | many))
 
@@ -124,8 +125,10 @@ def test_making_weights(child):
 
 @pytest.mark.parametrize("tiles,rows,f32,group,form", [
     (256, 1, 0, 128, "few4"), (256, 5, 0, 128, "few8"), (256, 16, 0, 128, "few16"), (64, 64, 0, 128, "few16"), (256, 24, 0, 128, "outs32_rows16"), (256, 60, 0, 32, "outs32_rows32"),
-    (256, 128, 0, 128, "outs64_rows32_16"), (688, 128, 0, 128, "outs64_rows32"), (1136, 48, 0, 64, "outs64_rows48"), (688, 256, 0, 128, "outs64_rows64"),
-    (688, 256, 0, 32, "outs128_rows64"), (256, 777, 0, 128, "outs128_rows64"), (3126, 512, 0, 128, "outs128_rows64"), (64, 64, 1, 64, "few16"),
+    (256, 128, 0, 128, "outs64_rows32_16"), (1537, 17, 0, 128, "outs64_rows32"), (688, 48, 0, 128, "outs48_rows48"), (257, 97, 0, 32, "outs64_rows48"),
+    (385, 97, 0, 64, "outs64_rows64_16"), (688, 256, 0, 64, "outs64_rows64"), (385, 97, 0, 32, "outs64_rows32"), (1136, 48, 0, 64, "outs80_rows64"), (1136, 32, 0, 128, "outs96_rows32"),
+    (688, 256, 0, 32, "outs96_rows64"), (1376, 48, 0, 64, "outs112_rows48"), (256, 777, 0, 128, "outs128_rows64"), (3126, 512, 0, 128, "outs128_rows64"),
+    (64, 64, 1, 64, "few16"),
     (256, 128, 1, 64, "outs64_rows16"), (3126, 512, 1, 64, "outs128_rows64")])
 def test_the_rule(tmp_path, tiles, rows, f32, group, form):
     source = tmp_path / "rule.cpp"

@@ -1,4 +1,4 @@
-"""Registers of the products of weights in 4 bits, as the compiler reports them: none goes to memory, and forms for many rows leave room for four waves on a
+"""Registers of the products of weights in 4 bits, as the compiler reports them: none goes to memory, and forms for many rows leave some for four waves on a
 SIMD, which their arithmetic needs."""
 import os
 import re
@@ -24,6 +24,6 @@ def test_products_fit_their_registers(source):
         elif name:
             kernels.setdefault(name, {})[key] = value
     few, many = ([v for k, v in kernels.items() if kind in k] for kind in ("k_packed_few", "k_packed_many"))
-    assert len(few) == 3 * 2 * 3 and len(many) == 2 * (7 + 7 + 6)
+    assert len(few) == 3 * 2 * 3 and len(many) == 2 * (13 + 13 + 10)
     assert all(v["VGPRs Spill"] == "0" for v in few + many), [(k, v["VGPRs Spill"]) for k, v in kernels.items() if v.get("VGPRs Spill") != "0"]
-    assert all(int(v["Occupancy"]) >= 4 for v in many)
+    assert all(int(v["VGPRs"]) + int(v["AGPRs"]) <= 512 // 4 for v in many)
