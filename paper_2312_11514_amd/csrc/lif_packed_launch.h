@@ -15,15 +15,24 @@ void launch_product_form(const ProductArgs& a, hipStream_t s) {
     auto go = [&](auto kernel, int outs, int rows, int waves) {
         hipLaunchKernelGGL(kernel, dim3((tiles + outs - 1) / outs, (a.rows + rows - 1) / rows), dim3(waves * 64), 0, s, a);
     };
-    const PackedForm f = packed_form(tiles, a.rows, kF32, G);
+    const PackedForm f = packed_form(tiles, a.w.in_tiles, a.rows, kF32, G);
     switch (f) {
         case PackedForm::few4: return go(k_packed_few<X, G, ZEROS, 1, 4, 8>, 1, 16, 8);
         case PackedForm::few8: return go(k_packed_few<X, G, ZEROS, 2, 4 / kWide, 8>, 1, 16, 8);
         case PackedForm::few16: return go(k_packed_few<X, G, ZEROS, 4, 2 / kWide, 8 / kWide>, 1, 16, 8 / kWide);
         case PackedForm::outs32_rows16: return go(k_packed_many<X, G, ZEROS, 1, 2, 4>, 2, 16, 8);
         case PackedForm::outs128_rows64: return go(k_packed_many<X, G, ZEROS, 4, 8, 1>, 8, 64, 8);
+        case PackedForm::outs32_rows16_16:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 1, 2, 8>, 2, 16, 16);
+            break;
         case PackedForm::outs32_rows32:
             if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 2, 2, 4>, 2, 32, 8);
+            break;
+        case PackedForm::outs32_rows32_16:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 2, 2, 8>, 2, 32, 16);
+            break;
+        case PackedForm::outs48_rows32:
+            if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 2, 3, 5>, 3, 32, 15);
             break;
         case PackedForm::outs48_rows48:
             if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 3, 3, 4>, 3, 48, 12);

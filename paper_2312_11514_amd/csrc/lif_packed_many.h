@@ -8,7 +8,7 @@
 // arithmetic one about one, a read of LDS two, and a wave alone has one slot in two; with 64 rows there are four arithmetic instructions and one read to a
 // matrix instruction, with 16 rows nine.  1024 rows of 4096 by 11008, fp16: 130 us, 0.71 PFLOP/s of the 1.37 that a library's large product reaches; rows in 8 bits
 // 92 us, 1.0 PFLOP/s; 777 rows by 4096 with zero points 48 us (0.54; a library's fp16 product of these sizes 42); 48 rows in 8 bits with scales by groups by 18176
-// outputs 27 us; 64 rows by 4096 7.8 us, 60 rows of 11008 in groups of 32, bf16, 23.5 us.
+// outputs 27 us; 64 rows by 4096 7.8 us, 60 rows of 11008 in groups of 32, bf16, 20 us.
 #pragma once
 
 #include "lif_packed_few.h"

@@ -107,9 +107,9 @@ def child(tmp_path_factory):
 
 
 def test_products(child):
-    forms = child("multiply", 1, 150)
+    forms = child("multiply", 1, 500)
     few = {"('few', %s, %d)" % (f32, q) for f32 in (False, True) for q in (1, 2, 4)}
-    many = {"('many', False, %d, %d, %d)" % f for f in ((1, 2, 4), (2, 2, 4), (2, 4, 4), (2, 4, 2), (3, 3, 4), (3, 4, 2), (4, 4, 4), (4, 4, 2), (4, 5, 3), (2, 6, 2), (4, 6, 2),
+    many = {"('many', False, %d, %d, %d)" % f for f in ((1, 2, 4), (1, 2, 8), (2, 2, 4), (2, 2, 8), (2, 3, 5), (2, 4, 4), (2, 4, 2), (3, 3, 4), (3, 4, 2), (4, 4, 4), (4, 4, 2), (4, 5, 3), (2, 6, 2), (4, 6, 2),
                                                           (3, 7, 2), (4, 8, 1))}
     many |= {"('many', True, %d, %d, %d)" % f for f in ((1, 2, 4), (1, 4, 2), (4, 8, 1))}
     assert set(forms) == few | many, sorted(set(forms) ^ (few | many))
@@ -123,18 +123,18 @@ def test_making_weights(child):
     assert child("make") == 3 * 2 + 3 + 1
 
 
-@pytest.mark.parametrize("tiles,rows,f32,group,form", [
-    (256, 1, 0, 128, "few4"), (256, 5, 0, 128, "few8"), (256, 16, 0, 128, "few16"), (64, 64, 0, 128, "few16"), (256, 24, 0, 128, "outs32_rows16"), (256, 60, 0, 32, "outs32_rows32"),
-    (256, 128, 0, 128, "outs64_rows32_16"), (1537, 17, 0, 128, "outs64_rows32"), (688, 48, 0, 128, "outs48_rows48"), (257, 97, 0, 32, "outs64_rows48"),
-    (385, 97, 0, 64, "outs64_rows64_16"), (688, 256, 0, 64, "outs64_rows64"), (385, 97, 0, 32, "outs64_rows32"), (1136, 48, 0, 64, "outs80_rows64"), (1136, 32, 0, 128, "outs96_rows32"),
-    (688, 256, 0, 32, "outs96_rows64"), (1376, 48, 0, 64, "outs112_rows48"), (256, 777, 0, 128, "outs128_rows64"), (3126, 512, 0, 128, "outs128_rows64"),
-    (64, 64, 1, 64, "few16"),
-    (256, 128, 1, 64, "outs64_rows16"), (3126, 512, 1, 64, "outs128_rows64")])
-def test_the_rule(tmp_path, tiles, rows, f32, group, form):
+@pytest.mark.parametrize("tiles,in_tiles,rows,f32,group,form", [
+    (256, 32, 1, 0, 128, "few4"), (256, 32, 5, 0, 128, "few8"), (256, 32, 16, 0, 128, "few16"), (64, 32, 64, 0, 128, "few16"), (256, 32, 24, 0, 128, "outs32_rows16"),
+    (256, 86, 24, 0, 128, "outs32_rows16_16"), (256, 32, 60, 0, 32, "outs32_rows32"), (256, 86, 60, 0, 32, "outs32_rows32_16"), (688, 32, 24, 0, 128, "outs48_rows32"),
+    (688, 32, 48, 0, 128, "outs48_rows48"), (256, 32, 128, 0, 128, "outs64_rows32_16"), (1537, 32, 17, 0, 128, "outs64_rows32"), (257, 32, 97, 0, 32, "outs64_rows48"),
+    (385, 32, 97, 0, 64, "outs64_rows64_16"), (688, 32, 256, 0, 64, "outs64_rows64"), (385, 32, 97, 0, 32, "outs64_rows32"), (1136, 36, 48, 0, 64, "outs80_rows64"),
+    (1136, 32, 32, 0, 128, "outs96_rows32"), (688, 32, 256, 0, 32, "outs96_rows64"), (1376, 32, 48, 0, 64, "outs112_rows48"), (256, 32, 777, 0, 128, "outs128_rows64"),
+    (3126, 32, 512, 0, 128, "outs128_rows64"), (64, 32, 64, 1, 64, "few16"), (256, 32, 128, 1, 64, "outs64_rows16"), (3126, 32, 512, 1, 64, "outs128_rows64")])
+def test_the_rule(tmp_path, tiles, in_tiles, rows, f32, group, form):
     source = tmp_path / "rule.cpp"
     header = os.path.join(os.path.dirname(HERE), "paper_2312_11514_amd", "csrc", "lif_packed_form.h")
-    source.write_text('#include "%s"\nint main() { return lif::packed_form(%d, %d, %s, %d) == lif::PackedForm::%s ? 0 : 1; }\n' %
-                      (header, tiles, rows, "true" if f32 else "false", group, form))
+    source.write_text('#include "%s"\nint main() { return lif::packed_form(%d, %d, %d, %s, %d) == lif::PackedForm::%s ? 0 : 1; }\n' %
+                      (header, tiles, in_tiles, rows, "true" if f32 else "false", group, form))
     subprocess.run(["g++", "-std=c++17", "-o", str(tmp_path / "rule"), str(source)], check=True)
     assert subprocess.run([str(tmp_path / "rule")]).returncode == 0
 

@@ -151,20 +151,19 @@ def test_large_products(dtype, rows, n_in, n_out):
     check_product(np.random.default_rng(rows), rows, n_in, n_out, 128, True, dtype)
 
 
-# rows and outputs that the rule gives each of its workgroups, by outputs and rows of them (groups of 32 have no 64 by 64 and no 80 by 64)
-FORMS = {"32x16": (17, 2061), "32x32": (17, 4109), "64x32_16": (17, 8205), "64x32": (17, 24589), "48x48": (33, 8205), "64x48": (97, 4109), "64x64_16": (97, 6157), "64x64": (321, 5389),
-         "80x64": (65, 8205), "96x32": (17, 16397), "96x64": (97, 10253), "112x48": (33, 20493), "128x64": (97, 12301)}
+# rows, outputs and inputs that the rule gives to each of its workgroups, by outputs and rows of them (groups of 32 have no 64 by 64 and no 80 by 64)
+FORMS = {"32x16": (17, 2061, 712), "32x16_16": (17, 2061, 5128), "32x32": (17, 4109, 712), "32x32_16": (17, 4109, 5128), "48x32": (17, 11565, 712),
+         "48x48": (33, 8205, 712), "64x32": (17, 12301, 136), "64x32_16": (33, 6157, 1528), "64x48": (33, 8205, 136), "64x64": (49, 8205, 136),
+         "64x64_16": (97, 6157, 1528), "80x64": (33, 16397, 712), "96x32": (17, 16397, 712), "96x64": (97, 10253, 712), "112x48": (65, 12557, 712),
+         "128x64": (97, 12301, 136)}
 
 
 @pytest.mark.parametrize("form", FORMS)
-@pytest.mark.parametrize("kind,group", [("f16", 64), ("bf16", 32), ("f16", 128), ("row", 32), ("group", 64)])
-def test_every_workgroup(kind, group, form):
-    """With fewer tiles of the inputs than sets of waves that take them in turn, and with more"""
-    for n_in in (136, 712):
-        rows, n_out = FORMS[form]
-        rng = np.random.default_rng(n_out + n_in)
-        check_product(rng, rows, n_in, n_out, group, (n_in == 712) == (group != 32), "bf16" if kind in ("row", "group") else kind, bias=n_in == 712,
-                      eight=kind if kind in ("row", "group") else None)
+@pytest.mark.parametrize("kind,group,zeros", [("f16", 64, True), ("bf16", 32, False), ("f16", 128, False), ("row", 32, True), ("group", 64, True)])
+def test_every_workgroup(kind, group, zeros, form):
+    rows, n_out, n_in = FORMS[form]
+    check_product(np.random.default_rng(n_out + n_in), rows, n_in, n_out, group, zeros, "bf16" if kind in ("row", "group") else kind, bias=True,
+                  eight=kind if kind in ("row", "group") else None)
 
 
 def test_largest_magnitudes():
