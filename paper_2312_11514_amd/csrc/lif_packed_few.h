@@ -4,18 +4,21 @@
 //
 // A tile of 16 outputs is one operand, 16 rows of x the other, and the lane (r, q) gets row r of the outputs 4 q .. 4 q + 3: with one row in use of 16 the
 // products still cost less than the bytes.  Codes become elements by masks, exactly:
-//   fp16  64 + c is a pattern of bits; so is 1024 + c or 1024 + 16 c, and minus 1032, or times 1/16 minus 72, that is c - 8
-//   bf16  (128 + c) / 2^16 is a pattern of bits
+//   fp16  16 + c is a pattern of bits; so is 1024 + c or 1024 + 16 c, and minus 1032, or times 1/16 minus 72, that is c - 8
+//   bf16  (16 + c) / 2^16 is a pattern of bits
 //   fp32  c - 8 in bf16; x / 2^11 is three bf16 pieces of 8 bits each, which are exact together
 //   8 bits  16 (c - 8), whole numbers throughout
-// What is too much comes off with the sum of x.  Every group's sum is fp32 (or whole), and its step and zero point are applied to that: weights are not rounded.
+// What is too much comes off with the sum of x: little of it, so that a group's sum is not much smaller than what it is rounded as on its way.  (Sums of 11008
+// inputs with a common offset of a fifth of their spread are off by up to 0.8e-6 of them in fp16 and 0.5e-6 in bf16; with 64 + c and 128 + c, an instruction less
+// for eight codes and 0 to 2 % of the time of one row, by 2.8e-6 and 3.7e-6, where one addition after the other in fp32 leaves 2.6e-6.)
+// Every group's sum is fp32 (or whole), and its step and zero point are applied to that: weights are not rounded.
 // bf16 and fp32 rows may be as large as what sums are held in: with 2^-16 or 2^-11 on one side no group's sum is infinite before its step is applied, and an
 // output gets the factor back at its end.
 //
 // What bounds it, up to 16 rows: the launch and one round trip to memory where the matrix is small (one row of 4096 by 4096, fp16: 3.6 us, 1.8 of them the launch,
 // 4.7 where no cache has the codes), the bytes where it is large (one row by 50001 outputs, groups of 64 with zero points: 19.7 us, 22.5 from memory, 116 MB at
 // 5.1 TB/s of the 6.3 that a plain read reaches), and between them what a tile costs in instructions: a SIMD issues one in four cycles, and the bytes of a tile
-// take a compute unit 100 cycles.  So codes take seven instructions for eight of them, the offset of their patterns comes off on the matrix cores, which have
+// take a compute unit 100 cycles.  So codes take eight instructions for eight of them, the offset of their patterns comes off on the matrix cores, which have
 // the time, and groups stand side by side in columns that rows have no use for (with an addition for every two codes and steps group by group 27 us instead of
 // 19.9).  16 rows by 11008 outputs: 9.1 us, 11.6 from memory.  fp32 pays for its conversions: 8 rows of 2560 by 10240, groups of 32: 11 us for 16 MB.
 // Four waves instead of eight: the same for 50001 outputs, 3.7 us instead of 3.55 for 4096; sixteen: 30 and 4.1.
@@ -44,22 +47,22 @@ template <typename X> struct Operand;
 template <> struct Operand<_Float16> {
     static constexpr int kPieces = 1;
     static constexpr float kUp = 1.f;        // what an output is multiplied by at its end
-    static constexpr float kMiddle = -64.f;  // the code that counts 0
+    static constexpr float kMiddle = -16.f;  // the code that counts 0
     typedef f16x8 Word;
     static __device__ __forceinline__ Word codes(unsigned w) {
-        auto pair = [](unsigned v) { return (v & 0x00f000f0u) ^ 0x54805480u; };
-        return __builtin_bit_cast(Word, u32x4{pair(w << 4), pair(w), pair(w >> 4), pair(w >> 8)});
+        auto pair = [](unsigned v) { return (v & 0x03c003c0u) ^ 0x4e004e00u; };
+        return __builtin_bit_cast(Word, u32x4{pair(w << 6), pair(w << 2), pair(w >> 2), pair(w >> 6)});
     }
     static __device__ __forceinline__ Word all(float v) { const _Float16 o = (_Float16)v; return Word{o, o, o, o, o, o, o, o}; }
     static __device__ __forceinline__ f32x4 mul(Word a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 template <> struct Operand<__bf16> {
     static constexpr int kPieces = 1;
-    static constexpr float kUp = 65536.f, kMiddle = -128.f;
+    static constexpr float kUp = 65536.f, kMiddle = -16.f;
     typedef bf16x8 Word;
     static __device__ __forceinline__ Word codes(unsigned w) {
-        auto pair = [](unsigned v) { return (v & 0x000f000fu) ^ 0x3b083b08u; };      // (128 + c) / 2^16
-        return __builtin_bit_cast(Word, u32x4{pair(w), pair(w >> 4), pair(w >> 8), pair(w >> 12)});
+        auto pair = [](unsigned v) { return (v & 0x00780078u) ^ 0x39c039c0u; };      // (16 + c) / 2^16
+        return __builtin_bit_cast(Word, u32x4{pair(w << 3), pair(w >> 1), pair(w >> 5), pair(w >> 9)});
     }
     static __device__ __forceinline__ Word all(float v) { const __bf16 o = (__bf16)(v / kUp); return Word{o, o, o, o, o, o, o, o}; }
     static __device__ __forceinline__ f32x4 mul(Word a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
