@@ -97,8 +97,9 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const ProductArgs&
                                              (int)((rows - 1) * (int)a.x_stride * bytes + a.w.n_in * bytes), 0x00027000);
 }
 
-// sum of eight elements
+// sum of eight elements, each divided by kUp before it is added: it may be the largest of its type
 __device__ __forceinline__ float sum_of(const f16x8& v) {
+    static_assert(Operand<_Float16>::kUp == 1.f, "not divided here");
     const f16x2 one{(_Float16)1.f, (_Float16)1.f};
     float s = 0.f;
 #pragma unroll
@@ -108,13 +109,13 @@ __device__ __forceinline__ float sum_of(const f16x8& v) {
 __device__ __forceinline__ float sum_of(const bf16x8& v) {
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += (float)v[i];
+    for (int i = 0; i < 8; ++i) s = __builtin_fmaf((float)v[i], 1.f / Operand<__bf16>::kUp, s);
     return s;
 }
 __device__ __forceinline__ float sum_of(const Eight<float>::Raw& v) {
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += v[i];
+    for (int i = 0; i < 8; ++i) s = __builtin_fmaf(v[i], 1.f / Operand<float>::kUp, s);
     return s;
 }
 

@@ -143,7 +143,7 @@ struct Staged {
                     b.x[0][row][at] = __builtin_bit_cast(u32x4, v[u]);
                 }
                 if constexpr (SUMS) {
-                    const float s = lanes_sum<G / 8>(sum_of(v[u]) * (1.f / Operand<X>::kUp));
+                    const float s = lanes_sum<G / 8>(sum_of(v[u]));
                     if (in && c % (G / 8) == 0) b.sum[c / (G / 8)][row] = s;
                 }
             }
