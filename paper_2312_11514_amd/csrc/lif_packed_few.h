@@ -6,14 +6,14 @@
 // products still cost less than the bytes.  Codes become elements by masks, exactly:
 //   fp16  16 + c is a pattern of bits; so is 1024 + c or 1024 + 16 c, and minus 1032, or times 1/16 minus 72, that is c - 8
 //   bf16  (16 + c) / 2^16 is a pattern of bits
-//   fp32  c - 8 in bf16; x / 2^11 is three bf16 pieces of 8 bits each, which are exact together
+//   fp32  (c - 8) / 2^15 in bf16; x is three bf16 pieces of 8 bits each, which are exact together down to 2^-133
 //   8 bits  16 (c - 8), whole numbers throughout
 // What is too much comes off with the sum of x: little of it, so that a group's sum is not much smaller than what it is rounded as on its way.  (Sums of 11008
 // inputs with a common offset of a fifth of their spread are off by up to 0.8e-6 of them in fp16 and 0.5e-6 in bf16; with 64 + c and 128 + c, an instruction less
 // for eight codes and 0 to 2 % of the time of one row, by 2.8e-6 and 3.7e-6, where one addition after the other in fp32 leaves 2.6e-6.)
 // Every group's sum is fp32 (or whole), and its step and zero point are applied to that: weights are not rounded.
-// bf16 and fp32 rows may be as large as what sums are held in: with 2^-16 or 2^-11 on one side no group's sum is infinite before its step is applied, and an
-// output gets the factor back at its end.
+// bf16 and fp32 rows may be as large as what sums are held in: with 2^-16 or 2^-15 on the codes no group's sum is infinite before its step is applied (128
+// inputs, zero points to 255), and an output gets the factor back at its end.
 //
 // What bounds it, up to 16 rows: the launch and one round trip to memory where the matrix is small (one row of 4096 by 4096, fp16: 3.6 us, 1.8 of them the launch,
 // 4.7 where no cache has the codes), the bytes where it is large (one row by 50001 outputs, groups of 64 with zero points: 19.7 us, 22.5 from memory, 116 MB at
@@ -31,6 +31,7 @@
 namespace lif {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 struct ProductArgs {
     PackedView w;
@@ -69,16 +70,19 @@ template <> struct Operand<__bf16> {
 };
 template <> struct Operand<float> {
     static constexpr int kPieces = 3;
-    static constexpr float kUp = 2048.f, kMiddle = 8.f;
+    static constexpr float kUp = 32768.f, kMiddle = 8.f;
     typedef bf16x8 Word;
     static __device__ __forceinline__ Word codes(unsigned w) {
-        auto pair = [&](int p) {
-            const float a = (float)code_of(w, 2 * p), b = (float)code_of(w, 2 * p + 1);      // no more than 4 bits: the upper half has all of it
-            return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
+        // 16 (c - 8) by bytes of both halves: codes 0, 4, 1, 5 and 2, 6, 3, 7
+        const int low = (int)(w << 4 & 0xf0f0f0f0u), high = (int)(w & 0xf0f0f0f0u);
+        auto byte = [](int v, int i) { return __builtin_bit_cast(unsigned, (float)(signed char)(v >> 8 * i)); };
+        auto pair = [&](int v, int i) {                      // no more than 4 bits: the upper halves have all of it; 19 off each exponent, and 0 stays 0
+            const unsigned both = __builtin_amdgcn_perm(byte(v, i + 2), byte(v, i), 0x07060302u);
+            return __builtin_bit_cast(unsigned, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, both), u16x2{19 << 7, 19 << 7}));
         };
-        return __builtin_bit_cast(Word, u32x4{pair(0), pair(1), pair(2), pair(3)});
+        return __builtin_bit_cast(Word, u32x4{pair(low, 0), pair(high, 0), pair(low, 1), pair(high, 1)});
     }
-    static __device__ __forceinline__ Word all(float v) { const __bf16 o = (__bf16)v; return Word{o, o, o, o, o, o, o, o}; }
+    static __device__ __forceinline__ Word all(float v) { const __bf16 o = (__bf16)(v / kUp); return Word{o, o, o, o, o, o, o, o}; }
     static __device__ __forceinline__ f32x4 mul(Word a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Operand<signed char> {    // 16 (c - 8)
@@ -127,7 +131,7 @@ __device__ __forceinline__ Pieces pieces_of(const Eight<float>::Raw& v) {
     u32x4 w[3];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        float a = v[2 * i] * (1.f / Operand<float>::kUp), b = v[2 * i + 1] * (1.f / Operand<float>::kUp);
+        float a = v[2 * i], b = v[2 * i + 1];
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
             const unsigned ua = __builtin_bit_cast(unsigned, a), ub = __builtin_bit_cast(unsigned, b);

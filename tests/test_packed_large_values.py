@@ -44,3 +44,47 @@ def test_finite_results_of_large_neighbours(rows, dtype, group, zeros):
     got = out.cpu().double().numpy()
     assert np.isfinite(got).all(), np.unique(np.nonzero(~np.isfinite(got))[0])
     assert (np.abs(got - y) <= bound_of(y, size, N_IN, group, dtype)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", ROWS)
+def test_finite_results_of_large_rows_and_zero_points(rows, dtype, group):
+    """Zero points up to 255: a group's sum is up to 128 * 255 times the largest value before its step is applied"""
+    rng = np.random.default_rng(rows + group)
+    codes, step, zero = random_weights(rng, N_OUT, N_IN, group, True)
+    zero = rng.integers(200, 256, zero.shape).astype(np.float64)
+    step = step * 2.0 ** -17                               # answers: up to 712 products of 3.3e38 with 255 * 2^-17 * 1.5 / sqrt(712) = 2.6e37
+    m = packed(codes, step, zero, group, True, dtype)
+    x = large_rows(rng, rows, dtype)
+    out = torch.empty(rows, N_OUT, dtype=DTYPES[dtype], device="cuda")
+    m.multiply(x.cuda(), out)
+    y, size = O.product(x.double().numpy(), codes, step, zero, group, middle=MIDDLE[dtype])
+    assert np.abs(y).max() < 2e38
+    got = out.cpu().double().numpy()
+    assert np.isfinite(got).all(), np.unique(np.nonzero(~np.isfinite(got))[0])
+    assert (np.abs(got - y) <= bound_of(y, size, N_IN, group, dtype)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", ROWS)
+def test_small_rows(rows, dtype, zeros):
+    """Rows of the smallest values: of x nothing above 2^-133 is lost, and of an addition within a group or of an output nothing above 2^-133 times the step
+    (or once)"""
+    rng = np.random.default_rng(rows)
+    group = 64
+    codes, step, zero = random_weights(rng, N_OUT, N_IN, group, zeros)
+    step = step * 2.0 ** 8
+    m = packed(codes, step, zero, group, zeros, dtype)
+    x = torch.from_numpy((rng.standard_normal((rows, N_IN)) * 2.0 ** -122).astype(np.float32)).to(DTYPES[dtype])
+    out = torch.empty(rows, N_OUT, dtype=DTYPES[dtype], device="cuda")
+    m.multiply(x.cuda(), out)
+    y, size = O.product(x.double().numpy(), codes, step, zero, group, middle=MIDDLE[dtype])
+    additions = 3 * group if dtype == "f32" else group     # (three pieces of an fp32 element)
+    lost = step.sum(1) * 2 * additions * 2.0 ** -133 + (step.shape[1] + 24) * 2.0 ** -133
+    lost = lost + np.abs(O.weights_of(codes, step, zero, group)).sum(1) * 2.0 ** -133 * (dtype == "f32")
+    got = out.cpu().double().numpy()
+    assert np.abs(y).mean() > 2.0 ** -113 and (np.abs(got - y) <= bound_of(y, size, N_IN, group, dtype) + lost).all()
