@@ -663,8 +663,8 @@ int lif_packed_dequantize(lif_packed* packed, void* weights, int64_t stride, voi
 /*
  * out[t, n] = sum_k x[t, k] * scale[n, k / group] * (code[n, k] - zero[n, k / group]) + bias[n]
  * Weights are not rounded further: a group's sum is fp32 (whole numbers for rows in 8 bits), scaled, added up in fp32 and rounded once to E.  Sums have a
- * fixed order for a given number of rows.  x_stride is at most 2^22.  In bf16 and fp32 what lies below 2^-133 in x, in its products
- * with whole numbers and in an output may be lost.  A row that holds infinity or NaN, or meets a scale that does, gives infinity or NaN there; other rows do not
+ * fixed order for a given number of rows.  x_stride is at most 2^22.  In bf16, fp32 and 8 bits by groups what lies below 2^-133 in x, in its products with
+ * whole numbers and in an output may be lost.  A row that holds infinity or NaN, or meets a scale that does, gives infinity or NaN there; other rows do not
  * see it.
  */
 int lif_packed_multiply(lif_packed* packed, const lif_packed_rows* rows, void* stream);

@@ -12,8 +12,8 @@
 // inputs with a common offset of a fifth of their spread are off by up to 0.8e-6 of them in fp16 and 0.5e-6 in bf16; with 64 + c and 128 + c, an instruction less
 // for eight codes and 0 to 2 % of the time of one row, by 2.8e-6 and 3.7e-6, where one addition after the other in fp32 leaves 2.6e-6.)
 // Every group's sum is fp32 (or whole), and its step and zero point are applied to that: weights are not rounded.
-// bf16 and fp32 rows may be as large as what sums are held in: with 2^-16 or 2^-15 on the codes no group's sum is infinite before its step is applied (128
-// inputs, zero points to 255), and an output gets the factor back at its end.
+// bf16 and fp32 rows, and rows in 8 bits with scales by groups, may be as large as what sums are held in: with 2^-16 or 2^-15 on the codes, or 2^-20 on the
+// scales, no group's sum is infinite before its step is applied (128 inputs, zero points to 255), and an output gets the factor back at its end.
 //
 // What bounds it, up to 16 rows: the launch and one round trip to memory where the matrix is small (one row of 4096 by 4096, fp16: 3.6 us, 1.8 of them the launch,
 // 4.7 where no cache has the codes), the bytes where it is large (one row by 50001 outputs, groups of 64 with zero points: 19.7 us, 22.5 from memory, 116 MB at
@@ -88,11 +88,13 @@ template <> struct Operand<float> {
 template <> struct Operand<signed char> {    // 16 (c - 8)
     static constexpr float kUp = 0.0625f, kMiddle = 8.f;
 };
-// an element of a row in 8 bits that has a scale for each group of the weights
+// an element of a row in 8 bits that has a scale for each group of the weights: divided by kDown when a group's sum is multiplied by it
 struct ByGroup {
     signed char code;
 };
-template <> struct Operand<ByGroup> : Operand<signed char> {};
+template <> struct Operand<ByGroup> {
+    static constexpr float kUp = 65536.f, kMiddle = 8.f, kDown = 16.f * kUp;
+};
 
 // Rows first .. first + n - 1 of x as a buffer: what lies behind the last of them is 0, and so is every row that is not there.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const ProductArgs& a, int bytes, int first, int n) {
@@ -306,7 +308,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_packed_few(ProductArgs a) {
                 const unsigned word = gw[d / UNIT][v][i];
                 float s = (float)acc[v][i];
                 if constexpr (ZEROS) s = __builtin_fmaf(Operand<X>::kMiddle - zero_of(word), (float)sum[v][i], s);
-                if constexpr (kByGroup) s *= xs[d / UNIT][v];
+                if constexpr (kByGroup) s *= xs[d / UNIT][v] * (1.f / Operand<X>::kDown);
                 y[i] = __builtin_fmaf(step_of(word), s, y[i]);
             }
         }

@@ -152,7 +152,7 @@ struct Staged {
 #pragma unroll
             for (int u = 0; u < kScales; ++u) {
                 const int i = u * THREADS + tid;
-                if (i < S * kRows) b.scale[i / kRows][i % kRows] = scales[u];
+                if (i < S * kRows) b.scale[i / kRows][i % kRows] = scales[u] * (1.f / Operand<X>::kDown);
             }
         }
     }

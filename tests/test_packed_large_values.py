@@ -88,3 +88,29 @@ def test_small_rows(rows, dtype, zeros):
     lost = lost + np.abs(O.weights_of(codes, step, zero, group)).sum(1) * 2.0 ** -133 * (dtype == "f32")
     got = out.cpu().double().numpy()
     assert np.abs(y).mean() > 2.0 ** -113 and (np.abs(got - y) <= bound_of(y, size, N_IN, group, dtype) + lost).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["row", "group"])
+@pytest.mark.parametrize("group,zeros", [(32, False), (64, True), (128, False), (128, True)])
+@pytest.mark.parametrize("rows", ROWS)
+def test_finite_results_of_large_rows_in_8_bits(rows, group, zeros, kind):
+    """Scales up to the largest of an fp32 row, 3.4e38 / 127"""
+    rng = np.random.default_rng(rows + group)
+    codes, step, zero = random_weights(rng, N_OUT, N_IN, group, zeros)
+    if zeros:
+        zero = rng.integers(200, 256, zero.shape).astype(np.float64)
+    step = step * 2.0 ** -17                               # answers: as of test_finite_results_of_large_rows_and_zero_points
+    m = packed(codes, step, zero, group, zeros, "f32")
+    x = rng.integers(90, 128, (rows, N_IN)) * rng.choice([-1, 1], (rows, 1))
+    x[2::4] *= rng.choice([-1, 1], x[2::4].shape)
+    s = (rng.uniform(0.5, 1.0, (rows, step.shape[1] if kind == "group" else 1)) * 2.6e36).astype(np.float32)
+    s[3::4] = 1e-3
+    xs = x * np.repeat(s.astype(np.float64), group if kind == "group" else N_IN, 1)[:, :N_IN]
+    out = torch.empty(rows, N_OUT, device="cuda")
+    m.multiply(torch.from_numpy(x.astype(np.int8)).cuda(), out, scales=torch.from_numpy(s).cuda())
+    y, size = O.product(xs, codes, step, zero, group, middle=MIDDLE["i8"])
+    assert np.abs(y).max() < 2e38
+    got = out.cpu().double().numpy()
+    assert np.isfinite(got).all(), np.unique(np.nonzero(~np.isfinite(got))[0])
+    assert (np.abs(got - y) <= bound_of(y, size, N_IN, group, "f32", True)).all()
