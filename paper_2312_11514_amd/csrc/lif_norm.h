@@ -3,8 +3,8 @@
 //   h = residual + x      RMS  h / sqrt(mean h^2 + eps) * w      LAYER  (h - mean h) / sqrt(var h + eps) * w + b      NONE  h
 //   8 bits: step = max |y| * (1 / 127) (of the row, or of every `group` elements), code = y / step to the nearest whole number
 //
-// A workgroup has one row, in registers.  The sums are fp64 and everything else is a fixed chain of fp32 operations, so that codes do not depend on
-// how a row is dealt to threads.
+// A workgroup has one row, in registers.  The sums are fp64, in an order that the width alone decides, and everything else is a fixed chain of fp32
+// operations: rows and codes do not depend on how many rows there are.
 // What bounds it: one row, the launch (1.8 of 2.5 us, 3.2 in 8 bits) and what a wave does one after the other; many, the bytes: 2048 rows of 4544 in bf16 with a
 // layer norm 16.4 us where the last-level cache has them, 20 from memory (74 MB, 3.7 TB/s of the 5.2 that a large copy reaches; 8 bits 19.5 and 22); 4096 rows of
 // 8192 fp16 48.5 us, 5.5 TB/s.  (With everything in fp64 and a mean of 0 taken off in RMS norms, and codes that compare each element with the half: 2.8, 3.8, 18.4
@@ -27,15 +27,35 @@ struct NormArgs {
 
 constexpr int kNormMaxWaves = 16;
 
-// sum over the workgroup, in every thread, in a fixed order.  `slot` holds a value per wave; every call has slots of its own.
+// Which piece of a row a thread has.  With one or two a thread the order of the sums is the same: pieces 32 apart, within each run of 64 of them, are added
+// first (two lanes of a wave, or one lane's two), then the 32 sums of a run, and then runs by twos, fours and so on (waves, or the halves of one).
+template <int V>
+__device__ __forceinline__ int piece_of(int v, int tid, int threads) {
+    if constexpr (V == 2) return (tid & ~31) * 2 + 32 * v + (tid & 31);
+    return v * threads + tid;
+}
+// Sum over 16 or 32 lanes, by twos, fours and so on; `lane` is the last of them.
+template <int LANES>
+__device__ __forceinline__ double lanes_sum_at(double v, int lane) {
+    v += dpp_from<0x111, 0xf>(v);                            // row_shr:1, 2, 4, 8
+    v += dpp_from<0x112, 0xf>(v);
+    v += dpp_from<0x114, 0xf>(v);
+    v += dpp_from<0x118, 0xf>(v);
+    if constexpr (LANES == 32) v += dpp_from<0x142, 0xa>(v); // row_bcast:15 into rows 1 and 3
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+// Sum over the workgroup of what threads have of V pieces each, in every thread.  `slot` holds a value per wave; every call has slots of its own.
+template <int V>
 __device__ __forceinline__ double block_sum(double v, double* slot, int waves) {
-    v = wave_sum(v);
+    if constexpr (V == 1) v = lanes_sum_at<32>(swap_add<32>(v, v), 31);
+    else v = wave_sum(v);
     if (waves == 1) return v;
-    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) slot[threadIdx.x >> 6] = v;
     lds_barrier();
-    double s = 0;
-    for (int i = 0; i < waves; ++i) s += slot[i];
-    return s;
+    return lanes_sum_at<16>(lane < waves ? slot[lane] : 0., 15);
 }
 __device__ __forceinline__ unsigned block_max(unsigned v, unsigned* slot, int waves) {
     v = lanes_max(v, 64);
@@ -59,45 +79,47 @@ __global__ void k_add_norm(NormArgs a) {
     typename Eight<T>::Raw xs[V], rs[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int at = 8 * (v * threads + tid);
+        const int at = 8 * piece_of<V>(v, tid, threads);
         xs[v] = rs[v] = typename Eight<T>::Raw{};
         if (at < width) {
             xs[v] = Eight<T>::load((const T*)a.x + row * a.x_stride + at);
             if (a.residual) rs[v] = Eight<T>::load((const T*)a.residual + row * a.residual_stride + at);
         }
     }
-    double s = 0;
+    double s = 0, second = 0;                                // of a thread's pieces; with two of them, of the second
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int at = 8 * (v * threads + tid);
+        double& sum = V == 2 && v == 1 ? second : s;
+        const int at = 8 * piece_of<V>(v, tid, threads);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             h[v][e] = a.residual ? (float)rs[v][e] + (float)xs[v][e] : (float)xs[v][e];
-            if constexpr (NORM == 1) s = __builtin_fma((double)h[v][e], (double)h[v][e], s);
-            if constexpr (NORM == 2) s += (double)h[v][e];
+            if constexpr (NORM == 1) sum = __builtin_fma((double)h[v][e], (double)h[v][e], sum);
+            if constexpr (NORM == 2) sum += (double)h[v][e];
         }
         if (a.total && at < width) store_eight<T>((T*)a.total + row * a.total_stride + at, h[v]);
     }
     if constexpr (NORM != 0) {
         if constexpr (NORM == 2) {
-            const double mean = block_sum(s, sums[0], waves) / width;
-            s = 0;
+            const double mean = block_sum<V>(s + second, sums[0], waves) / width;
+            s = second = 0;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                if (8 * (v * threads + tid) < width) {
+                double& sum = V == 2 && v == 1 ? second : s;
+                if (8 * piece_of<V>(v, tid, threads) < width) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const double d = (double)h[v][e] - mean;
                         h[v][e] = (float)d;
-                        s = __builtin_fma(d, d, s);
+                        sum = __builtin_fma(d, d, sum);
                     }
                 }
             }
         }
-        const float inverse = (float)(1.0 / __builtin_sqrt(block_sum(s, sums[1], waves) / width + (double)a.eps));
+        const float inverse = (float)(1.0 / __builtin_sqrt(block_sum<V>(s + second, sums[1], waves) / width + (double)a.eps));
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int at = 8 * (v * threads + tid);
+            const int at = 8 * piece_of<V>(v, tid, threads);
             if (at < width) {
                 float w[8], b[8];
                 if (a.weight) load_floats8(a.weight + at, w);
@@ -115,7 +137,7 @@ __global__ void k_add_norm(NormArgs a) {
     if constexpr (!EIGHT) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int at = 8 * (v * threads + tid);
+            const int at = 8 * piece_of<V>(v, tid, threads);
             if (at < width) store_eight<T>((T*)a.out + row * a.out_stride + at, h[v]);
         }
     } else {
@@ -123,7 +145,7 @@ __global__ void k_add_norm(NormArgs a) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             most[v] = 0;
-            if (8 * (v * threads + tid) < width) {
+            if (8 * piece_of<V>(v, tid, threads) < width) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) most[v] = max(most[v], magnitude_bits(h[v][e]));
             }
@@ -132,7 +154,7 @@ __global__ void k_add_norm(NormArgs a) {
         if (a.group == 0) all = block_max(all, largest, waves);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int at = 8 * (v * threads + tid);
+            const int at = 8 * piece_of<V>(v, tid, threads);
             const unsigned top = a.group ? lanes_max(most[v], a.group / 8) : all;
             const float step = grid_step(__builtin_bit_cast(float, top) * (1.f / 127.f));
             float t[8];
