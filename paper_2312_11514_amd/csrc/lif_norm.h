@@ -5,10 +5,10 @@
 //
 // A workgroup has one row, in registers.  The sums are fp64, in an order that the width alone decides, and everything else is a fixed chain of fp32
 // operations: rows and codes do not depend on how many rows there are.
-// What bounds it: one row, the launch (1.8 of 2.5 us, 3.2 in 8 bits) and what a wave does one after the other; many, the bytes: 2048 rows of 4544 in bf16 with a
-// layer norm 16.4 us where the last-level cache has them, 20 from memory (74 MB, 3.7 TB/s of the 5.2 that a large copy reaches; 8 bits 19.5 and 22); 4096 rows of
-// 8192 fp16 48.5 us, 5.5 TB/s.  (With everything in fp64 and a mean of 0 taken off in RMS norms, and codes that compare each element with the half: 2.8, 3.8, 18.4
-// and 22.4 us.)
+// What bounds it: one row, the launch (1.8 of 2.4 us, 3.2 in 8 bits) and what a wave does one after the other; many, the bytes: 2048 rows of 4544 in bf16 with a
+// layer norm 15.9 us where the last-level cache has them, 20 from memory (74 MB, 3.7 TB/s of the 5.2 that a large copy reaches; 8 bits 18.7 and 22); 4096 rows of
+// 8192 fp16 48.4 us, 5.5 TB/s; 512 rows of 65536 fp32 with a layer norm 113 us, 4.8 TB/s.  (With everything in fp64 and a mean of 0 taken off in RMS norms, and
+// codes that compare each element with the half: 2.8, 3.8, 18.4 and 22.4 us.)
 #pragma once
 
 #include "lif_rows.h"
@@ -76,28 +76,34 @@ __global__ void k_add_norm(NormArgs a) {
     const int tid = threadIdx.x, threads = blockDim.x, waves = threads >> 6, width = a.width;
     const long long row = blockIdx.x;
     float h[V][8];
-    typename Eight<T>::Raw xs[V], rs[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int at = 8 * piece_of<V>(v, tid, threads);
-        xs[v] = rs[v] = typename Eight<T>::Raw{};
-        if (at < width) {
-            xs[v] = Eight<T>::load((const T*)a.x + row * a.x_stride + at);
-            if (a.residual) rs[v] = Eight<T>::load((const T*)a.residual + row * a.residual_stride + at);
-        }
-    }
     double s = 0, second = 0;                                // of a thread's pieces; with two of them, of the second
+    // Pieces on their way at a time: with eight a thread, rows as they come and as fp32 do not fit the 128 registers of 16 waves.
+    constexpr int ASKED = V < 8 ? V : sizeof(T) == 4 ? 2 : 4;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        double& sum = V == 2 && v == 1 ? second : s;
-        const int at = 8 * piece_of<V>(v, tid, threads);
+    for (int first = 0; first < V; first += ASKED) {
+        typename Eight<T>::Raw xs[ASKED], rs[ASKED];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            h[v][e] = a.residual ? (float)rs[v][e] + (float)xs[v][e] : (float)xs[v][e];
-            if constexpr (NORM == 1) sum = __builtin_fma((double)h[v][e], (double)h[v][e], sum);
-            if constexpr (NORM == 2) sum += (double)h[v][e];
+        for (int u = 0; u < ASKED; ++u) {
+            const int at = 8 * piece_of<V>(first + u, tid, threads);
+            xs[u] = rs[u] = typename Eight<T>::Raw{};
+            if (at < width) {
+                xs[u] = Eight<T>::load((const T*)a.x + row * a.x_stride + at);
+                if (a.residual) rs[u] = Eight<T>::load((const T*)a.residual + row * a.residual_stride + at);
+            }
         }
-        if (a.total && at < width) store_eight<T>((T*)a.total + row * a.total_stride + at, h[v]);
+#pragma unroll
+        for (int u = 0; u < ASKED; ++u) {
+            const int v = first + u, at = 8 * piece_of<V>(v, tid, threads);
+            double& sum = V == 2 && v == 1 ? second : s;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[v][e] = a.residual ? (float)rs[u][e] + (float)xs[u][e] : (float)xs[u][e];
+                if constexpr (NORM == 1) sum = __builtin_fma((double)h[v][e], (double)h[v][e], sum);
+                if constexpr (NORM == 2) sum += (double)h[v][e];
+            }
+            if (a.total && at < width) store_eight<T>((T*)a.total + row * a.total_stride + at, h[v]);
+        }
+        if constexpr (ASKED < V) __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (NORM != 0) {
         if constexpr (NORM == 2) {
@@ -106,6 +112,11 @@ __global__ void k_add_norm(NormArgs a) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 double& sum = V == 2 && v == 1 ? second : s;
+                // (widened anew: the compiler would keep what the first sum has made of it, in twice the registers)
+                if constexpr (V == 8) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(h[v][e]));
+                }
                 if (8 * piece_of<V>(v, tid, threads) < width) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
