@@ -27,6 +27,7 @@
 #include <type_traits>
 
 #include "lif_packed.h"
+#include "lif_packed_form.h"
 
 namespace lif {
 
@@ -354,10 +355,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_packed_few(ProductArgs a) {
     }
 }
 
-void launch_product_f32(const ProductArgs& a, bool zeros, hipStream_t s);
-void launch_product_f16(const ProductArgs& a, bool zeros, hipStream_t s);
-void launch_product_bf16(const ProductArgs& a, bool zeros, hipStream_t s);
-void launch_product_i8(const ProductArgs& a, bool zeros, hipStream_t s);
-void launch_product_i8_groups(const ProductArgs& a, bool zeros, hipStream_t s);
+// per type of the rows; false: there is no such form, nothing was launched
+bool launch_product_f32(const ProductArgs& a, PackedForm f, bool zeros, hipStream_t s);
+bool launch_product_f16(const ProductArgs& a, PackedForm f, bool zeros, hipStream_t s);
+bool launch_product_bf16(const ProductArgs& a, PackedForm f, bool zeros, hipStream_t s);
+bool launch_product_i8(const ProductArgs& a, PackedForm f, bool zeros, hipStream_t s);
+bool launch_product_i8_groups(const ProductArgs& a, PackedForm f, bool zeros, hipStream_t s);
 
 }  // namespace lif

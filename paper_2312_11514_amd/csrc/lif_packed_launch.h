@@ -1,4 +1,4 @@
-// Which kernel takes a product.
+// The kernel of a form.
 #pragma once
 
 #include "lif_packed_few.h"
@@ -7,15 +7,16 @@
 
 namespace lif {
 
+// Whether it launched: not every form is compiled for every type and group.
 template <typename X, int G, bool ZEROS>
-void launch_product_form(const ProductArgs& a, hipStream_t s) {
+bool launch_product_form(const ProductArgs& a, PackedForm f, hipStream_t s) {
     const int tiles = (a.w.n_out + kTileOut - 1) / kTileOut;
     constexpr bool kF32 = sizeof(X) == 4;
     constexpr int kWide = kF32 ? 2 : 1;
     auto go = [&](auto kernel, int outs, int rows, int waves) {
         hipLaunchKernelGGL(kernel, dim3((tiles + outs - 1) / outs, (a.rows + rows - 1) / rows), dim3(waves * 64), 0, s, a);
+        return true;
     };
-    const PackedForm f = packed_form(tiles, a.w.in_tiles, a.rows, kF32, G);
     switch (f) {
         case PackedForm::few4: return go(k_packed_few<X, G, ZEROS, 1, 4, 8>, 1, 16, 8);
         case PackedForm::few8: return go(k_packed_few<X, G, ZEROS, 2, 4 / kWide, 8>, 1, 16, 8);
@@ -68,12 +69,14 @@ void launch_product_form(const ProductArgs& a, hipStream_t s) {
             if constexpr (!kF32) return go(k_packed_many<X, G, ZEROS, 3, 7, 2>, 7, 48, 14);
             break;
     }
+    return false;
 }
 template <typename X>
-void launch_product_as(const ProductArgs& a, bool zeros, hipStream_t s) {
-    if (a.w.group == 32) zeros ? launch_product_form<X, 32, true>(a, s) : launch_product_form<X, 32, false>(a, s);
-    else if (a.w.group == 64) zeros ? launch_product_form<X, 64, true>(a, s) : launch_product_form<X, 64, false>(a, s);
-    else zeros ? launch_product_form<X, 128, true>(a, s) : launch_product_form<X, 128, false>(a, s);
+bool launch_product_as(const ProductArgs& a, PackedForm f, bool zeros, hipStream_t s) {
+    if (a.w.group == 32) return zeros ? launch_product_form<X, 32, true>(a, f, s) : launch_product_form<X, 32, false>(a, f, s);
+    if (a.w.group == 64) return zeros ? launch_product_form<X, 64, true>(a, f, s) : launch_product_form<X, 64, false>(a, f, s);
+    if (a.w.group == 128) return zeros ? launch_product_form<X, 128, true>(a, f, s) : launch_product_form<X, 128, false>(a, f, s);
+    return false;
 }
 
 }  // namespace lif

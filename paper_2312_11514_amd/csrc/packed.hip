@@ -230,12 +230,10 @@ int lif_packed_multiply(lif_packed* p, const lif_packed_rows* rows, void* stream
     const ProductArgs a{p->view, static_cast<const char*>(rows->x), static_cast<char*>(rows->out), rows->x_scales, rows->bias, x_stride,
                         rows->out_stride, rows->n_rows, (int32_t)groups, c.dtype};
     hipStream_t s = (hipStream_t)stream;
-    const bool z = c.zeros != 0;
-    if (eight && groups > 1) launch_product_i8_groups(a, z, s);
-    else if (eight) launch_product_i8(a, z, s);
-    else if (c.dtype == LIF_F32) launch_product_f32(a, z, s);
-    else if (c.dtype == LIF_F16) launch_product_f16(a, z, s);
-    else launch_product_bf16(a, z, s);
+    const auto launch = eight && groups > 1 ? launch_product_i8_groups : eight ? launch_product_i8 : c.dtype == LIF_F32 ? launch_product_f32
+                        : c.dtype == LIF_F16 ? launch_product_f16 : launch_product_bf16;
+    const PackedForm form = packed_form(out_tiles(c), p->view.in_tiles, rows->n_rows, !eight && c.dtype == LIF_F32, c.group);
+    if (!launch(a, form, c.zeros != 0, s)) return fail(LIF_HIP_ERROR, "no kernel for this form of product");
     return launched();
 }
 

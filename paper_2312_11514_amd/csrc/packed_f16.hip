@@ -1,5 +1,5 @@
 #include "lif_packed_launch.h"
 
 namespace lif {
-void launch_product_f16(const ProductArgs& a, bool zeros, hipStream_t s) { launch_product_as<_Float16>(a, zeros, s); }
+bool launch_product_f16(const ProductArgs& a, PackedForm f, bool zeros, hipStream_t s) { return launch_product_as<_Float16>(a, f, zeros, s); }
 }  // namespace lif

@@ -1,5 +1,5 @@
 #include "lif_packed_launch.h"
 
 namespace lif {
-void launch_product_i8_groups(const ProductArgs& a, bool zeros, hipStream_t s) { launch_product_as<ByGroup>(a, zeros, s); }
+bool launch_product_i8_groups(const ProductArgs& a, PackedForm f, bool zeros, hipStream_t s) { return launch_product_as<ByGroup>(a, f, zeros, s); }
 }  // namespace lif
