@@ -653,7 +653,8 @@ int lif_packed_quantize(lif_packed* packed, const void* weights, int64_t stride,
 /*
  * (Neither these arrays nor the full weights of the two other calls may overlap the arrays of the matrix.)
  * From codes (device, [n_out x n_in / 2], two in a byte, the lower input in the lower half), scales [n_out x ceil(n_in / group)] fp32, which are
- * rounded to 16 significant bits (fp16 and bf16 values are kept), and zeros [n_out x ceil(n_in / group)], 0..255, NULL if the configuration has none.
+ * rounded to 16 significant bits (fp16 and bf16 values are kept; those below the normal numbers to multiples of 2^-141; what is infinite, or would be, is
+ * not a number), and zeros [n_out x ceil(n_in / group)], 0..255, NULL if the configuration has none.
  */
 int lif_packed_pack(lif_packed* packed, const uint8_t* codes, const float* scales, const uint8_t* zeros, void* stream);
 

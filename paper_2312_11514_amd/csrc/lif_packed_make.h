@@ -101,8 +101,7 @@ __global__ __launch_bounds__(256) void k_packed_pack(PackedView w, const unsigne
             float step = 0.f;
             unsigned zero = 8;
             if (p.in) {
-                const float s = scales[g];
-                step = grid_step(s);
+                step = sixteen_bits(scales[g]);              // (no weight is looked for on its grid: small ones are kept)
                 if (zeros) zero = zeros[g];
             }
             *group_word(w, tile, p.at) = (__builtin_bit_cast(unsigned, step) & ~0xffu) | zero;

@@ -59,12 +59,16 @@ __device__ __forceinline__ unsigned lanes_max(unsigned v, int lanes) {
     return v;
 }
 
-// A step of a grid of whole numbers: fp32 with 16 significant bits, halves up.  (k + 1/2) * step is then exact for |k| <= 127, and which whole number is
-// nearest to v / step can be told exactly, by a comparison.  Steps below 2^-110, where that would end, are 0: everything is 0.  Not finite: NaN.
-__device__ __forceinline__ float grid_step(float v) {
+// fp32 to 16 significant bits, halves up; not finite: NaN.
+__device__ __forceinline__ float sixteen_bits(float v) {
     const unsigned bits = __builtin_bit_cast(unsigned, v);
     if ((bits & 0x7fffffffu) >= 0x7f7fff80u) return __builtin_nanf("");
-    const float s = __builtin_bit_cast(float, (bits + 0x80u) & ~0xffu);
+    return __builtin_bit_cast(float, (bits + 0x80u) & ~0xffu);
+}
+// A step of a grid of whole numbers: (k + 1/2) * step is then exact for |k| <= 127, and which whole number is nearest to v / step can be told exactly, by a
+// comparison.  Steps below 2^-110, where that would end, are 0: everything is 0.
+__device__ __forceinline__ float grid_step(float v) {
+    const float s = sixteen_bits(v);
     return __builtin_fabsf(s) < 0x1p-110f ? 0.f : s;
 }
 
