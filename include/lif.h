@@ -638,7 +638,8 @@ typedef struct lif_packed_rows {
 size_t lif_packed_code_bytes(const lif_packed_config* cfg);
 size_t lif_packed_group_bytes(const lif_packed_config* cfg);
 
-/* As lif_create: validates, enqueues nothing; call lif_packed_quantize or lif_packed_pack first (or fill the arrays with those of an equal handle). */
+/* As lif_create: validates (the two arrays must not overlap), enqueues nothing; call lif_packed_quantize or lif_packed_pack first (or fill the arrays
+ * with those of an equal handle). */
 int lif_packed_create(const lif_packed_config* cfg, const lif_packed_buffers* buf, lif_packed** out);
 int lif_packed_destroy(lif_packed* packed);
 

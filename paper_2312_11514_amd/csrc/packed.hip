@@ -152,6 +152,9 @@ int lif_packed_create(const lif_packed_config* cfg, const lif_packed_buffers* bu
     if (!aligned(buf->codes, 16) || !aligned(buf->groups, 16)) return fail(LIF_INVALID_ARG, "codes and groups must be 16-byte aligned");
     if (buf->code_bytes < lif_packed_code_bytes(cfg) || buf->group_bytes < lif_packed_group_bytes(cfg))
         return fail(LIF_INVALID_ARG, "codes or groups too small");
+    const int64_t code_bytes = (int64_t)lif_packed_code_bytes(cfg), group_bytes = (int64_t)lif_packed_group_bytes(cfg);
+    if (overlap(Span{buf->codes, code_bytes, code_bytes, 1}, Span{buf->groups, group_bytes, group_bytes, 1}))
+        return fail(LIF_INVALID_ARG, "codes and groups must not overlap");
     lif_packed* p = new (std::nothrow) lif_packed;
     if (!p) return fail(LIF_INVALID_ARG, "out of host memory");
     p->cfg = *cfg;
