@@ -19,8 +19,8 @@ from . import binding as _b
 from .binding import LIF_INVALID_ARG, LifError
 
 # lif_norm_rows and lif_packed_rows, filled in one go; the bytes themselves are the argument, so that threads share none
-_NORM, _PRODUCT = struct.Struct("@7P4q5if"), struct.Struct("@4P2q2i")
-assert _NORM.size == C.sizeof(_b.LifNormRows) and _PRODUCT.size == C.sizeof(_b.LifPackedRows)
+_NORM, _PRODUCT, _CONFIG = struct.Struct("@7P4q5if"), struct.Struct("@4P2q2i"), struct.Struct("@5i")
+assert _NORM.size == C.sizeof(_b.LifNormRows) and _PRODUCT.size == C.sizeof(_b.LifPackedRows) and _CONFIG.size == C.sizeof(_b.LifPackedConfig)
 
 
 def _refuse(message):
@@ -104,9 +104,13 @@ def add_norm(x, out, *, norm=_b.NORM_RMS, eps=1e-5, weight=None, bias=None, resi
         r_ptr, r_stride = residual.data_ptr(), _like(residual, shape, dtype, device, "residual")
     if total is not None:
         t_ptr, t_stride = total.data_ptr(), _like(total, shape, dtype, device, "total")
-    rc = _Torch.add_norm(_NORM.pack(x.data_ptr(), r_ptr, t_ptr, out.data_ptr(), s_ptr, _floats(weight, width, device, "weight") if weight is not None else 0,
-                                    _floats(bias, width, device, "bias") if bias is not None else 0, _stride(x, "x"), r_stride, t_stride, out_stride,
-                                    rows, width, code, norm, group, eps), _b._stream())
+    w_ptr, b_ptr = _floats(weight, width, device, "weight") if weight is not None else 0, _floats(bias, width, device, "bias") if bias is not None else 0
+    try:
+        args = _NORM.pack(x.data_ptr(), r_ptr, t_ptr, out.data_ptr(), s_ptr, w_ptr, b_ptr, _stride(x, "x"), r_stride, t_stride, out_stride, rows, width, code,
+                          norm, group, eps)
+    except (struct.error, OverflowError) as e:
+        _refuse(f"the number of rows, norm, group or eps: {e}")
+    rc = _Torch.add_norm(args, _b._stream())
     if rc:
         _b._check(rc)
 
@@ -124,7 +128,10 @@ class PackedLinear:
         if dtype not in _Torch.types:
             _refuse("dtype must be f32, f16 or bf16")
         self.tdtype = _Torch.types[dtype]
-        self.cfg = _b.LifPackedConfig(n_out, n_in, group, int(bool(zeros)), _Torch.codes[self.tdtype])
+        try:                                               # (ctypes takes numbers of more bits for others)
+            self.cfg = _b.LifPackedConfig.from_buffer_copy(_CONFIG.pack(n_out, n_in, group, int(bool(zeros)), _Torch.codes[self.tdtype]))
+        except struct.error as e:
+            _refuse(f"configuration: {e}")
         code_bytes, group_bytes = self.lib.lif_packed_code_bytes(C.byref(self.cfg)), self.lib.lif_packed_group_bytes(C.byref(self.cfg))
         if code_bytes == 0:
             _refuse("configuration rejected by lif_packed_code_bytes")
@@ -194,8 +201,11 @@ class PackedLinear:
                 x_group, s_ptr = self.group, _floats(scales, rows * groups, device, "scales")
             else:
                 s_ptr = _floats(scales, rows, device, "scales")
-        rc = _Torch.multiply(self.handle, _PRODUCT.pack(
-            x.data_ptr(), s_ptr, _floats(bias, self.n_out, device, "bias") if bias is not None else 0, out.data_ptr(), _stride(x, "x"),
-            _like(out, (*shape[:-1], self.n_out), dtype, device, "out"), rows, x_group), _b._stream())
+        b_ptr, out_stride = _floats(bias, self.n_out, device, "bias") if bias is not None else 0, _like(out, (*shape[:-1], self.n_out), dtype, device, "out")
+        try:
+            args = _PRODUCT.pack(x.data_ptr(), s_ptr, b_ptr, out.data_ptr(), _stride(x, "x"), out_stride, rows, x_group)
+        except struct.error as e:
+            _refuse(f"the number of rows: {e}")
+        rc = _Torch.multiply(self.handle, args, _b._stream())
         if rc:
             _b._check(rc)
