@@ -176,6 +176,8 @@ class PackedLinear:
         self._here()
         for t, dtype, columns, what in ((codes, _Torch.uint8, self.n_in // 2, "codes"), (scales, _Torch.float32, self.row_groups, "scales"),
                                         (zeros, _Torch.uint8, self.row_groups, "zeros")):
+            if t is None and what != "zeros":
+                _refuse(f"{what} must be given")
             if t is not None and (t.dtype is not dtype or t.shape != (self.n_out, columns) or t.get_device() != self._gpu or not t.is_contiguous()):
                 _refuse(f"{what} must be a contiguous {dtype} tensor [{self.n_out}, {columns}] beside the matrix")
         _b._check(self.lib.lif_packed_pack(self.handle, codes.data_ptr(), scales.data_ptr(), _b._ptr(zeros), _b._stream()))

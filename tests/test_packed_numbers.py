@@ -66,3 +66,14 @@ def test_rows_of_a_product(on_a_gpu):
     m.n_out, m.n_in, m.group, m.row_groups, m.tdtype, m._gpu, m.handle = 16, 8, 32, 1, torch.float16, 0, None
     with pytest.raises(lif.LifError):
         m.multiply(Rows(1 << 31, 8, torch.float16), Rows(1 << 31, 16, torch.float16))
+
+
+@pytest.mark.parametrize("codes,scales", [(None, torch.ones(16, 1)), (torch.zeros(16, 4, dtype=torch.uint8), None)])
+def test_codes_and_scales_are_no_options(on_a_gpu, monkeypatch, codes, scales):
+    m = object.__new__(lif.PackedLinear)
+    m.n_out, m.n_in, m.group, m.row_groups, m.tdtype, m._gpu, m.handle = 16, 8, 32, 1, torch.float16, 0, None
+    for t in (codes, scales):
+        if t is not None:
+            monkeypatch.setattr(t, "get_device", lambda: 0, raising=False)
+    with pytest.raises(lif.LifError, match="must be given"):
+        m.pack(codes, scales)
