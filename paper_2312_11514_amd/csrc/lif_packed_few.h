@@ -4,13 +4,14 @@
 //
 // A tile of 16 outputs is one operand, 16 rows of x the other, and the lane (r, q) gets row r of the outputs 4 q .. 4 q + 3: with one row in use of 16 the
 // products still cost less than the bytes.  Codes become elements by masks, exactly:
-//   fp16  16 + c is a pattern of bits; so is 1024 + c or 1024 + 16 c, and minus 1032, or times 1/16 minus 72, that is c - 8
+//   fp16  64 + c is a pattern of bits, an instruction further 16 + c; so is 1024 + c or 1024 + 16 c, and minus 1032, or times 1/16 minus 72, that is c - 8
 //   bf16  (16 + c) / 2^16 is a pattern of bits
 //   fp32  (c - 8) / 2^15 in bf16; x is three bf16 pieces of 8 bits each, which are exact together down to 2^-133
 //   8 bits  16 (c - 8), whole numbers throughout
-// What is too much comes off with the sum of x: little of it, so that a group's sum is not much smaller than what it is rounded as on its way.  (Sums of 11008
-// inputs with a common offset of a fifth of their spread are off by up to 0.8e-6 of them in fp16 and 0.5e-6 in bf16; with 64 + c and 128 + c, an instruction less
-// for eight codes and 0 to 2 % of the time of one row, by 2.8e-6 and 3.7e-6, where one addition after the other in fp32 leaves 2.6e-6.)
+// What is too much comes off with the sum of x: little of it, so that a group's sum is not much smaller than what it is rounded as on its way, by 32 inputs in
+// turn without zero points, by the group with them.  Of 11008 inputs with a common offset of a fifth of their spread sums are off by up to 1.0e-6 of them in
+// fp16, 1.6e-6 with zero points in groups of 64, 0.8e-6 in groups of 128, where codes are 16 + c; 0.5e-6 in bf16.  One addition after the other in fp32 leaves
+// 2.6e-6.  (64 + c and 128 + c throughout: 2.8e-6 and 3.7e-6.  16 + c in fp16 throughout: at most 0.8e-6, but one row by 50001 outputs 22.4 us instead of 21.9.)
 // Every group's sum is fp32 (or whole), and its step and zero point are applied to that: weights are not rounded.
 // bf16 and fp32 rows, and rows in 8 bits with scales by groups, may be as large as what sums are held in: with 2^-16 or 2^-15 on the codes, or 2^-20 on the
 // scales, no group's sum is infinite before its step is applied (128 inputs, zero points to 255), and an output gets the factor back at its end.
@@ -18,7 +19,7 @@
 // What bounds it, up to 16 rows: the launch and one round trip to memory where the matrix is small (one row of 4096 by 4096, fp16: 3.6 us, 1.8 of them the launch,
 // 4.7 where no cache has the codes), the bytes where it is large (one row by 50001 outputs, groups of 64 with zero points: 19.7 us, 22.5 from memory, 116 MB at
 // 5.1 TB/s of the 6.3 that a plain read reaches), and between them what a tile costs in instructions: a SIMD issues one in four cycles, and the bytes of a tile
-// take a compute unit 100 cycles.  So codes take eight instructions for eight of them, the offset of their patterns comes off on the matrix cores, which have
+// take a compute unit 100 cycles.  So codes take seven or eight instructions for eight of them, the offset of their patterns comes off on the matrix cores, which have
 // the time, and groups stand side by side in columns that rows have no use for (with an addition for every two codes and steps group by group 27 us instead of
 // 19.9).  16 rows by 11008 outputs: 9.1 us, 11.6 from memory.  fp32 pays for its conversions: 8 rows of 2560 by 10240, groups of 32: 11 us for 16 MB.
 // Four waves instead of eight: the same for 50001 outputs, 3.7 us instead of 3.55 for 4096; sixteen: 30 and 4.1.
@@ -49,11 +50,11 @@ template <typename X> struct Operand;
 template <> struct Operand<_Float16> {
     static constexpr int kPieces = 1;
     static constexpr float kUp = 1.f;        // what an output is multiplied by at its end
-    static constexpr float kMiddle = -16.f;  // the code that counts 0
+    static constexpr float kMiddle = -64.f;  // the code that counts 0
     typedef f16x8 Word;
     static __device__ __forceinline__ Word codes(unsigned w) {
-        auto pair = [](unsigned v) { return (v & 0x03c003c0u) ^ 0x4e004e00u; };
-        return __builtin_bit_cast(Word, u32x4{pair(w << 6), pair(w << 2), pair(w >> 2), pair(w >> 6)});
+        auto pair = [](unsigned v) { return (v & 0x00f000f0u) ^ 0x54805480u; };
+        return __builtin_bit_cast(Word, u32x4{pair(w << 4), pair(w), pair(w >> 4), pair(w >> 8)});
     }
     static __device__ __forceinline__ Word all(float v) { const _Float16 o = (_Float16)v; return Word{o, o, o, o, o, o, o, o}; }
     static __device__ __forceinline__ f32x4 mul(Word a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -95,6 +96,16 @@ struct ByGroup {
 };
 template <> struct Operand<ByGroup> {
     static constexpr float kUp = 65536.f, kMiddle = 8.f, kDown = 16.f * kUp;
+};
+
+// The same for a group and its zero points.
+template <typename X, int G, bool ZEROS> struct Near : Operand<X> {};
+template <> struct Near<_Float16, 128, true> : Operand<_Float16> {
+    static constexpr float kMiddle = -16.f;
+    static __device__ __forceinline__ Word codes(unsigned w) {
+        auto pair = [](unsigned v) { return (v & 0x03c003c0u) ^ 0x4e004e00u; };
+        return __builtin_bit_cast(Word, u32x4{pair(w << 6), pair(w << 2), pair(w >> 2), pair(w >> 6)});
+    }
 };
 
 // Rows first .. first + n - 1 of x as a buffer: what lies behind the last of them is 0, and so is every row that is not there.
@@ -285,7 +296,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_packed_few(ProductArgs a) {
                     }
                 }
             } else {
-                using O = Operand<X>;
+                using O = Near<X, G, ZEROS>;
 #pragma unroll
                 for (int j = s * PER; j < (s + 1) * PER; ++j) {
                     const auto c = O::codes(tile[d][j]);
@@ -308,7 +319,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_packed_few(ProductArgs a) {
             for (int i = 0; i < 4; ++i) {
                 const unsigned word = gw[d / UNIT][v][i];
                 float s = (float)acc[v][i];
-                if constexpr (ZEROS) s = __builtin_fmaf(Operand<X>::kMiddle - zero_of(word), (float)sum[v][i], s);
+                if constexpr (ZEROS) s = __builtin_fmaf(Near<X, G, ZEROS>::kMiddle - zero_of(word), (float)sum[v][i], s);
                 if constexpr (kByGroup) s *= xs[d / UNIT][v] * (1.f / Operand<X>::kDown);
                 y[i] = __builtin_fmaf(step_of(word), s, y[i]);
             }

@@ -17,10 +17,10 @@ namespace lif {
 
 // The codes as they come, where the sum of x is taken off anyway; in fp16 without zero points c - 8 itself, from which nothing has to be.  (With zero points
 // c itself, two instructions more for a pair: 777 rows by 4096 50 us instead of 48.)
-template <typename X, bool ZEROS>
-struct Exact : Operand<X> {};
-template <>
-struct Exact<_Float16, false> {
+template <typename X, int G, bool ZEROS>
+struct Exact : Near<X, G, ZEROS> {};
+template <int G>
+struct Exact<_Float16, G, false> {
     static constexpr float kMiddle = 8.f;
     static __device__ __forceinline__ f16x8 codes(unsigned w) {
         const unsigned u = w >> 8;
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(64 * WN * WK, 4) void k_packed_many(ProductArgs a) 
     constexpr int S = kTileIn / G, PER = 4 / S, THREADS = 64 * WN;
     constexpr bool kBytes = sizeof(X) == 1, kByGroup = std::is_same_v<X, ByGroup>;
     // What codes are off by comes off with the sum of x, once per group, or on the matrix cores, once per word: in groups of one word these have the time.
-    constexpr bool kOff = !ZEROS && Exact<X, ZEROS>::kMiddle != 8.f, kShift = kOff && PER == 1, kSums = ZEROS || (kOff && !kShift);
+    constexpr bool kOff = !ZEROS && Exact<X, G, ZEROS>::kMiddle != 8.f, kShift = kOff && PER == 1, kSums = ZEROS || (kOff && !kShift);
     using Stage = Staged<X, G, kSums, NT, THREADS>;
     union Shared {
         typename Stage::Buffer x[WK][2];
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(64 * WN * WK, 4) void k_packed_many(ProductArgs a) 
                 using O = Operand<X>;
 #pragma unroll
                 for (int j = s * PER; j < (s + 1) * PER; ++j) {
-                    const typename O::Word c = Exact<X, ZEROS>::codes(tile[d][j]);
+                    const typename O::Word c = Exact<X, G, ZEROS>::codes(tile[d][j]);
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(64 * WN * WK, 4) void k_packed_many(ProductArgs a) 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 step[i] = step_of(gw[d][s][i]);
-                off[i] = Exact<X, ZEROS>::kMiddle - (ZEROS ? zero_of(gw[d][s][i]) : 8.f);
+                off[i] = Exact<X, G, ZEROS>::kMiddle - (ZEROS ? zero_of(gw[d][s][i]) : 8.f);
             }
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
