@@ -189,7 +189,7 @@ void launch_add_norm_pieces(const NormArgs& a, int threads, hipStream_t s) {
     else a.norm == 0 ? go(k_add_norm<T, V, false, 0>) : a.norm == 1 ? go(k_add_norm<T, V, false, 1>) : go(k_add_norm<T, V, false, 2>);
 }
 // Few rows last as long as one of them: a piece a thread (one row of 4096, fp16: 2.5 us, with two 2.7, with eight 5.5).  Many are bound by what all threads
-// do together, and two pieces a thread share sums and barriers (2048 rows of 4544, bf16, layer norm: 17.5 us with one, 16.4 with two, 17.1 with four).
+// do together, and two pieces a thread share sums and barriers (2048 rows of 4544, bf16, layer norm: 17.5 us with one, 15.9 with two, 17.1 with four).
 template <typename T>
 void launch_add_norm_as(const NormArgs& a, hipStream_t s) {
     const int pieces = a.width / 8;

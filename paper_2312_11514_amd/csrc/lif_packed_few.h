@@ -17,11 +17,11 @@
 // scales, no group's sum is infinite before its step is applied (128 inputs, zero points to 255), and an output gets the factor back at its end.
 //
 // What bounds it, up to 16 rows: the launch and one round trip to memory where the matrix is small (one row of 4096 by 4096, fp16: 3.6 us, 1.8 of them the launch,
-// 4.7 where no cache has the codes), the bytes where it is large (one row by 50001 outputs, groups of 64 with zero points: 19.7 us, 22.5 from memory, 116 MB at
-// 5.1 TB/s of the 6.3 that a plain read reaches), and between them what a tile costs in instructions: a SIMD issues one in four cycles, and the bytes of a tile
+// 4.8 where no cache has the codes), the bytes where it is large (one row by 50001 outputs, groups of 64 with zero points: 19.2 us, 22.3 from memory, 116 MB at
+// 5.2 TB/s of the 6.3 that a plain read reaches), and between them what a tile costs in instructions: a SIMD issues one in four cycles, and the bytes of a tile
 // take a compute unit 100 cycles.  So codes take seven or eight instructions for eight of them, the offset of their patterns comes off on the matrix cores, which have
 // the time, and groups stand side by side in columns that rows have no use for (with an addition for every two codes and steps group by group 27 us instead of
-// 19.9).  16 rows by 11008 outputs: 9.1 us, 11.6 from memory.  fp32 pays for its conversions: 8 rows of 2560 by 10240, groups of 32: 11 us for 16 MB.
+// 19.9).  16 rows by 11008 outputs: 9.0 us, 11.6 from memory.  fp32 pays for its conversions: 8 rows of 2560 by 10240, groups of 32: 10.5 us for 16 MB.
 // Four waves instead of eight: the same for 50001 outputs, 3.7 us instead of 3.55 for 4096; sixteen: 30 and 4.1.
 #pragma once
 

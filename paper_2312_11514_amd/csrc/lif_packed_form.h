@@ -13,7 +13,9 @@ enum class PackedForm { few4, few8, few16, outs32_rows16, outs32_rows16_16, outs
 // first of them (outs128_rows64: 256 workgroups 28.4 us, 258 42.8, 512 45.0): us for 4096 inputs in fp16 with groups of 128, in fp32 with groups of 64 and zero
 // points, from 17 to 1024 rows by 1024 to 50000 outputs.  More than 8 waves begin and add up half a microsecond later, whatever the inputs; but for that other
 // inputs, types and groups scale the times alike.  Widths of 48, 80, 96 and 112 outputs are there for what 64 and 128 leave idle (48 rows by 18176, bytes with scales
-// by groups: 284 workgroups of 64 outputs 30.9 us, 228 of 80 24.7), more waves for long inputs (60 rows of 11008 by 4096, bf16, groups of 32: 8 waves 22.5, 16 19.3).
+// by groups of 64: outs80_rows64 24, the next one 26; 24 rows by 11008, fp16: outs48_rows32 9.6, 10.3; 32 by 18176, fp16: outs96_rows32 15.3, 17.2; 256 by 11008, bf16,
+// groups of 32: outs96_rows64 58, 64; 48 by 22016, fp16, groups of 64: outs112_rows48 21.8, 22.8), more waves for long inputs (60 rows of 11008 by 4096, bf16, groups
+// of 32: 8 waves 22.9, 16 21).
 // Against the fastest of these forms the rule's choice loses 0.6 % on average and 6 % at most in fp16, 0.7 and 9 % in bf16 with groups of 32, 1.6 and 20 % in bytes
 // with scales by groups of 64 (1024, 4096 and 11008 inputs), 0.3 and 3 % in fp32.
 // E.g. 4096 outputs, fp16: 24 rows 5.7 (few16 6.0, outs64_rows32_16 9.3), 128 rows 10.4 (outs32_rows16 14.0, outs64_rows64 15.8), 512 rows 28.5 (outs64_rows32

@@ -6,9 +6,9 @@
 //
 // What bounds it: the instructions of a SIMD.  By measurement a matrix instruction takes two issue slots of four cycles of the sixteen that it works, an
 // arithmetic one about one, a read of LDS two, and a wave alone has one slot in two; with 64 rows there are four arithmetic instructions and one read to a
-// matrix instruction, with 16 rows nine.  1024 rows of 4096 by 11008, fp16: 130 us, 0.71 PFLOP/s of the 1.37 that a library's large product reaches; rows in 8 bits
-// 92 us, 1.0 PFLOP/s; 777 rows by 4096 with zero points 48 us (0.54; a library's fp16 product of these sizes 42); 48 rows in 8 bits with scales by groups by 18176
-// outputs 27 us; 64 rows by 4096 7.8 us, 60 rows of 11008 in groups of 32, bf16, 20 us.
+// matrix instruction, with 16 rows nine.  1024 rows of 4096 by 11008, fp16: 128 to 139 us, 0.66 to 0.72 PFLOP/s of the 1.37 that a library's large product
+// reaches; rows in 8 bits 94 us, 1.0 PFLOP/s; 777 rows by 4096 with zero points 48 to 49 us (0.53; a library's fp16 product of these sizes 42); 48 rows of 4544 in
+// 8 bits with scales by groups by 18176 outputs 26 us; 64 rows by 4096 8.1 us, 60 rows of 11008 in groups of 32, bf16, 20 to 21 us.
 #pragma once
 
 #include "lif_packed_few.h"
