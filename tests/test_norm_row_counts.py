@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import paper_2312_11514_amd as lif
-from tests.packed_harness import DTYPES, NORMS
+from oracle import packed_oracle as O
+from tests.packed_harness import DTYPES, NORMS, values
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +33,21 @@ def test_rows_of_outliers(dtype, width, norm):
     for first, last in ((0, 1), (1, 1024), (1024, 1500)):
         call(x[first:last], some[first:last], scales=other[first:last])
     assert torch.equal(some, codes) and torch.equal(other, scales)
+
+
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+@pytest.mark.parametrize("rows,width", [(1030, 8), (1030, 40), (1030, 136), (1030, 264), (1030, 520), (1030, 1288), (1030, 4544), (1030, 8200), (2, 40008), (3, 65536)])
+def test_codes_of_many_rows_and_of_wide_ones_bit_for_bit(rows, width, group):
+    """Two pieces of a row to a thread, and eight"""
+    for i, (dtype, norm) in enumerate([("f32", "layer"), ("bf16", "rms"), ("f16", "none")]):
+        rng = np.random.default_rng(width + group + i)
+        (x, xs), (r, rs) = values(rng, (rows, width), dtype), values(rng, (rows, width), dtype, 3.0)
+        w, b = rng.uniform(0.5, 1.5, width).astype(np.float32), rng.standard_normal(width).astype(np.float32) if norm == "layer" else None
+        out, total = torch.empty(rows, width, dtype=torch.int8, device="cuda"), r.cuda()
+        scales = torch.empty(rows, -(-width // group) if group else 1, device="cuda")
+        lif.add_norm(x.cuda(), out, norm=NORMS[norm], weight=torch.from_numpy(w).cuda(), bias=torch.from_numpy(b).cuda() if b is not None else None,
+                     residual=total, total=total, scales=scales, group=group)
+        h, y = O.sum_and_norm(xs, rs, norm, 1e-5, w if norm != "none" else None, b)
+        codes, step = O.rows_in_8_bits(y, group)
+        assert np.array_equal(scales.cpu().double().numpy(), step) and np.array_equal(out.cpu().numpy(), codes)
+        assert torch.equal(total.cpu(), torch.from_numpy(h).to(DTYPES[dtype]))
